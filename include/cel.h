@@ -15,6 +15,11 @@
  *   cel_order_place  Order-Place baseline placement               (Section 5.2, 6.2.2)
  *   cel_comm_sums    the parts of the comm/compute ratio CCR      (Section 5.1.1, eq. 1)
  *
+ * and of operations of a transformer training step, which a user runs to
+ * measure the costs that the graph's nodes carry (Section 4.2.1):
+ *
+ *   cel_attention, cel_attention_grad  causal attention over a packed batch
+ *
  * Conventions (all entry points):
  *  - Arrays are DEVICE pointers owned by the caller unless marked (host).  The
  *    library never frees or keeps a caller pointer after it returns.
@@ -31,6 +36,11 @@
  *    makespan (eq. 7).  All results are exact integers, hence deterministic.
  *  - Return value: CEL_OK or a negative CEL_E_* code; cel_last_error() gives a
  *    message for the calling thread.  Outputs are unspecified after an error.
+ *  - The operations of a training step (cel_attention and the entry points
+ *    behind it) only enqueue their work on `stream` and return: they read
+ *    nothing back, take their scratch memory from the caller, and may be
+ *    captured into a graph.  What they cannot check without reading device
+ *    memory is defined for every content of it.
  *  - Calls on the same device may run concurrently on different streams.  The
  *    stretches of a call that spread one kernel over the whole GPU take turns
  *    between host threads; a call that has waited a second for its turn goes
@@ -322,6 +332,57 @@ int cel_makespan_model(const cel_graph *g, const cel_devices *d, const cel_heter
  * Errors: CEL_E_ARG, CEL_E_ORDER, CEL_E_HIP, CEL_E_NOMEM. */
 int cel_colocate(const cel_graph *g, const int32_t *order, const int32_t *group,
                  int32_t n_groups, int32_t K, uint8_t *node_dev, hipStream_t stream);
+
+/* Element types of the training-step operations. */
+enum { CEL_BF16 = 0, CEL_F16 = 1, CEL_F32 = 2 };
+
+/* A [tokens][heads][dim] view of device memory: element (t, h, c) lies at
+ * p + t * row + h * head + c (strides in elements, >= 0).  The address is a
+ * multiple of 16 bytes and both strides are multiples of 8; row <= 2^23. */
+typedef struct {
+  void *p;
+  int64_t row, head;
+} cel_rows;
+
+/* A packed batch and its attention: n_seq sequences one behind the other,
+ * sequence s the tokens seq_ptr[s] .. seq_ptr[s + 1] - 1 (device int32
+ * [n_seq + 1], non-decreasing, within 0 .. tokens; equal entries are an empty
+ * sequence).  Tokens before the first and behind the last sequence belong to
+ * none.  A seq_ptr that decreases or leaves 0 .. tokens gives unspecified
+ * results, without an access outside the arrays. */
+typedef struct {
+  int32_t type;                  /* of all rows: CEL_BF16 or CEL_F16 */
+  int32_t tokens, n_seq;         /* >= 0 */
+  int32_t heads, kv_heads, dim;  /* heads a multiple of kv_heads: query head h reads key/value
+                                  * head h / (heads / kv_heads); dim 8, 16, ... 128 */
+  float scale;                   /* of the scores, > 0 (usually 1 / sqrt(dim)) */
+  const int32_t *seq_ptr;
+  cel_rows q, k, v;              /* q: heads; k, v: kv_heads; read-only */
+} cel_attn;
+
+/* Causal attention: token i sees the tokens j <= i of its own sequence.
+ *   s_ij = scale <q_i, k_j>;  lse_i = log sum_j exp s_ij
+ *   out_i = sum_j exp(s_ij - lse_i) v_j
+ * A token of no sequence has out = 0 and lse = -infinity.  What a token does
+ * not see does not reach it, be it an infinity or NaN.  Sums and statistics
+ * are 32 bit; the weights are rounded to the rows' type as matrix operands.
+ * Outputs: out (a view with `heads` heads), lse float [heads][tokens]; they
+ * overlap no input.
+ * Errors: CEL_E_ARG, CEL_E_HIP. */
+int cel_attention(const cel_attn *a, const cel_rows *out, float *lse, hipStream_t stream);
+
+/* The gradient of cel_attention: of out's gradient dout, with out and lse as
+ * that call gave them for the same descriptor.  With p_ij = exp(s_ij - lse_i)
+ * and ds_ij = p_ij (<dout_i, v_j> - <dout_i, out_i>):
+ *   dq_i = scale sum_j ds_ij k_j;  dk_j = scale sum_i ds_ij q_i;  dv_j = sum_i p_ij dout_i
+ * dk and dv sum over the query heads of their key/value head, in a fixed
+ * order: the same inputs give the same bits.  A token of no sequence has
+ * gradients of 0.  delta: scratch, float [heads][tokens].
+ * Outputs: dq (heads), dk, dv (kv_heads); they overlap no input nor each other.
+ * Errors: CEL_E_ARG, CEL_E_HIP. */
+int cel_attention_grad(const cel_attn *a, const cel_rows *out, const float *lse, const cel_rows *dout,
+                       float *delta, const cel_rows *dq, const cel_rows *dk, const cel_rows *dv,
+                       hipStream_t stream);
 
 /* Diagnostics: per-kernel device time.  After cel_timing(1), every call
  * records a pair of HIP events on its stream around each of its main kernel

@@ -8,6 +8,7 @@ stream.  There is no CPU fallback: a missing library or a failed call raises.
 from __future__ import annotations
 
 import ctypes as C
+import math
 import os
 from dataclasses import dataclass
 
@@ -23,7 +24,8 @@ CLUSTER_DP, CLUSTER_GREEDY = 0, 1
 EXPORTS = ("cel_topo_levels", "cel_blevel", "cel_cpd_order", "cel_dfs_order", "cel_cluster", "cel_place", "cel_place_ext", "cel_makespan", "cel_makespan_noalloc",
            "cel_makespan_info", "cel_makespan_blocks_info", "cel_makespan_relax", "cel_blevel_info", "cel_policy_iteration",
            "cel_topo_levels_info", "cel_cluster_info",
-           "cel_order_place", "cel_comm_sums", "cel_makespan_model", "cel_colocate", "cel_step_latency", "cel_timing", "cel_kernel_stats", "cel_last_error", "cel_version")
+           "cel_order_place", "cel_comm_sums", "cel_makespan_model", "cel_colocate",
+           "cel_attention", "cel_attention_grad", "cel_step_latency", "cel_timing", "cel_kernel_stats", "cel_last_error", "cel_version")
 
 
 class CelError(RuntimeError):
@@ -47,6 +49,17 @@ class _Hetero(C.Structure):
 class _Devices(C.Structure):
     _fields_ = [("D", C.c_int32), ("cap", C.POINTER(C.c_int64)),
                 ("bw", C.c_int64), ("lat", C.c_int64)]
+
+
+class _Rows(C.Structure):
+    _fields_ = [("p", C.c_void_p), ("row", C.c_int64), ("head", C.c_int64)]
+
+
+class _Attn(C.Structure):
+    _fields_ = [("type", C.c_int32), ("tokens", C.c_int32), ("n_seq", C.c_int32),
+                ("heads", C.c_int32), ("kv_heads", C.c_int32), ("dim", C.c_int32),
+                ("scale", C.c_float), ("seq_ptr", C.c_void_p),
+                ("q", _Rows), ("k", _Rows), ("v", _Rows)]
 
 
 _lib = None
@@ -76,11 +89,14 @@ def lib() -> C.CDLL:
         L.cel_comm_sums.argtypes = [G, Dv, vp, C.POINTER(i64), C.POINTER(i64), vp]
         L.cel_makespan_model.argtypes = [G, Dv, C.POINTER(_Hetero), vp, i32, vp, i32, vp, vp, vp, vp]
         L.cel_colocate.argtypes = [G, vp, vp, i32, i32, vp, vp]
+        At, Ro = C.POINTER(_Attn), C.POINTER(_Rows)
+        L.cel_attention.argtypes = [At, Ro, vp, vp]
+        L.cel_attention_grad.argtypes = [At, Ro, vp, Ro, vp, Ro, Ro, Ro, vp]
         for f in ("cel_topo_levels", "cel_blevel", "cel_cluster", "cel_place", "cel_place_ext",
                   "cel_makespan",
                   "cel_makespan_noalloc",
                   "cel_cpd_order", "cel_dfs_order", "cel_order_place", "cel_comm_sums", "cel_makespan_model",
-                  "cel_colocate", "cel_version"):
+                  "cel_colocate", "cel_attention", "cel_attention_grad", "cel_version"):
             getattr(L, f).restype = C.c_int
         L.cel_last_error.argtypes = []
         L.cel_last_error.restype = C.c_char_p
@@ -464,3 +480,110 @@ def makespan(g: Graph, d: Devices, order, level, level_ptr, n_levels, node_dev, 
     if want_times:
         st, fi = st[:, :n], fi[:, :n]
     return ms, st, fi
+
+
+# ---------------------------------------------- operations of a training step
+# They enqueue their work on the current stream of the tensors' device and
+# return; outputs and scratch come from torch's allocator on that stream.  An
+# input that another stream fills or frees is the caller's to order, as with
+# any torch operation.
+
+_TYPES = {torch.bfloat16: 0, torch.float16: 1, torch.float32: 2}
+
+
+def _refuse(what):
+    raise CelError(E_ARG, what)
+
+
+def _on(t):
+    """The tensor's device as the current one for the launches of a call."""
+    return torch.cuda.device(t.device)
+
+
+def _same_device(fn, **tensors):
+    dev = None
+    for name, t in tensors.items():
+        if not isinstance(t, torch.Tensor) or not t.is_cuda:
+            _refuse(f"{fn}: {name} is not a tensor on a ROCm device")
+        if dev is not None and t.device != dev:
+            _refuse(f"{fn}: {name} is on {t.device}, not on {dev}")
+        dev = t.device
+
+
+def _aligned(t):
+    return (t.stride(2) == 1 or t.shape[2] <= 1) and t.stride(0) % 8 == 0 and t.stride(1) % 8 == 0 and \
+        t.stride(0) <= 1 << 23 and t.data_ptr() % 16 == 0
+
+
+def _view(t):
+    return _Rows(t.data_ptr(), t.stride(0), t.stride(1))
+
+
+def _attn(fn, q, k, v, seq_ptr, scale):
+    """-> (descriptor, tensors to keep alive).  Views that the kernels cannot read as they are
+    (values not contiguous, addresses or strides off 16 bytes) are copied."""
+    _same_device(fn, q=q, k=k, v=v, seq_ptr=seq_ptr)
+    for name, t in (("q", q), ("k", k), ("v", v)):
+        if t.dim() != 3 or t.dtype != q.dtype or t.dtype not in (torch.bfloat16, torch.float16):
+            _refuse(f"{fn}: {name} is not [tokens, heads, dim] in bfloat16 or float16 as q is")
+    T, H, d = q.shape
+    if k.shape != v.shape or k.shape[0] != T or k.shape[2] != d:
+        _refuse(f"{fn}: shapes q {tuple(q.shape)}, k {tuple(k.shape)}, v {tuple(v.shape)}")
+    if seq_ptr.dim() != 1 or seq_ptr.dtype != torch.int32 or seq_ptr.numel() < 1:
+        _refuse(f"{fn}: seq_ptr is not int32 [sequences + 1]")
+    if T >= 1 << 31:
+        _refuse(f"{fn}: {T} tokens")
+    q, k, v = (t if _aligned(t) else t.clone(memory_format=torch.contiguous_format) for t in (q, k, v))
+    ptr = seq_ptr.contiguous()
+    a = _Attn(_TYPES[q.dtype], T, ptr.numel() - 1, H, k.shape[1], d,
+              1.0 / math.sqrt(max(d, 1)) if scale is None else float(scale), ptr.data_ptr(),
+              _view(q), _view(k), _view(v))
+    return a, (q, k, v, ptr)
+
+
+def attention(q, k, v, seq_ptr, scale=None):
+    """Causal attention over a packed batch: sequence s is the tokens seq_ptr[s] ..
+    seq_ptr[s + 1] - 1 (int32, on the device), a token sees itself and the earlier tokens of its
+    sequence.  q [T, heads, dim], k and v [T, kv_heads, dim] in bfloat16 or float16, any strides
+    (views of a fused projection are read in place); heads a multiple of kv_heads, dim a multiple
+    of 8 up to 128; scale: of the scores, 1 / sqrt(dim) by default.
+    -> (out [T, heads, dim], lse float32 [heads, T]); tokens of no sequence have 0 and -inf."""
+    a, keep = _attn("attention", q, k, v, seq_ptr, scale)
+    with _on(q):
+        out = torch.empty(q.shape, dtype=q.dtype, device=q.device)
+        lse = torch.empty((q.shape[1], q.shape[0]), dtype=torch.float32, device=q.device)
+        _check(lib().cel_attention(C.byref(a), C.byref(_view(out)), _p(lse), _stream()))
+    return out, lse
+
+
+def attention_grad(dout, q, k, v, out, lse, seq_ptr, scale=None, grads=None):
+    """The gradient of attention() at dout [T, heads, dim], with its out and lse.
+    -> (dq, dk, dv) as q, k, v are shaped.  grads: three tensors to write them to (for instance views
+    of one fused gradient; values contiguous, addresses and strides multiples of 16 bytes).  The same
+    inputs give the same bits."""
+    fn = "attention_grad"
+    a, keep = _attn(fn, q, k, v, seq_ptr, scale)
+    _same_device(fn, q=q, dout=dout, out=out, lse=lse)
+    T, H, d = q.shape
+    for name, t in (("dout", dout), ("out", out)):
+        if t.shape != q.shape or t.dtype != q.dtype:
+            _refuse(f"{fn}: {name} is {tuple(t.shape)} {t.dtype}, not as q")
+    if lse.shape != (H, T) or lse.dtype != torch.float32:
+        _refuse(f"{fn}: lse is not float32 [heads, tokens]")
+    with _on(q):
+        dout, out = (t if _aligned(t) else t.clone(memory_format=torch.contiguous_format) for t in (dout, out))
+        lse = lse.contiguous()
+        if grads is None:
+            grads = tuple(torch.empty(t.shape, dtype=q.dtype, device=q.device) for t in (q, k, v))
+        else:
+            _same_device(fn, q=q, **{f"grads[{i}]": t for i, t in enumerate(grads)})
+            if len(grads) != 3:
+                _refuse(f"{fn}: grads are not three tensors")
+            for name, t, x in zip(("dq", "dk", "dv"), grads, (q, k, v)):
+                if t.shape != x.shape or t.dtype != q.dtype or (t.numel() and not _aligned(t)):
+                    _refuse(f"{fn}: {name} cannot be written in place: {tuple(t.shape)} {t.dtype}, strides {t.stride()}")
+        delta = torch.empty((H, T), dtype=torch.float32, device=q.device)
+        views = [_view(t) for t in grads]
+        _check(lib().cel_attention_grad(C.byref(a), C.byref(_view(out)), _p(lse), C.byref(_view(dout)), _p(delta),
+                                        *(C.byref(x) for x in views), _stream()))
+    return tuple(grads)
