@@ -19,6 +19,7 @@
  * measure the costs that the graph's nodes carry (Section 4.2.1):
  *
  *   cel_attention, cel_attention_grad  causal attention over a packed batch
+ *   cel_embed, cel_embed_grad          embedding lookup, gradient by sorted tokens
  *
  * Conventions (all entry points):
  *  - Arrays are DEVICE pointers owned by the caller unless marked (host).  The
@@ -383,6 +384,38 @@ int cel_attention(const cel_attn *a, const cel_rows *out, float *lse, hipStream_
 int cel_attention_grad(const cel_attn *a, const cel_rows *out, const float *lse, const cel_rows *dout,
                        float *delta, const cel_rows *dq, const cel_rows *dk, const cel_rows *dv,
                        hipStream_t stream);
+
+/* Rows of an embedding table by token id.  An id outside 0 .. vocab - 1 is
+ * padding: its row is zero and it gives no gradient. */
+typedef struct {
+  int32_t type;                   /* of the rows read: CEL_BF16, CEL_F16 or CEL_F32 */
+  int32_t id_bytes;               /* 4 (int32) or 8 (int64) */
+  int64_t tokens, vocab, hidden;  /* tokens < 2^31, 1 <= vocab < 2^31 - 1, 1 <= hidden <= 2^24 */
+  int64_t stride;                 /* elements between two rows read (table or dx), >= hidden */
+  const void *ids;                /* [tokens] */
+  float scale;
+} cel_embed_args;
+
+/* out_t = scale * table[ids_t]: one product in 32 bits, rounded once.
+ * Inputs: table [vocab] rows of `hidden` values, `stride` apart.
+ * Outputs: out [tokens][hidden] in the table's type.
+ * Errors: CEL_E_ARG, CEL_E_HIP. */
+int cel_embed(const cel_embed_args *a, const void *table, void *out, hipStream_t stream);
+
+/* The gradient of cel_embed's table at dx, the gradient of its rows:
+ * grad_v = scale * sum over t with ids_t = v of dx_t, 0 for a word that does
+ * not occur (every element of grad is written).  Tokens are sorted by id and
+ * added in 32 bits in the batch's order, with every aligned 64 sorted tokens
+ * of one word added up first: the same inputs give the same bits.
+ * Inputs: dx [tokens] rows of `hidden` values, `stride` apart; scratch of
+ * cel_embed_grad_scratch(tokens, vocab, hidden) bytes, aligned to 256.
+ * Outputs: grad [vocab][hidden], of grad_type: the rows' type or CEL_F32.
+ * Errors: CEL_E_ARG, CEL_E_HIP. */
+int cel_embed_grad(const cel_embed_args *a, const void *dx, void *scratch, int32_t grad_type, void *grad,
+                   hipStream_t stream);
+
+/* Bytes of scratch that cel_embed_grad takes, or CEL_E_ARG. */
+int64_t cel_embed_grad_scratch(int64_t tokens, int64_t vocab, int64_t hidden);
 
 /* Diagnostics: per-kernel device time.  After cel_timing(1), every call
  * records a pair of HIP events on its stream around each of its main kernel

@@ -25,7 +25,7 @@ EXPORTS = ("cel_topo_levels", "cel_blevel", "cel_cpd_order", "cel_dfs_order", "c
            "cel_makespan_info", "cel_makespan_blocks_info", "cel_makespan_relax", "cel_blevel_info", "cel_policy_iteration",
            "cel_topo_levels_info", "cel_cluster_info",
            "cel_order_place", "cel_comm_sums", "cel_makespan_model", "cel_colocate",
-           "cel_attention", "cel_attention_grad", "cel_step_latency", "cel_timing", "cel_kernel_stats", "cel_last_error", "cel_version")
+           "cel_attention", "cel_attention_grad", "cel_embed", "cel_embed_grad", "cel_embed_grad_scratch", "cel_step_latency", "cel_timing", "cel_kernel_stats", "cel_last_error", "cel_version")
 
 
 class CelError(RuntimeError):
@@ -62,6 +62,12 @@ class _Attn(C.Structure):
                 ("q", _Rows), ("k", _Rows), ("v", _Rows)]
 
 
+class _Embed(C.Structure):
+    _fields_ = [("type", C.c_int32), ("id_bytes", C.c_int32),
+                ("tokens", C.c_int64), ("vocab", C.c_int64), ("hidden", C.c_int64), ("stride", C.c_int64),
+                ("ids", C.c_void_p), ("scale", C.c_float)]
+
+
 _lib = None
 
 
@@ -92,11 +98,16 @@ def lib() -> C.CDLL:
         At, Ro = C.POINTER(_Attn), C.POINTER(_Rows)
         L.cel_attention.argtypes = [At, Ro, vp, vp]
         L.cel_attention_grad.argtypes = [At, Ro, vp, Ro, vp, Ro, Ro, Ro, vp]
+        Em = C.POINTER(_Embed)
+        L.cel_embed.argtypes = [Em, vp, vp, vp]
+        L.cel_embed_grad.argtypes = [Em, vp, vp, i32, vp, vp]
+        L.cel_embed_grad_scratch.argtypes = [i64, i64, i64]
+        L.cel_embed_grad_scratch.restype = i64
         for f in ("cel_topo_levels", "cel_blevel", "cel_cluster", "cel_place", "cel_place_ext",
                   "cel_makespan",
                   "cel_makespan_noalloc",
                   "cel_cpd_order", "cel_dfs_order", "cel_order_place", "cel_comm_sums", "cel_makespan_model",
-                  "cel_colocate", "cel_attention", "cel_attention_grad", "cel_version"):
+                  "cel_colocate", "cel_attention", "cel_attention_grad", "cel_embed", "cel_embed_grad", "cel_version"):
             getattr(L, f).restype = C.c_int
         L.cel_last_error.argtypes = []
         L.cel_last_error.restype = C.c_char_p
@@ -587,3 +598,52 @@ def attention_grad(dout, q, k, v, out, lse, seq_ptr, scale=None, grads=None):
         _check(lib().cel_attention_grad(C.byref(a), C.byref(_view(out)), _p(lse), C.byref(_view(dout)), _p(delta),
                                         *(C.byref(x) for x in views), _stream()))
     return tuple(grads)
+
+
+def _embed(fn, what, rows, ids, vocab, scale):
+    """-> (descriptor, rows with contiguous values, ids): checks that embed and embed_grad share."""
+    _same_device(fn, **{what: rows, "ids": ids})
+    if rows.dim() != 2 or rows.dtype not in _TYPES:
+        _refuse(f"{fn}: {what} is not [rows, hidden] in bfloat16, float16 or float32")
+    if ids.dim() != 1 or ids.dtype not in (torch.int32, torch.int64):
+        _refuse(f"{fn}: ids are not int32 or int64 [tokens]")
+    h = rows.shape[1]
+    if (h > 1 and rows.stride(1) != 1) or (rows.shape[0] > 1 and rows.stride(0) < h):
+        rows = rows.clone(memory_format=torch.contiguous_format)
+    ids = ids.contiguous()
+    stride = rows.stride(0) if rows.shape[0] > 1 else h
+    return _Embed(_TYPES[rows.dtype], ids.element_size(), ids.numel(), vocab, h, stride, ids.data_ptr(),
+                  float(scale)), rows, ids
+
+
+def embed(table, ids, scale=1.0):
+    """scale * table[ids]: rows of table [vocab, hidden] (bfloat16, float16 or float32, rows any
+    stride apart) by token id (int32 or int64 [tokens]); an id outside [0, vocab) is padding, a row
+    of zeros. -> [tokens, hidden] in the table's type."""
+    a, table, ids = _embed("embed", "table", table, ids, table.shape[0] if isinstance(table, torch.Tensor) else 0, scale)
+    with _on(table):
+        out = torch.empty((ids.numel(), table.shape[1]), dtype=table.dtype, device=table.device)
+        _check(lib().cel_embed(C.byref(a), _p(table), _p(out), _stream()))
+    return out
+
+
+def embed_grad(dx, ids, vocab, scale=1.0, dtype=None):
+    """The gradient of embed()'s table at dx [tokens, hidden], the gradient of its rows: a dense
+    [vocab, hidden] in `dtype` (dx's by default, or float32), zeros for words that do not occur.
+    The tokens are sorted by id and added in 32 bits in a fixed order: the same inputs give the
+    same bits."""
+    fn = "embed_grad"
+    a, dx, ids = _embed(fn, "dx", dx, ids, int(vocab), scale)
+    if ids.numel() != dx.shape[0]:
+        _refuse(f"{fn}: {ids.numel()} ids of {dx.shape[0]} rows")
+    dtype = dx.dtype if dtype is None else dtype
+    if dtype not in (dx.dtype, torch.float32):
+        _refuse(f"{fn}: a gradient in {dtype} of rows in {dx.dtype}")
+    with _on(dx):
+        size = lib().cel_embed_grad_scratch(ids.numel(), int(vocab), dx.shape[1])
+        if size < 0:
+            _check(int(size))
+        work = torch.empty(size, dtype=torch.uint8, device=dx.device)
+        grad = torch.empty((int(vocab), dx.shape[1]), dtype=dtype, device=dx.device)
+        _check(lib().cel_embed_grad(C.byref(a), _p(dx), _p(work), _TYPES[dtype], _p(grad), _stream()))
+    return grad
