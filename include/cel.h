@@ -338,8 +338,9 @@ int cel_colocate(const cel_graph *g, const int32_t *order, const int32_t *group,
 enum { CEL_BF16 = 0, CEL_F16 = 1, CEL_F32 = 2 };
 
 /* A [tokens][heads][dim] view of device memory: element (t, h, c) lies at
- * p + t * row + h * head + c (strides in elements, >= 0).  The address is a
- * multiple of 16 bytes and both strides are multiples of 8; row <= 2^23. */
+ * p + t * row + h * head + c (strides in elements).  The address is a
+ * multiple of 16 bytes and both strides are multiples of 8; dim <= row <= 2^23,
+ * 0 <= head. */
 typedef struct {
   void *p;
   int64_t row, head;
@@ -378,11 +379,11 @@ int cel_attention(const cel_attn *a, const cel_rows *out, float *lse, hipStream_
  *   dq_i = scale sum_j ds_ij k_j;  dk_j = scale sum_i ds_ij q_i;  dv_j = sum_i p_ij dout_i
  * dk and dv sum over the query heads of their key/value head, in a fixed
  * order: the same inputs give the same bits.  A token of no sequence has
- * gradients of 0.  delta: scratch, float [heads][tokens].
+ * gradients of 0.  scratch: float [2][heads][tokens].
  * Outputs: dq (heads), dk, dv (kv_heads); they overlap no input nor each other.
  * Errors: CEL_E_ARG, CEL_E_HIP. */
 int cel_attention_grad(const cel_attn *a, const cel_rows *out, const float *lse, const cel_rows *dout,
-                       float *delta, const cel_rows *dq, const cel_rows *dk, const cel_rows *dv,
+                       float *scratch, const cel_rows *dq, const cel_rows *dk, const cel_rows *dv,
                        hipStream_t stream);
 
 /* Rows of an embedding table by token id.  An id outside 0 .. vocab - 1 is

@@ -522,8 +522,8 @@ def _same_device(fn, **tensors):
 
 
 def _aligned(t):
-    return (t.stride(2) == 1 or t.shape[2] <= 1) and t.stride(0) % 8 == 0 and t.stride(1) % 8 == 0 and \
-        t.stride(0) <= 1 << 23 and t.data_ptr() % 16 == 0
+    return t.stride(2) == 1 and t.stride(0) % 8 == 0 and t.stride(1) % 8 == 0 and \
+        t.shape[2] <= t.stride(0) <= 1 << 23 and t.data_ptr() % 16 == 0
 
 
 def _view(t):
@@ -593,9 +593,9 @@ def attention_grad(dout, q, k, v, out, lse, seq_ptr, scale=None, grads=None):
             for name, t, x in zip(("dq", "dk", "dv"), grads, (q, k, v)):
                 if t.shape != x.shape or t.dtype != q.dtype or (t.numel() and not _aligned(t)):
                     _refuse(f"{fn}: {name} cannot be written in place: {tuple(t.shape)} {t.dtype}, strides {t.stride()}")
-        delta = torch.empty((H, T), dtype=torch.float32, device=q.device)
+        scratch = torch.empty((2, H, T), dtype=torch.float32, device=q.device)
         views = [_view(t) for t in grads]
-        _check(lib().cel_attention_grad(C.byref(a), C.byref(_view(out)), _p(lse), C.byref(_view(dout)), _p(delta),
+        _check(lib().cel_attention_grad(C.byref(a), C.byref(_view(out)), _p(lse), C.byref(_view(dout)), _p(scratch),
                                         *(C.byref(x) for x in views), _stream()))
     return tuple(grads)
 

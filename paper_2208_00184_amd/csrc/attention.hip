@@ -91,7 +91,8 @@ struct AttnArgs {
   Rows q, k, v, out, dout, dq, dk, dv;
   const int32_t *ptr;
   int32_t S, T, H, K, d, tiles;
-  float *lse, *delta;
+  float *lse;
+  float *rows;  // the backward pass's scratch: lse in units of log 2, D, each [heads][tokens]
   float scale;
 };
 
@@ -107,19 +108,40 @@ template <int DP>
 __device__ inline int chunk_at(int r, int c) {  // byte offset
   return r * (DP * 2) + ((c ^ swz<DP>(r)) << 4);
 }
-// Rows [r0, r0 + kStep) of a head; rows at or past `end`, and values past d, are zero.
+// Copies rows [r0, r0 + kStep) of one head of a view straight into LDS, 16
+// bytes a lane; rows at or past `end`, and values past d, become zeros: they
+// lie beyond the buffer descriptor's size.  The copy is in order with the
+// wave's other loads and done once vmcnt says so.
 template <int DP>
-__device__ inline void stage(char *lds, const Rows &x, int head, int r0, int end, int d, int tid) {
-  constexpr int C = DP / 8;
-#pragma unroll
-  for (int i = 0; i < kStep * C / (kWaves * 64); i++) {
-    const int at = i * (kWaves * 64) + tid, r = at / C, c = at % C;
-    u32x4 val = {0, 0, 0, 0};
-    if (r0 + r < end && c * 8 < d)
-      val = *reinterpret_cast<const u32x4 *>(x.p + 2 * ((int64_t)(r0 + r) * x.row + (int64_t)head * x.head + c * 8));
-    *reinterpret_cast<u32x4 *>(lds + chunk_at<DP>(r, c)) = val;
+struct Stager {
+  static constexpr int C = DP / 8, kLoads = kStep * C / (kWaves * 64), kRowsApart = kWaves * 64 / C;
+  const char *base;
+  uint32_t at, row;  // this lane's offset in a tile; bytes between rows
+  __device__ Stager(const Rows &x, int d, int tid) : base(x.p), row((uint32_t)(2 * x.row)) {
+    const int r = tid / C, c = (tid % C) ^ swz<DP>(r);  // the rows of a lane's loads share swz: 16 divides kRowsApart
+    at = c * 8 < d ? (uint32_t)r * row + 16 * c : 0x80000000u;
   }
+  __device__ void load(char *lds, int64_t head_bytes, int r0, int end, int wave) const {
+    const int rows = min(end - r0, kStep);
+    const __amdgpu_buffer_rsrc_t buf = __builtin_amdgcn_make_buffer_rsrc(
+        const_cast<char *>(base + head_bytes + (int64_t)r0 * row), 0, rows > 0 ? (uint32_t)rows * row : 0u, 0x00020000);
+#pragma unroll
+    for (int i = 0; i < kLoads; i++)
+      __builtin_amdgcn_raw_ptr_buffer_load_lds(
+          buf, (__attribute__((address_space(3))) void *)(lds + (i * kWaves + wave) * 1024), 16,
+          at + (uint32_t)i * kRowsApart * row, 0, 0, 0);
+  }
+};
+static_assert(Stager<64>::kRowsApart % 16 == 0 && Stager<128>::kRowsApart % 16 == 0, "swz repeats after 16 rows");
+// Between tiles: this wave's copies have landed and its reads of LDS are
+// done; after it, every wave's are.
+__device__ inline void next_tile() {
+  __builtin_amdgcn_s_waitcnt(0x0070);  // vmcnt(0), lgkmcnt(0)
+  __builtin_amdgcn_fence(__ATOMIC_RELEASE, "workgroup", "local");
+  __builtin_amdgcn_s_barrier();
+  __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "workgroup", "local");
 }
+
 // Left operand: rows 32 t + lane % 32, columns 16 kk + 8 (lane / 32) + 0..7.
 template <int DP>
 __device__ inline u32x4 rows_at(const char *lds, int t, int kk, int lane) {
@@ -264,10 +286,11 @@ __device__ inline bool not_finite(const acc16 (&acc)[N], float by) {
 // One tile of 128 tokens of one query head: each wave 32 of them, over the
 // keys from the first row's sequence on.
 template <class T, int DP, int DC>
-__global__ void __launch_bounds__(kWaves * 64) k_attention(AttnArgs A) {
-  __shared__ char s_k[kStep * DP * 2], s_v[kStep * DP * 2];
+__global__ void __launch_bounds__(kWaves * 64, 2) k_attention(AttnArgs A) {
+  constexpr int kTile = kStep * DP * 2;
+  __shared__ __align__(16) char s_kv[2][2][kTile];  // two tiles of keys and values: one in use, one on its way
   __shared__ int s_range[2][kWaves];
-  const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, h4 = 4 * (lane >> 5);
+  const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), h4 = 4 * (lane >> 5);
   const int item = item_of(blockIdx.x, gridDim.x);
   const int head = item / A.tiles, tile = A.tiles - 1 - item % A.tiles, kvh = head / (A.H / A.K);
   const int i = tile * kBlock + wave * kRows + (lane & 31);  // this lane's row
@@ -290,18 +313,27 @@ __global__ void __launch_bounds__(kWaves * 64) k_attention(AttnArgs A) {
   u32x4 q[DC / 16];
   load_rows(q, A.q, head, i, A.T, A.d, lane);
   const float c = A.scale * kLog2e, far = 8.f / c;
+  const Stager<DP> ks(A.k, A.d, tid), vs(A.v, A.d, tid);
+  const int64_t k_head = 2 * kvh * A.k.head, v_head = 2 * kvh * A.v.head;
   acc16 o[DC / 32];
   float m, mc, l;
   for (int careful = 0;; careful = 1) {
 #pragma unroll
     for (int n = 0; n < DC / 32; n++) o[n] = acc16{};
     m = -INFINITY, mc = 0.f, l = 0.f;
-    for (int a = k0; a <= k1; a += kStep) {
-      __syncthreads();
-      stage<DP>(s_k, A.k, kvh, a, k1 + 1, A.d, tid);
-      stage<DP>(s_v, A.v, kvh, a, k1 + 1, A.d, tid);
-      __syncthreads();
+    int now = 0;
+    if (k0 <= k1) {
+      ks.load(s_kv[0][0], k_head, k0, k1 + 1, wave);
+      vs.load(s_kv[0][1], v_head, k0, k1 + 1, wave);
+    }
+    for (int a = k0; a <= k1; a += kStep, now ^= 1) {
+      next_tile();
+      if (a + kStep <= k1) {
+        ks.load(s_kv[now ^ 1][0], k_head, a + kStep, k1 + 1, wave);
+        vs.load(s_kv[now ^ 1][1], v_head, a + kStep, k1 + 1, wave);
+      }
       if (a > w_last || a + kStep <= w_first) continue;
+      const char *s_k = s_kv[now][0], *s_v = s_kv[now][1];
       acc16 s[2] = {};
 #pragma unroll
       for (int t = 0; t < 2; t++)
@@ -369,12 +401,13 @@ __global__ void __launch_bounds__(kWaves * 64) k_attention(AttnArgs A) {
   }
 }
 
-// dq of a tile of 128 tokens of one query head; leaves D_i in delta for k_attention_dkv.
+// dq of a tile of 128 tokens of one query head; leaves lse_i and D_i in rows for k_attention_dkv.
 template <class T, int DP, int DC>
-__global__ void __launch_bounds__(kWaves * 64) k_attention_dq(AttnArgs A) {
-  __shared__ char s_k[kStep * DP * 2], s_v[kStep * DP * 2];
+__global__ void __launch_bounds__(kWaves * 64, 2) k_attention_dq(AttnArgs A) {
+  constexpr int kTile = kStep * DP * 2;
+  __shared__ __align__(16) char s_kv[2][2][kTile];
   __shared__ int s_range[2][kWaves];
-  const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, h4 = 4 * (lane >> 5);
+  const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), h4 = 4 * (lane >> 5);
   const int item = item_of(blockIdx.x, gridDim.x);
   const int head = item / A.tiles, tile = A.tiles - 1 - item % A.tiles, kvh = head / (A.H / A.K);
   const int i = tile * kBlock + wave * kRows + (lane & 31);
@@ -411,18 +444,30 @@ __global__ void __launch_bounds__(kWaves * 64) k_attention_dq(AttnArgs A) {
     D = half_sum(D);
   }
   const float lse2 = real ? A.lse[(int64_t)head * A.T + i] * kLog2e : INFINITY;
-  if (i < A.T && lane < 32) A.delta[(int64_t)head * A.T + i] = D;
+  if (i < A.T && lane < 32) {
+    A.rows[(int64_t)head * A.T + i] = lse2;
+    A.rows[((int64_t)A.H + head) * A.T + i] = D;
+  }
   const float c = A.scale * kLog2e;
+  const Stager<DP> ks(A.k, A.d, tid), vs(A.v, A.d, tid);
+  const int64_t k_head = 2 * kvh * A.k.head, v_head = 2 * kvh * A.v.head;
   acc16 dq[DC / 32];
   for (int careful = 0;; careful = 1) {
 #pragma unroll
     for (int n = 0; n < DC / 32; n++) dq[n] = acc16{};
-    for (int a = k0; a <= k1; a += kStep) {
-      __syncthreads();
-      stage<DP>(s_k, A.k, kvh, a, k1 + 1, A.d, tid);
-      stage<DP>(s_v, A.v, kvh, a, k1 + 1, A.d, tid);
-      __syncthreads();
+    int now = 0;
+    if (k0 <= k1) {
+      ks.load(s_kv[0][0], k_head, k0, k1 + 1, wave);
+      vs.load(s_kv[0][1], v_head, k0, k1 + 1, wave);
+    }
+    for (int a = k0; a <= k1; a += kStep, now ^= 1) {
+      next_tile();
+      if (a + kStep <= k1) {
+        ks.load(s_kv[now ^ 1][0], k_head, a + kStep, k1 + 1, wave);
+        vs.load(s_kv[now ^ 1][1], v_head, a + kStep, k1 + 1, wave);
+      }
       if (a > w_last || a + kStep <= w_first) continue;
+      const char *s_k = s_kv[now][0], *s_v = s_kv[now][1];
       const int lo = first - a, hi = i - a;
       const bool masked = a < w_from || a + kStep - 1 > w_upto;
       u32x4 ds[4];
@@ -470,11 +515,12 @@ __global__ void __launch_bounds__(kWaves * 64) k_attention_dq(AttnArgs A) {
 // them, over the query heads that share it and the rows up to the end of the
 // last token's sequence, in that order whatever the launch.
 template <class T, int DP, int DC>
-__global__ void __launch_bounds__(kWaves * 64) k_attention_dkv(AttnArgs A) {
-  __shared__ char s_q[kStep * DP * 2], s_g[kStep * DP * 2];
-  __shared__ float s_lse[kStep], s_delta[kStep];
+__global__ void __launch_bounds__(kWaves * 64, DP == 64 ? 2 : 1) k_attention_dkv(AttnArgs A) {
+  constexpr int kTile = kStep * DP * 2;
+  __shared__ __align__(16) char s_qg[2][2][kTile];
+  __shared__ __align__(16) float s_row[2][2][kStep];  // of A.rows
   __shared__ int s_range[2][kWaves];
-  const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, h4 = 4 * (lane >> 5);
+  const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), h4 = 4 * (lane >> 5);
   const int item = item_of(blockIdx.x, gridDim.x);
   const int kvh = item / A.tiles, tile = item % A.tiles, group = A.H / A.K;
   const int j = tile * kBlock + wave * kRows + (lane & 31);  // this lane's key
@@ -499,62 +545,74 @@ __global__ void __launch_bounds__(kWaves * 64) k_attention_dkv(AttnArgs A) {
   load_rows(k, A.k, kvh, j, A.T, A.d, lane);
   load_rows(v, A.v, kvh, j, A.T, A.d, lane);
   const float c = A.scale * kLog2e;
+  const Stager<DP> qs(A.q, A.d, tid), gs(A.dout, A.d, tid);
+  const int steps = i1 < i0 ? 0 : (i1 - i0) / kStep + 1, all = steps * group;
+  // tile n of all: rows i0 + kStep (n % steps) on of the group's head n / steps
+  auto load = [&](int n, int to) {
+    const int head = kvh * group + n / steps, a = i0 + kStep * (n % steps);
+    qs.load(s_qg[to][0], 2 * head * A.q.head, a, i1 + 1, wave);
+    gs.load(s_qg[to][1], 2 * head * A.dout.head, a, i1 + 1, wave);
+    if (wave < 2) {  // 64 rows' lse by wave 0, their D by wave 1
+      const float *from = A.rows + ((int64_t)wave * A.H + head) * A.T + a;
+      const int rows = min(i1 + 1 - a, kStep);
+      const __amdgpu_buffer_rsrc_t buf =
+          __builtin_amdgcn_make_buffer_rsrc(const_cast<float *>(from), 0, 4 * rows, 0x00020000);
+      __builtin_amdgcn_raw_ptr_buffer_load_lds(buf, (__attribute__((address_space(3))) void *)s_row[to][wave], 4,
+                                               4 * lane, 0, 0, 0);
+    }
+  };
   acc16 dk[DC / 32], dv[DC / 32];
   for (int careful = 0;; careful = 1) {
 #pragma unroll
     for (int n = 0; n < DC / 32; n++) dk[n] = dv[n] = acc16{};
-    for (int head = kvh * group; head < (kvh + 1) * group; head++)
-      for (int a = i0; a <= i1; a += kStep) {
-        __syncthreads();
-        stage<DP>(s_q, A.q, head, a, i1 + 1, A.d, tid);
-        stage<DP>(s_g, A.dout, head, a, i1 + 1, A.d, tid);
-        if (tid < kStep) {
-          const bool in = a + tid <= i1;
-          s_lse[tid] = in ? A.lse[(int64_t)head * A.T + a + tid] * kLog2e : INFINITY;
-          s_delta[tid] = in ? A.delta[(int64_t)head * A.T + a + tid] : 0.f;
+    if (all) load(0, 0);
+    for (int n = 0; n < all; n++) {
+      const int a = i0 + kStep * (n % steps), now = n & 1;
+      next_tile();
+      if (n + 1 < all) load(n + 1, now ^ 1);
+      if (a > w_last || a + kStep <= w_first) continue;
+      const char *s_q = s_qg[now][0], *s_g = s_qg[now][1];
+      const float *s_lse = s_row[now][0], *s_delta = s_row[now][1];
+      const int lo = j - a, hi = last - 1 - a;  // of the 64 rows, those that see this key
+      const bool masked = a < w_from || a + kStep - 1 > w_upto;
+      u32x4 p[4], ds[4];
+#pragma unroll
+      for (int t = 0; t < 2; t++) {
+        acc16 s = {}, dp = {};
+#pragma unroll
+        for (int kk = 0; kk < DC / 16; kk++) {
+          s = Half<T>::mma(rows_at<DP>(s_q, t, kk, lane), k[kk], s);
+          dp = Half<T>::mma(rows_at<DP>(s_g, t, kk, lane), v[kk], dp);
         }
-        __syncthreads();
-        if (a > w_last || a + kStep <= w_first) continue;
-        const int lo = j - a, hi = last - 1 - a;  // of the 64 rows, those that see this key
-        const bool masked = a < w_from || a + kStep - 1 > w_upto;
-        u32x4 p[4], ds[4];
 #pragma unroll
-        for (int t = 0; t < 2; t++) {
-          acc16 s = {}, dp = {};
-#pragma unroll
-          for (int kk = 0; kk < DC / 16; kk++) {
-            s = Half<T>::mma(rows_at<DP>(s_q, t, kk, lane), k[kk], s);
-            dp = Half<T>::mma(rows_at<DP>(s_g, t, kk, lane), v[kk], dp);
+        for (int r = 0; r < 16; r++) {
+          const int x = 32 * t + 8 * (r / 4) + r % 4 + h4;
+          s[r] = exp2_(fmaf(s[r], c, -s_lse[x]));
+          dp[r] = s[r] * (dp[r] - s_delta[x]);
+          if (masked) {
+            const bool seen = x >= lo && x <= hi;
+            s[r] = seen ? s[r] : 0.f;
+            dp[r] = seen ? dp[r] : 0.f;
           }
-#pragma unroll
-          for (int r = 0; r < 16; r++) {
-            const int x = 32 * t + 8 * (r / 4) + r % 4 + h4;
-            s[r] = exp2_(fmaf(s[r], c, -s_lse[x]));
-            dp[r] = s[r] * (dp[r] - s_delta[x]);
-            if (masked) {
-              const bool seen = x >= lo && x <= hi;
-              s[r] = seen ? s[r] : 0.f;
-              dp[r] = seen ? dp[r] : 0.f;
-            }
-          }
-          p[2 * t] = operand<T>(s, 0);
-          p[2 * t + 1] = operand<T>(s, 1);
-          ds[2 * t] = operand<T>(dp, 0);
-          ds[2 * t + 1] = operand<T>(dp, 1);
         }
-        if (masked && careful) {
-          careful_product<T, DP, DC>(s_g, dv, p, lo, hi, lane);
-          careful_product<T, DP, DC>(s_q, dk, ds, lo, hi, lane);
-        } else {
-#pragma unroll
-          for (int jj = 0; jj < 4; jj++)
-#pragma unroll
-            for (int n = 0; n < DC / 32; n++) {
-              dv[n] = Half<T>::mma(cols_at<DP>(s_g, n, jj, lane), p[jj], dv[n]);
-              dk[n] = Half<T>::mma(cols_at<DP>(s_q, n, jj, lane), ds[jj], dk[n]);
-            }
-        }
+        p[2 * t] = operand<T>(s, 0);
+        p[2 * t + 1] = operand<T>(s, 1);
+        ds[2 * t] = operand<T>(dp, 0);
+        ds[2 * t + 1] = operand<T>(dp, 1);
       }
+      if (masked && careful) {
+        careful_product<T, DP, DC>(s_g, dv, p, lo, hi, lane);
+        careful_product<T, DP, DC>(s_q, dk, ds, lo, hi, lane);
+      } else {
+#pragma unroll
+        for (int jj = 0; jj < 4; jj++)
+#pragma unroll
+          for (int n = 0; n < DC / 32; n++) {
+            dv[n] = Half<T>::mma(cols_at<DP>(s_g, n, jj, lane), p[jj], dv[n]);
+            dk[n] = Half<T>::mma(cols_at<DP>(s_q, n, jj, lane), ds[jj], dk[n]);
+          }
+      }
+    }
     if (careful || !__syncthreads_or(real && (not_finite(dk, A.scale) || not_finite(dv, 1.f)))) break;
   }
   if (j < A.T) {
@@ -573,7 +631,7 @@ int check_rows(const cel_rows *x, const cel_attn *a, const char *fn, const char 
   if (!x || !x->p) return set_error(CEL_E_ARG, "%s: %s is NULL", fn, what);
   if ((reinterpret_cast<uintptr_t>(x->p) & 15) || x->row % 8 || x->head % 8)
     return set_error(CEL_E_ARG, "%s: %s is not aligned to 16 bytes in its address and strides", fn, what);
-  if (x->row < 0 || x->head < 0 || x->row > (1 << 23) || x->head > (int64_t(1) << 40))
+  if (x->row < a->dim || x->head < 0 || x->row > (1 << 23) || x->head > (int64_t(1) << 40))
     return set_error(CEL_E_ARG, "%s: %s has a stride out of range", fn, what);
   return CEL_OK;
 }
@@ -643,7 +701,7 @@ extern "C" int cel_attention(const cel_attn *a, const cel_rows *out, float *lse,
 }
 
 extern "C" int cel_attention_grad(const cel_attn *a, const cel_rows *out, const float *lse, const cel_rows *dout,
-                                  float *delta, const cel_rows *dq, const cel_rows *dk, const cel_rows *dv,
+                                  float *scratch, const cel_rows *dq, const cel_rows *dk, const cel_rows *dv,
                                   hipStream_t s) {
   const char *fn = "cel_attention_grad";
   int rc = check_attn(a, fn);
@@ -654,11 +712,11 @@ extern "C" int cel_attention_grad(const cel_attn *a, const cel_rows *out, const 
       (rc = check_rows(dout, a, fn, "dout")) || (rc = check_rows(dq, a, fn, "dq")) ||
       (rc = check_rows(dk, a, fn, "dk")) || (rc = check_rows(dv, a, fn, "dv")))
     return rc;
-  if (!lse || !delta) return set_error(CEL_E_ARG, "%s: lse or delta is NULL", fn);
+  if (!lse || !scratch) return set_error(CEL_E_ARG, "%s: lse or scratch is NULL", fn);
   AttnArgs A = args_of(a);
   A.out = rows_of(out), A.dout = rows_of(dout), A.dq = rows_of(dq), A.dk = rows_of(dk), A.dv = rows_of(dv);
   A.lse = const_cast<float *>(lse);
-  A.delta = delta;
+  A.rows = scratch;
   CEL_BY_TYPE(k_attention_dq, A.tiles * A.H);
   CEL_BY_TYPE(k_attention_dkv, A.tiles * A.K);
   return CEL_OK;
