@@ -23,6 +23,7 @@
 // take 16-bit operands only at their full rate; the sum under p's quotient
 // adds the unrounded values.
 #include <cmath>
+#include <type_traits>
 
 #include "cel_internal.h"
 
@@ -108,6 +109,12 @@ template <int DP>
 __device__ inline int chunk_at(int r, int c) {  // byte offset
   return r * (DP * 2) + ((c ^ swz<DP>(r)) << 4);
 }
+// x, as far as the compiler knows made from the loop's variable `by`: what is
+// made from it inside the loop is not kept in registers across the loop.
+__device__ __forceinline__ int fresh(int x, int by) {
+  asm("" : "+v"(x) : "s"(by));
+  return x;
+}
 // Copies rows [r0, r0 + kStep) of one head of a view straight into LDS, 16
 // bytes a lane; rows at or past `end`, and values past d, become zeros: they
 // lie beyond the buffer descriptor's size.  The copy is in order with the
@@ -142,26 +149,36 @@ __device__ inline void next_tile() {
   __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "workgroup", "local");
 }
 
+// Where a lane reads a staged tile: byte offsets of its first chunk, by rows
+// and by columns.  The others follow by flipping bits of the chunk's position.
+template <int DP>
+struct Lane {
+  static constexpr int RB = 2 * DP;
+  int rows, cols;
+  __device__ explicit Lane(int lane) {
+    const int i = lane & 15, h = lane >> 5;
+    rows = chunk_at<DP>(lane & 31, h);
+    cols = chunk_at<DP>(4 * h + (i >> 2), 2 * ((lane >> 4) & 1) + ((i & 3) >> 1)) + 8 * (i & 1);
+  }
+};
 // Left operand: rows 32 t + lane % 32, columns 16 kk + 8 (lane / 32) + 0..7.
 template <int DP>
-__device__ inline u32x4 rows_at(const char *lds, int t, int kk, int lane) {
-  return *reinterpret_cast<const u32x4 *>(lds + chunk_at<DP>(32 * t + (lane & 31), 2 * kk + (lane >> 5)));
+__device__ inline u32x4 rows_at(const char *lds, int rows, int t, int kk) {
+  return *reinterpret_cast<const u32x4 *>(lds + (rows ^ (kk << 5)) + t * 32 * Lane<DP>::RB);
 }
 // Left operand of the transpose: its row 32 n + lane % 32 is a column of the
 // tile, its k the tile's rows 16 j + 4 (lane / 32) + 0..3 and, behind them,
 // those 8 further on.  A transposed read gives lane i of 16 lanes the i-th of
 // 16 columns of four rows, of which lane i addresses row i / 4, columns 4 (i % 4) + 0..3.
 template <int DP>
-__device__ inline u32x4 cols_at(const char *lds, int n, int j, int lane) {
+__device__ inline u32x4 cols_at(const char *lds, int cols, int n, int j) {
   typedef __attribute__((ext_vector_type(4))) short s16x4;
   typedef __attribute__((address_space(3))) s16x4 *lds_ptr;
-  const int i = lane & 15, c = 4 * n + 2 * ((lane >> 4) & 1) + ((i & 3) >> 1);
   u32x4 a;
 #pragma unroll
   for (int u = 0; u < 2; u++) {
-    const int r = 16 * j + 8 * u + 4 * (lane >> 5) + (i >> 2);
-    const s16x4 x =
-        __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_ptr)(lds + chunk_at<DP>(r, c) + 8 * (i & 1)));
+    const s16x4 x = __builtin_amdgcn_ds_read_tr16_b64_v4i16(
+        (lds_ptr)(lds + (cols ^ (n << 6) ^ (u << 5)) + (16 * j + 8 * u) * Lane<DP>::RB));
     const u32x2 y = __builtin_bit_cast(u32x2, x);
     a[2 * u] = y[0];
     a[2 * u + 1] = y[1];
@@ -183,13 +200,14 @@ __device__ inline uint32_t not_numbers(uint32_t x) {
 // and to the bits of a tile without others; each row x's infinities and NaN
 // are a product of their own, added where the column sees x.
 template <class T, int DP, int DC>
-__device__ __forceinline__ void careful_product(const char *lds, acc16 (&acc)[DC / 32], const u32x4 (&b)[4],
-                                                int lo, int hi, int lane) {
+__device__ __forceinline__ void careful_product(const char *lds, acc16 (&acc)[DC / 32], const u32x4 (&b)[4], int cols,
+                                                int lo, int hi, int lane, int a0) {
+  lane = fresh(lane, a0), cols = fresh(cols, a0);
 #pragma unroll
   for (int j = 0; j < 4; j++)
 #pragma unroll
     for (int n = 0; n < DC / 32; n++) {
-      u32x4 a = cols_at<DP>(lds, n, j, lane), off;
+      u32x4 a = cols_at<DP>(lds, cols, n, j), off;
 #pragma unroll
       for (int w = 0; w < 4; w++) {
         const uint32_t m = not_numbers<T>(a[w]);
@@ -283,150 +301,222 @@ __device__ inline bool not_finite(const acc16 (&acc)[N], float by) {
   return !(t == 0.f);
 }
 
+// The tokens of the other side that a lane's token deals with, as an interval
+// (empty: lo > hi), and what follows for its wave and workgroup: all that any of
+// their tokens deals with, and what every token of the wave deals with.
+struct Reach {
+  int lo, hi;            // this lane's
+  int any_lo, any_hi;    // this wave's union
+  int all_lo, all_hi;    // this wave's intersection
+  int from, to;          // the workgroup's union
+  __device__ bool real() const { return lo <= hi; }
+  __device__ bool skips(int a) const { return a > any_hi || a + kStep <= any_lo; }
+  __device__ bool masks(int a) const { return a < all_lo || a + kStep - 1 > all_hi; }
+  __device__ int steps() const { return to < from ? 0 : (to - from) / kStep + 1; }
+};
+// forward: the keys that token i sees; else the rows that see it.
+__device__ inline Reach reach_of(const AttnArgs &A, int i, bool forward, int (*s_reach)[kWaves], int wave) {
+  int first, last;
+  sequence_of(A, i, first, last);
+  Reach R;
+  const bool real = last > first;
+  R.lo = !real ? INT32_MAX : forward ? first : i;
+  R.hi = !real ? -1 : forward ? i : last - 1;
+  R.any_lo = wave_min(R.lo), R.any_hi = wave_max(R.hi);
+  R.all_lo = wave_max(real ? R.lo : -1), R.all_hi = wave_min(real ? R.hi : INT32_MAX);
+  s_reach[0][wave] = R.any_lo;
+  s_reach[1][wave] = R.any_hi;
+  __syncthreads();
+  R.from = INT32_MAX, R.to = -1;
+#pragma unroll
+  for (int w = 0; w < kWaves; w++) {
+    R.from = min(R.from, s_reach[0][w]);
+    R.to = max(R.to, s_reach[1][w]);
+  }
+  R.from = __builtin_amdgcn_readfirstlane(R.from), R.to = __builtin_amdgcn_readfirstlane(R.to);
+  R.any_lo = __builtin_amdgcn_readfirstlane(R.any_lo), R.any_hi = __builtin_amdgcn_readfirstlane(R.any_hi);
+  R.all_lo = __builtin_amdgcn_readfirstlane(R.all_lo), R.all_hi = __builtin_amdgcn_readfirstlane(R.all_hi);
+  return R;
+}
+
+// n tiles through two buffers: load(t, buffer) starts the copy of tile t, which
+// runs while step(t - 1, other buffer) computes.  The buffers are LDS variables
+// of their own and the loop is written out for both, so that the compiler sees
+// which reads a copy in flight concerns and waits for no other.
+template <int I>
+struct Buffer {
+  static constexpr int at = I;
+};
+template <bool SLOWLY, class Load, class Step>  // one tile at a time: for the rare pass over infinities and NaN
+__device__ __forceinline__ void through_tiles(int n, Load load, Step step) {
+  if constexpr (SLOWLY) {
+#pragma unroll 1
+    for (int t = 0; t < n; t++) {
+      next_tile();
+      load(t, Buffer<0>{});
+      next_tile();
+      step(t, Buffer<0>{});
+    }
+    return;
+  }
+  if (n > 0) load(0, Buffer<0>{});
+#pragma unroll 1
+  for (int t = 0; t < n; t += 2) {
+    next_tile();
+    if (t + 1 < n) load(t + 1, Buffer<1>{});
+    step(t, Buffer<0>{});
+    if (t + 1 >= n) break;
+    next_tile();
+    if (t + 2 < n) load(t + 2, Buffer<0>{});
+    step(t + 1, Buffer<1>{});
+  }
+}
+// acc += (columns of the staged tile)^T b, see careful_product.
+template <class T, int DP, int DC, bool CAREFUL>
+__device__ __forceinline__ void product(const char *lds, acc16 (&acc)[DC / 32], const u32x4 (&b)[4], int cols, bool masked,
+                                        int lo, int hi, int lane, int a) {
+  if (CAREFUL && masked) {
+    careful_product<T, DP, DC>(lds, acc, b, cols, lo, hi, lane, a);
+  } else {
+    cols = fresh(cols, a);
+#pragma unroll
+    for (int j = 0; j < 4; j++)
+#pragma unroll
+      for (int n = 0; n < DC / 32; n++) acc[n] = Half<T>::mma(cols_at<DP>(lds, cols, n, j), b[j], acc[n]);
+  }
+}
+// Rows 32 t .. of the staged tile times the operand f.
+template <class T, int DP, int KK>
+__device__ __forceinline__ acc16 rows_product(const char *lds, int t, const u32x4 (&f)[KK], int rows, int a) {
+  acc16 s = {};
+  rows = fresh(rows, a);
+#pragma unroll
+  for (int kk = 0; kk < KK; kk++) s = Half<T>::mma(rows_at<DP>(lds, rows, t, kk), f[kk], s);
+  return s;
+}
+// x's entries at 32 t .. of a tile outside lo .. hi, replaced.
+__device__ __forceinline__ void mask(acc16 &x, int t, int lo, int hi, float by, int lane) {
+#pragma unroll
+  for (int r = 0; r < 16; r++) {
+    const int at = 32 * t + 8 * (r / 4) + r % 4 + 4 * (lane >> 5);
+    x[r] = at >= lo && at <= hi ? x[r] : by;
+  }
+}
+
 // One tile of 128 tokens of one query head: each wave 32 of them, over the
 // keys from the first row's sequence on.
-template <class T, int DP, int DC>
-__global__ void __launch_bounds__(kWaves * 64, 2) k_attention(AttnArgs A) {
-  constexpr int kTile = kStep * DP * 2;
-  __shared__ __align__(16) char s_kv[2][2][kTile];  // two tiles of keys and values: one in use, one on its way
-  __shared__ int s_range[2][kWaves];
-  const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), h4 = 4 * (lane >> 5);
+template <class T, int DP, int DC, bool CAREFUL>
+__device__ __forceinline__ bool attention_tile(const AttnArgs &A, char *s_k0, char *s_k1, char *s_v0, char *s_v1,
+                                               int (*s_reach)[kWaves]) {
+  const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int item = item_of(blockIdx.x, gridDim.x);
   const int head = item / A.tiles, tile = A.tiles - 1 - item % A.tiles, kvh = head / (A.H / A.K);
   const int i = tile * kBlock + wave * kRows + (lane & 31);  // this lane's row
-  int first, last;                                           // its sequence
-  sequence_of(A, i, first, last);
-  const bool real = last > first;
-  const int w_first = wave_min(real ? first : INT32_MAX), w_last = wave_max(real ? i : -1);
-  const int w_upto = wave_min(real ? i : INT32_MAX), w_from = wave_max(real ? first : -1);
-  if (lane == 0) {
-    s_range[0][wave] = w_first;
-    s_range[1][wave] = w_last;
-  }
-  __syncthreads();
-  int k0 = INT32_MAX, k1 = -1;
-#pragma unroll
-  for (int w = 0; w < kWaves; w++) {
-    k0 = min(k0, s_range[0][w]);
-    k1 = max(k1, s_range[1][w]);
-  }
+  const Reach R = reach_of(A, i, true, s_reach, wave);
   u32x4 q[DC / 16];
   load_rows(q, A.q, head, i, A.T, A.d, lane);
   const float c = A.scale * kLog2e, far = 8.f / c;
+  const Lane<DP> L(lane);
   const Stager<DP> ks(A.k, A.d, tid), vs(A.v, A.d, tid);
   const int64_t k_head = 2 * kvh * A.k.head, v_head = 2 * kvh * A.v.head;
   acc16 o[DC / 32];
   float m, mc, l;
-  for (int careful = 0;; careful = 1) {
+  auto load = [&](int t, auto buf) {
+    const int a = R.from + t * kStep;
+    ks.load(buf.at ? s_k1 : s_k0, k_head, a, R.to + 1, wave);
+    vs.load(buf.at ? s_v1 : s_v0, v_head, a, R.to + 1, wave);
+  };
+  auto step = [&](int t0, auto buf) {
+    const int a = R.from + t0 * kStep;
+    if (R.skips(a)) return;
+    const char *s_k = buf.at ? s_k1 : s_k0, *s_v = buf.at ? s_v1 : s_v0;
+    const bool masked = R.masks(a);
+    const int lo = R.lo - a, hi = R.hi - a;  // of the 64 keys, those that this row sees
+    acc16 s[2];
+#pragma unroll
+    for (int t = 0; t < 2; t++) s[t] = rows_product<T, DP>(s_k, t, q, L.rows, a);
+    if (masked) {
+      mask(s[0], 0, lo, hi, -INFINITY, lane);
+      mask(s[1], 1, lo, hi, -INFINITY, lane);
+    }
+    float top = s[0][0];
+#pragma unroll
+    for (int t = 0; t < 2; t++)
+#pragma unroll
+      for (int r = 0; r < 16; r++) top = fmaxf(top, s[t][r]);
+    top = half_max(top);
+    // The reference m of the exponents follows the maximum only once that is
+    // 2^8 above it: p stays below 2^8, and the sums are seldom rescaled.
+    if (__any(top > m + far)) {
+      const float to = fmaxf(m, top);
+      const float by = to == -INFINITY ? 1.f : exp2_((m - to) * c);
+      m = to;
+      mc = m == -INFINITY ? 0.f : m * c;
+      l *= by;
+#pragma unroll
+      for (int n = 0; n < DC / 32; n++) o[n] *= by;
+    }
+    u32x4 p[4];
+#pragma unroll
+    for (int t = 0; t < 2; t++) {
+#pragma unroll
+      for (int r = 0; r < 16; r++) {
+        s[t][r] = exp2_(fmaf(s[t][r], c, -mc));
+        l += s[t][r];
+      }
+      p[2 * t] = operand<T>(s[t], 0);
+      p[2 * t + 1] = operand<T>(s[t], 1);
+    }
+    product<T, DP, DC, CAREFUL>(s_v, o, p, L.cols, masked, lo, hi, lane, a);
+  };
+  auto clear = [&] {
 #pragma unroll
     for (int n = 0; n < DC / 32; n++) o[n] = acc16{};
     m = -INFINITY, mc = 0.f, l = 0.f;
-    int now = 0;
-    if (k0 <= k1) {
-      ks.load(s_kv[0][0], k_head, k0, k1 + 1, wave);
-      vs.load(s_kv[0][1], v_head, k0, k1 + 1, wave);
-    }
-    for (int a = k0; a <= k1; a += kStep, now ^= 1) {
-      next_tile();
-      if (a + kStep <= k1) {
-        ks.load(s_kv[now ^ 1][0], k_head, a + kStep, k1 + 1, wave);
-        vs.load(s_kv[now ^ 1][1], v_head, a + kStep, k1 + 1, wave);
-      }
-      if (a > w_last || a + kStep <= w_first) continue;
-      const char *s_k = s_kv[now][0], *s_v = s_kv[now][1];
-      acc16 s[2] = {};
-#pragma unroll
-      for (int t = 0; t < 2; t++)
-#pragma unroll
-        for (int kk = 0; kk < DC / 16; kk++) s[t] = Half<T>::mma(rows_at<DP>(s_k, t, kk, lane), q[kk], s[t]);
-      const int lo = first - a, hi = i - a;  // of the 64 keys, those that this row sees
-      const bool masked = a < w_from || a + kStep - 1 > w_upto;
-      if (masked) {
-#pragma unroll
-        for (int t = 0; t < 2; t++)
-#pragma unroll
-          for (int r = 0; r < 16; r++) {
-            const int x = 32 * t + 8 * (r / 4) + r % 4 + h4;
-            s[t][r] = x >= lo && x <= hi ? s[t][r] : -INFINITY;
-          }
-      }
-      float top = s[0][0];
-#pragma unroll
-      for (int t = 0; t < 2; t++)
-#pragma unroll
-        for (int r = 0; r < 16; r++) top = fmaxf(top, s[t][r]);
-      top = half_max(top);
-      // The reference m of the exponents follows the maximum only once that
-      // is 2^8 above it: p stays below 2^8, and the sums are seldom rescaled.
-      if (__any(top > m + far)) {
-        const float to = fmaxf(m, top);
-        const float by = to == -INFINITY ? 1.f : exp2_((m - to) * c);
-        m = to;
-        mc = m == -INFINITY ? 0.f : m * c;
-        l *= by;
-#pragma unroll
-        for (int n = 0; n < DC / 32; n++) o[n] *= by;
-      }
-      u32x4 p[4];
-#pragma unroll
-      for (int t = 0; t < 2; t++) {
-#pragma unroll
-        for (int r = 0; r < 16; r++) {
-          s[t][r] = exp2_(fmaf(s[t][r], c, -mc));
-          l += s[t][r];
-        }
-        p[2 * t] = operand<T>(s[t], 0);
-        p[2 * t + 1] = operand<T>(s[t], 1);
-      }
-      if (masked && careful) {
-        careful_product<T, DP, DC>(s_v, o, p, lo, hi, lane);
-      } else {
-#pragma unroll
-        for (int j = 0; j < 4; j++)
-#pragma unroll
-          for (int n = 0; n < DC / 32; n++) o[n] = Half<T>::mma(cols_at<DP>(s_v, n, j, lane), p[j], o[n]);
-      }
-    }
-    // An infinity or NaN may come from a value that the row does not see.
-    if (careful || !__syncthreads_or(real && not_finite(o, 1.f))) break;
-  }
+  };
+  clear();
+  through_tiles<CAREFUL>(R.steps(), load, step);
+  // An infinity or NaN may come from a value that the row does not see.
+  if (!CAREFUL && __syncthreads_or(R.real() && not_finite(o, 1.f))) return false;
   l = half_sum(l);
   if (i < A.T) {
-    if (!real) {
+    if (!R.real()) {
 #pragma unroll
       for (int n = 0; n < DC / 32; n++) o[n] = acc16{};
     }
-    store_rows<T>(A.out, head, i, o, real ? 1.f / l : 0.f, A.d, lane);
-    if (lane < 32) A.lse[(int64_t)head * A.T + i] = real ? (mc + __builtin_amdgcn_logf(l)) * kLn2 : -INFINITY;
+    store_rows<T>(A.out, head, i, o, R.real() ? 1.f / l : 0.f, A.d, lane);
+    if (lane < 32) A.lse[(int64_t)head * A.T + i] = R.real() ? (mc + __builtin_amdgcn_logf(l)) * kLn2 : -INFINITY;
   }
+  return true;
 }
 
-// dq of a tile of 128 tokens of one query head; leaves lse_i and D_i in rows for k_attention_dkv.
-template <class T, int DP, int DC>
-__global__ void __launch_bounds__(kWaves * 64, 2) k_attention_dq(AttnArgs A) {
-  constexpr int kTile = kStep * DP * 2;
-  __shared__ __align__(16) char s_kv[2][2][kTile];
-  __shared__ int s_range[2][kWaves];
-  const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), h4 = 4 * (lane >> 5);
+// A workgroup runs its tile without regard to infinities and NaN, and where
+// the result has any, all of it again with: nothing of the first run is kept in
+// registers for the second.
+#define CEL_TILE_KERNEL(kernel, tile, a0, a1, b0, b1)                            \
+  template <class T, int DP, int DC>                                             \
+  __global__ void __launch_bounds__(kWaves * 64, 2) kernel(AttnArgs A) {         \
+    constexpr int kTile = kStep * DP * 2;                                        \
+    __shared__ __align__(16) char a0[kTile], a1[kTile], b0[kTile], b1[kTile];    \
+    __shared__ int s_reach[2][kWaves];                                           \
+    if (!tile<T, DP, DC, false>(A, a0, a1, b0, b1, s_reach))                     \
+      (void)tile<T, DP, DC, true>(A, a0, a1, b0, b1, s_reach);                   \
+  }
+CEL_TILE_KERNEL(k_attention, attention_tile, s_k0, s_k1, s_v0, s_v1)
+
+// dq of a tile of 128 tokens of one query head; leaves lse_i and D_i in rows
+// for k_attention_dkv.  D_i is <do_i, o_i> with the rounded o_i, except where a
+// wave's keys all lie in one tile: there, where o_i is large (few values
+// averaged) and its rounding would weigh as much as that of ds, it is the sum of
+// p_ij <do_i, v_j> in 32 bits, at the price of that tile's products twice.
+template <class T, int DP, int DC, bool CAREFUL>
+__device__ __forceinline__ bool dq_tile(const AttnArgs &A, char *s_k0, char *s_k1, char *s_v0, char *s_v1,
+                                        int (*s_reach)[kWaves]) {
+  const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int item = item_of(blockIdx.x, gridDim.x);
   const int head = item / A.tiles, tile = A.tiles - 1 - item % A.tiles, kvh = head / (A.H / A.K);
   const int i = tile * kBlock + wave * kRows + (lane & 31);
-  int first, last;
-  sequence_of(A, i, first, last);
-  const bool real = last > first;
-  const int w_first = wave_min(real ? first : INT32_MAX), w_last = wave_max(real ? i : -1);
-  const int w_upto = wave_min(real ? i : INT32_MAX), w_from = wave_max(real ? first : -1);
-  if (lane == 0) {
-    s_range[0][wave] = w_first;
-    s_range[1][wave] = w_last;
-  }
-  __syncthreads();
-  int k0 = INT32_MAX, k1 = -1;
-#pragma unroll
-  for (int w = 0; w < kWaves; w++) {
-    k0 = min(k0, s_range[0][w]);
-    k1 = max(k1, s_range[1][w]);
-  }
+  const Reach R = reach_of(A, i, true, s_reach, wave);
   u32x4 q[DC / 16], g[DC / 16];
   load_rows(q, A.q, head, i, A.T, A.d, lane);
   load_rows(g, A.dout, head, i, A.T, A.d, lane);
@@ -443,186 +533,168 @@ __global__ void __launch_bounds__(kWaves * 64, 2) k_attention_dq(AttnArgs A) {
     }
     D = half_sum(D);
   }
-  const float lse2 = real ? A.lse[(int64_t)head * A.T + i] * kLog2e : INFINITY;
-  if (i < A.T && lane < 32) {
-    A.rows[(int64_t)head * A.T + i] = lse2;
-    A.rows[((int64_t)A.H + head) * A.T + i] = D;
-  }
+  const float lse2 = R.real() ? A.lse[(int64_t)head * A.T + i] * kLog2e : INFINITY;
   const float c = A.scale * kLog2e;
+  const Lane<DP> L(lane);
   const Stager<DP> ks(A.k, A.d, tid), vs(A.v, A.d, tid);
   const int64_t k_head = 2 * kvh * A.k.head, v_head = 2 * kvh * A.v.head;
   acc16 dq[DC / 32];
-  for (int careful = 0;; careful = 1) {
+  auto load = [&](int t, auto buf) {
+    const int a = R.from + t * kStep;
+    ks.load(buf.at ? s_k1 : s_k0, k_head, a, R.to + 1, wave);
+    vs.load(buf.at ? s_v1 : s_v0, v_head, a, R.to + 1, wave);
+  };
+  auto step = [&](int t0, auto buf) {
+    const int a = R.from + t0 * kStep;
+    if (R.skips(a)) return;
+    const char *s_k = buf.at ? s_k1 : s_k0, *s_v = buf.at ? s_v1 : s_v0;
+    const bool masked = R.masks(a);
+    const int lo = R.lo - a, hi = R.hi - a;
+    if (R.any_lo >= a && R.any_hi < a + kStep) {
+      D = 0.f;
+#pragma unroll
+      for (int t = 0; t < 2; t++) {
+        acc16 s = rows_product<T, DP>(s_k, t, q, L.rows, a);
+        const acc16 dp = rows_product<T, DP>(s_v, t, g, L.rows, a);
+#pragma unroll
+        for (int r = 0; r < 16; r++) s[r] = exp2_(fmaf(s[r], c, -lse2)) * dp[r];
+        mask(s, t, lo, hi, 0.f, lane);
+#pragma unroll
+        for (int r = 0; r < 16; r++) D += s[r];
+      }
+      D = half_sum(D);
+    }
+    u32x4 ds[4];
+#pragma unroll
+    for (int t = 0; t < 2; t++) {
+      acc16 s = rows_product<T, DP>(s_k, t, q, L.rows, a);
+      const acc16 dp = rows_product<T, DP>(s_v, t, g, L.rows, a);
+#pragma unroll
+      for (int r = 0; r < 16; r++) s[r] = exp2_(fmaf(s[r], c, -lse2)) * (dp[r] - D);
+      if (masked) mask(s, t, lo, hi, 0.f, lane);
+      ds[2 * t] = operand<T>(s, 0);
+      ds[2 * t + 1] = operand<T>(s, 1);
+    }
+    product<T, DP, DC, CAREFUL>(s_k, dq, ds, L.cols, masked, lo, hi, lane, a);
+  };
+  auto clear = [&] {
 #pragma unroll
     for (int n = 0; n < DC / 32; n++) dq[n] = acc16{};
-    int now = 0;
-    if (k0 <= k1) {
-      ks.load(s_kv[0][0], k_head, k0, k1 + 1, wave);
-      vs.load(s_kv[0][1], v_head, k0, k1 + 1, wave);
-    }
-    for (int a = k0; a <= k1; a += kStep, now ^= 1) {
-      next_tile();
-      if (a + kStep <= k1) {
-        ks.load(s_kv[now ^ 1][0], k_head, a + kStep, k1 + 1, wave);
-        vs.load(s_kv[now ^ 1][1], v_head, a + kStep, k1 + 1, wave);
-      }
-      if (a > w_last || a + kStep <= w_first) continue;
-      const char *s_k = s_kv[now][0], *s_v = s_kv[now][1];
-      const int lo = first - a, hi = i - a;
-      const bool masked = a < w_from || a + kStep - 1 > w_upto;
-      u32x4 ds[4];
-#pragma unroll
-      for (int t = 0; t < 2; t++) {
-        acc16 s = {}, dp = {};
-#pragma unroll
-        for (int kk = 0; kk < DC / 16; kk++) {
-          s = Half<T>::mma(rows_at<DP>(s_k, t, kk, lane), q[kk], s);
-          dp = Half<T>::mma(rows_at<DP>(s_v, t, kk, lane), g[kk], dp);
-        }
-#pragma unroll
-        for (int r = 0; r < 16; r++) s[r] = exp2_(fmaf(s[r], c, -lse2)) * (dp[r] - D);
-        if (masked) {
-#pragma unroll
-          for (int r = 0; r < 16; r++) {
-            const int x = 32 * t + 8 * (r / 4) + r % 4 + h4;
-            s[r] = x >= lo && x <= hi ? s[r] : 0.f;
-          }
-        }
-        ds[2 * t] = operand<T>(s, 0);
-        ds[2 * t + 1] = operand<T>(s, 1);
-      }
-      if (masked && careful) {
-        careful_product<T, DP, DC>(s_k, dq, ds, lo, hi, lane);
-      } else {
-#pragma unroll
-        for (int j = 0; j < 4; j++)
-#pragma unroll
-          for (int n = 0; n < DC / 32; n++) dq[n] = Half<T>::mma(cols_at<DP>(s_k, n, j, lane), ds[j], dq[n]);
-      }
-    }
-    if (careful || !__syncthreads_or(real && not_finite(dq, A.scale))) break;
-  }
+  };
+  clear();
+  through_tiles<CAREFUL>(R.steps(), load, step);
+  if (!CAREFUL && __syncthreads_or(R.real() && not_finite(dq, A.scale))) return false;
   if (i < A.T) {
-    if (!real) {
-#pragma unroll
-      for (int n = 0; n < DC / 32; n++) dq[n] = acc16{};
-    }
+    if (!R.real()) clear();
     store_rows<T>(A.dq, head, i, dq, A.scale, A.d, lane);
+    if (lane < 32) {
+      A.rows[(int64_t)head * A.T + i] = lse2;
+      A.rows[((int64_t)A.H + head) * A.T + i] = D;
+    }
   }
+  return true;
 }
+CEL_TILE_KERNEL(k_attention_dq, dq_tile, s_k0, s_k1, s_v0, s_v1)
 
-// dk and dv of a tile of 128 tokens of one key/value head: each wave 32 of
-// them, over the query heads that share it and the rows up to the end of the
+// dk, dv or both of a tile of 128 tokens of one key/value head: each wave 32
+// of them, over the query heads that share it and the rows up to the end of the
 // last token's sequence, in that order whatever the launch.
-template <class T, int DP, int DC>
-__global__ void __launch_bounds__(kWaves * 64, DP == 64 ? 2 : 1) k_attention_dkv(AttnArgs A) {
-  constexpr int kTile = kStep * DP * 2;
-  __shared__ __align__(16) char s_qg[2][2][kTile];
-  __shared__ __align__(16) float s_row[2][2][kStep];  // of A.rows
-  __shared__ int s_range[2][kWaves];
+template <class T, int DP, int DC, bool DK, bool DV, bool CAREFUL>
+__device__ __forceinline__ bool dkv_tile(const AttnArgs &A, int kvh, int tile, char *s_q0, char *s_q1, char *s_g0,
+                                         char *s_g1, float *s_r0, float *s_r1, int (*s_reach)[kWaves]) {
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), h4 = 4 * (lane >> 5);
-  const int item = item_of(blockIdx.x, gridDim.x);
-  const int kvh = item / A.tiles, tile = item % A.tiles, group = A.H / A.K;
+  const int group = A.H / A.K;
   const int j = tile * kBlock + wave * kRows + (lane & 31);  // this lane's key
-  int first, last;
-  sequence_of(A, j, first, last);
-  const bool real = last > first;
-  // rows that see a key of this wave, of this workgroup; rows that see all of the wave's
-  const int w_first = wave_min(real ? j : INT32_MAX), w_last = wave_max(real ? last - 1 : -1);
-  const int w_upto = wave_min(real ? last - 1 : INT32_MAX), w_from = wave_max(real ? j : -1);
-  if (lane == 0) {
-    s_range[0][wave] = w_first;
-    s_range[1][wave] = w_last;
-  }
-  __syncthreads();
-  int i0 = INT32_MAX, i1 = -1;
-#pragma unroll
-  for (int w = 0; w < kWaves; w++) {
-    i0 = min(i0, s_range[0][w]);
-    i1 = max(i1, s_range[1][w]);
-  }
+  const Reach R = reach_of(A, j, false, s_reach, wave);
   u32x4 k[DC / 16], v[DC / 16];
   load_rows(k, A.k, kvh, j, A.T, A.d, lane);
-  load_rows(v, A.v, kvh, j, A.T, A.d, lane);
+  if (DK) load_rows(v, A.v, kvh, j, A.T, A.d, lane);
   const float c = A.scale * kLog2e;
+  const Lane<DP> L(lane);
   const Stager<DP> qs(A.q, A.d, tid), gs(A.dout, A.d, tid);
-  const int steps = i1 < i0 ? 0 : (i1 - i0) / kStep + 1, all = steps * group;
-  // tile n of all: rows i0 + kStep (n % steps) on of the group's head n / steps
-  auto load = [&](int n, int to) {
-    const int head = kvh * group + n / steps, a = i0 + kStep * (n % steps);
-    qs.load(s_qg[to][0], 2 * head * A.q.head, a, i1 + 1, wave);
-    gs.load(s_qg[to][1], 2 * head * A.dout.head, a, i1 + 1, wave);
+  const int steps = R.steps(), all = steps * group;
+  int l_head, l_a, s_a;  // where the copies and the steps stand
+  auto load = [&](int, auto buf) {
+    qs.load(buf.at ? s_q1 : s_q0, 2 * l_head * A.q.head, l_a, R.to + 1, wave);
+    gs.load(buf.at ? s_g1 : s_g0, 2 * l_head * A.dout.head, l_a, R.to + 1, wave);
     if (wave < 2) {  // 64 rows' lse by wave 0, their D by wave 1
-      const float *from = A.rows + ((int64_t)wave * A.H + head) * A.T + a;
-      const int rows = min(i1 + 1 - a, kStep);
-      const __amdgpu_buffer_rsrc_t buf =
+      const float *from = A.rows + ((int64_t)wave * A.H + l_head) * A.T + l_a;
+      const int rows = min(R.to + 1 - l_a, kStep);
+      const __amdgpu_buffer_rsrc_t buffer =
           __builtin_amdgcn_make_buffer_rsrc(const_cast<float *>(from), 0, 4 * rows, 0x00020000);
-      __builtin_amdgcn_raw_ptr_buffer_load_lds(buf, (__attribute__((address_space(3))) void *)s_row[to][wave], 4,
-                                               4 * lane, 0, 0, 0);
+      __builtin_amdgcn_raw_ptr_buffer_load_lds(
+          buffer, (__attribute__((address_space(3))) void *)((buf.at ? s_r1 : s_r0) + wave * kStep), 4, 4 * lane, 0, 0, 0);
     }
+    l_a += kStep;
+    if (l_a > R.to) l_a = R.from, l_head++;
   };
   acc16 dk[DC / 32], dv[DC / 32];
-  for (int careful = 0;; careful = 1) {
+  auto step = [&](int, auto buf) {
+    const int a = s_a;
+    s_a = a + kStep > R.to ? R.from : a + kStep;
+    if (R.skips(a)) return;
+    const char *s_q = buf.at ? s_q1 : s_q0, *s_g = buf.at ? s_g1 : s_g0;
+    const float *s_lse = buf.at ? s_r1 : s_r0, *s_D = s_lse + kStep;
+    const bool masked = R.masks(a);
+    const int lo = R.lo - a, hi = R.hi - a;  // of the 64 rows, those that see this key
+    u32x4 p[4], ds[4];
 #pragma unroll
-    for (int n = 0; n < DC / 32; n++) dk[n] = dv[n] = acc16{};
-    if (all) load(0, 0);
-    for (int n = 0; n < all; n++) {
-      const int a = i0 + kStep * (n % steps), now = n & 1;
-      next_tile();
-      if (n + 1 < all) load(n + 1, now ^ 1);
-      if (a > w_last || a + kStep <= w_first) continue;
-      const char *s_q = s_qg[now][0], *s_g = s_qg[now][1];
-      const float *s_lse = s_row[now][0], *s_delta = s_row[now][1];
-      const int lo = j - a, hi = last - 1 - a;  // of the 64 rows, those that see this key
-      const bool masked = a < w_from || a + kStep - 1 > w_upto;
-      u32x4 p[4], ds[4];
+    for (int t = 0; t < 2; t++) {
+      acc16 s = rows_product<T, DP>(s_q, t, k, L.rows, a);
 #pragma unroll
-      for (int t = 0; t < 2; t++) {
-        acc16 s = {}, dp = {};
-#pragma unroll
-        for (int kk = 0; kk < DC / 16; kk++) {
-          s = Half<T>::mma(rows_at<DP>(s_q, t, kk, lane), k[kk], s);
-          dp = Half<T>::mma(rows_at<DP>(s_g, t, kk, lane), v[kk], dp);
-        }
-#pragma unroll
-        for (int r = 0; r < 16; r++) {
-          const int x = 32 * t + 8 * (r / 4) + r % 4 + h4;
-          s[r] = exp2_(fmaf(s[r], c, -s_lse[x]));
-          dp[r] = s[r] * (dp[r] - s_delta[x]);
-          if (masked) {
-            const bool seen = x >= lo && x <= hi;
-            s[r] = seen ? s[r] : 0.f;
-            dp[r] = seen ? dp[r] : 0.f;
-          }
-        }
+      for (int r = 0; r < 16; r++) s[r] = exp2_(fmaf(s[r], c, -s_lse[32 * t + 8 * (r / 4) + r % 4 + h4]));
+      if (masked) mask(s, t, lo, hi, 0.f, lane);
+      if (DV) {
         p[2 * t] = operand<T>(s, 0);
         p[2 * t + 1] = operand<T>(s, 1);
+      }
+      if (DK) {
+        acc16 dp = rows_product<T, DP>(s_g, t, v, L.rows, a);
+#pragma unroll
+        for (int r = 0; r < 16; r++) dp[r] = s[r] * (dp[r] - s_D[32 * t + 8 * (r / 4) + r % 4 + h4]);
+        if (masked) mask(dp, t, lo, hi, 0.f, lane);
         ds[2 * t] = operand<T>(dp, 0);
         ds[2 * t + 1] = operand<T>(dp, 1);
       }
-      if (masked && careful) {
-        careful_product<T, DP, DC>(s_g, dv, p, lo, hi, lane);
-        careful_product<T, DP, DC>(s_q, dk, ds, lo, hi, lane);
-      } else {
-#pragma unroll
-        for (int jj = 0; jj < 4; jj++)
-#pragma unroll
-          for (int n = 0; n < DC / 32; n++) {
-            dv[n] = Half<T>::mma(cols_at<DP>(s_g, n, jj, lane), p[jj], dv[n]);
-            dk[n] = Half<T>::mma(cols_at<DP>(s_q, n, jj, lane), ds[jj], dk[n]);
-          }
-      }
     }
-    if (careful || !__syncthreads_or(real && (not_finite(dk, A.scale) || not_finite(dv, 1.f)))) break;
-  }
+    if (DV) product<T, DP, DC, CAREFUL>(s_g, dv, p, L.cols, masked, lo, hi, lane, a);
+    if (DK) product<T, DP, DC, CAREFUL>(s_q, dk, ds, L.cols, masked, lo, hi, lane, a);
+  };
+  auto clear = [&] {
+#pragma unroll
+    for (int n = 0; n < DC / 32; n++) dk[n] = dv[n] = acc16{};
+    l_head = kvh * group, l_a = s_a = R.from;
+  };
+  clear();
+  through_tiles<CAREFUL>(all, load, step);
+  if (!CAREFUL && __syncthreads_or(R.real() && ((DK && not_finite(dk, A.scale)) || (DV && not_finite(dv, 1.f))))) return false;
   if (j < A.T) {
-    if (!real) {
-#pragma unroll
-      for (int n = 0; n < DC / 32; n++) dk[n] = dv[n] = acc16{};
-    }
-    store_rows<T>(A.dk, kvh, j, dk, A.scale, A.d, lane);
-    store_rows<T>(A.dv, kvh, j, dv, 1.f, A.d, lane);
+    if (!R.real()) clear();
+    if (DK) store_rows<T>(A.dk, kvh, j, dk, A.scale, A.d, lane);
+    if (DV) store_rows<T>(A.dv, kvh, j, dv, 1.f, A.d, lane);
   }
+  return true;
+}
+
+// Up to 64 dimensions a wave holds both sums (4 products a tile).  Beyond,
+// both would take more than the 256 registers that let two waves share a SIMD:
+// a workgroup takes dv (2 products) or dk (3), which computes the scores twice.
+template <class T, int DP, int DC>
+__global__ void __launch_bounds__(kWaves * 64, 2) k_attention_dkv(AttnArgs A) {
+  constexpr int kTile = kStep * DP * 2;
+  __shared__ __align__(16) char s_q0[kTile], s_q1[kTile], s_g0[kTile], s_g1[kTile];
+  __shared__ __align__(16) float s_r0[2 * kStep], s_r1[2 * kStep];  // lse and D of the rows
+  __shared__ int s_reach[2][kWaves];
+  auto run = [&](auto dk, auto dv, int item) {
+    constexpr bool DK = decltype(dk)::value, DV = decltype(dv)::value;
+    const int kvh = item / A.tiles, tile = item % A.tiles;
+    if (!dkv_tile<T, DP, DC, DK, DV, false>(A, kvh, tile, s_q0, s_q1, s_g0, s_g1, s_r0, s_r1, s_reach))
+      (void)dkv_tile<T, DP, DC, DK, DV, true>(A, kvh, tile, s_q0, s_q1, s_g0, s_g1, s_r0, s_r1, s_reach);
+  };
+  const int item = item_of(blockIdx.x, gridDim.x);
+  if constexpr (DC <= 64) run(std::true_type{}, std::true_type{}, item);
+  else if (item & 1) run(std::true_type{}, std::false_type{}, item >> 1);
+  else run(std::false_type{}, std::true_type{}, item >> 1);
 }
 
 // ------------------------------------------------------------- entry points
@@ -718,6 +790,6 @@ extern "C" int cel_attention_grad(const cel_attn *a, const cel_rows *out, const 
   A.lse = const_cast<float *>(lse);
   A.rows = scratch;
   CEL_BY_TYPE(k_attention_dq, A.tiles * A.H);
-  CEL_BY_TYPE(k_attention_dkv, A.tiles * A.K);
+  CEL_BY_TYPE(k_attention_dkv, A.tiles * A.K * (A.d <= 64 ? 1 : 2));
   return CEL_OK;
 }
