@@ -34,6 +34,7 @@ constexpr int kWaves = 4;            // waves of a workgroup
 constexpr int kRows = 32;            // tile rows a wave owns
 constexpr int kBlock = kWaves * kRows;
 constexpr int kStep = 64;            // rows of the other side staged at once
+constexpr int kAhead = 4;             // reads of LDS stand this many matrix instructions before their use
 constexpr float kLog2e = 1.4426950408889634f;
 constexpr float kLn2 = 0.6931471805599453f;
 
@@ -371,6 +372,18 @@ __device__ __forceinline__ void through_tiles(int n, Load load, Step step) {
     step(t + 1, Buffer<1>{});
   }
 }
+// Orders what the compiler schedules here: N matrix instructions, each fed by
+// READS reads of LDS, with the reads AHEAD instructions before their use.
+template <int N, int READS, int AHEAD>
+__device__ __forceinline__ void feed() {
+  __builtin_amdgcn_sched_group_barrier(0x100, AHEAD * READS, 0);
+#pragma unroll
+  for (int i = 0; i < N - AHEAD; i++) {
+    __builtin_amdgcn_sched_group_barrier(0x008, 1, 0);
+    __builtin_amdgcn_sched_group_barrier(0x100, READS, 0);
+  }
+  __builtin_amdgcn_sched_group_barrier(0x008, AHEAD, 0);
+}
 // acc += (columns of the staged tile)^T b, see careful_product.
 template <class T, int DP, int DC, bool CAREFUL>
 __device__ __forceinline__ void product(const char *lds, acc16 (&acc)[DC / 32], const u32x4 (&b)[4], int cols, bool masked,
@@ -383,16 +396,21 @@ __device__ __forceinline__ void product(const char *lds, acc16 (&acc)[DC / 32], 
     for (int j = 0; j < 4; j++)
 #pragma unroll
       for (int n = 0; n < DC / 32; n++) acc[n] = Half<T>::mma(cols_at<DP>(lds, cols, n, j), b[j], acc[n]);
+    feed<4 * (DC / 32), 2, kAhead>();
   }
 }
-// Rows 32 t .. of the staged tile times the operand f.
+// x = rows 32 t .. of a staged tile times f, y = rows 32 u .. of another times g.
 template <class T, int DP, int KK>
-__device__ __forceinline__ acc16 rows_product(const char *lds, int t, const u32x4 (&f)[KK], int rows, int a) {
-  acc16 s = {};
+__device__ __forceinline__ void rows_products(acc16 &x, const char *lds, int t, const u32x4 (&f)[KK], acc16 &y,
+                                              const char *lds2, int u, const u32x4 (&g)[KK], int rows, int a) {
   rows = fresh(rows, a);
+  x = y = acc16{};
 #pragma unroll
-  for (int kk = 0; kk < KK; kk++) s = Half<T>::mma(rows_at<DP>(lds, rows, t, kk), f[kk], s);
-  return s;
+  for (int kk = 0; kk < KK; kk++) {
+    x = Half<T>::mma(rows_at<DP>(lds, rows, t, kk), f[kk], x);
+    y = Half<T>::mma(rows_at<DP>(lds2, rows, u, kk), g[kk], y);
+  }
+  feed<2 * KK, 1, kAhead>();
 }
 // x's entries at 32 t .. of a tile outside lo .. hi, replaced.
 __device__ __forceinline__ void mask(acc16 &x, int t, int lo, int hi, float by, int lane) {
@@ -433,8 +451,7 @@ __device__ __forceinline__ bool attention_tile(const AttnArgs &A, char *s_k0, ch
     const bool masked = R.masks(a);
     const int lo = R.lo - a, hi = R.hi - a;  // of the 64 keys, those that this row sees
     acc16 s[2];
-#pragma unroll
-    for (int t = 0; t < 2; t++) s[t] = rows_product<T, DP>(s_k, t, q, L.rows, a);
+    rows_products<T, DP>(s[0], s_k, 0, q, s[1], s_k, 1, q, L.rows, a);
     if (masked) {
       mask(s[0], 0, lo, hi, -INFINITY, lane);
       mask(s[1], 1, lo, hi, -INFINITY, lane);
@@ -554,8 +571,8 @@ __device__ __forceinline__ bool dq_tile(const AttnArgs &A, char *s_k0, char *s_k
       D = 0.f;
 #pragma unroll
       for (int t = 0; t < 2; t++) {
-        acc16 s = rows_product<T, DP>(s_k, t, q, L.rows, a);
-        const acc16 dp = rows_product<T, DP>(s_v, t, g, L.rows, a);
+        acc16 s, dp;
+        rows_products<T, DP>(s, s_k, t, q, dp, s_v, t, g, L.rows, a);
 #pragma unroll
         for (int r = 0; r < 16; r++) s[r] = exp2_(fmaf(s[r], c, -lse2)) * dp[r];
         mask(s, t, lo, hi, 0.f, lane);
@@ -567,8 +584,8 @@ __device__ __forceinline__ bool dq_tile(const AttnArgs &A, char *s_k0, char *s_k
     u32x4 ds[4];
 #pragma unroll
     for (int t = 0; t < 2; t++) {
-      acc16 s = rows_product<T, DP>(s_k, t, q, L.rows, a);
-      const acc16 dp = rows_product<T, DP>(s_v, t, g, L.rows, a);
+      acc16 s, dp;
+      rows_products<T, DP>(s, s_k, t, q, dp, s_v, t, g, L.rows, a);
 #pragma unroll
       for (int r = 0; r < 16; r++) s[r] = exp2_(fmaf(s[r], c, -lse2)) * (dp[r] - D);
       if (masked) mask(s, t, lo, hi, 0.f, lane);
@@ -638,23 +655,24 @@ __device__ __forceinline__ bool dkv_tile(const AttnArgs &A, int kvh, int tile, c
     const bool masked = R.masks(a);
     const int lo = R.lo - a, hi = R.hi - a;  // of the 64 rows, those that see this key
     u32x4 p[4], ds[4];
+    acc16 s[2], dp[2];
+    if (!DK) rows_products<T, DP>(s[0], s_q, 0, k, s[1], s_q, 1, k, L.rows, a);
 #pragma unroll
     for (int t = 0; t < 2; t++) {
-      acc16 s = rows_product<T, DP>(s_q, t, k, L.rows, a);
+      if (DK) rows_products<T, DP>(s[t], s_q, t, k, dp[t], s_g, t, v, L.rows, a);
 #pragma unroll
-      for (int r = 0; r < 16; r++) s[r] = exp2_(fmaf(s[r], c, -s_lse[32 * t + 8 * (r / 4) + r % 4 + h4]));
-      if (masked) mask(s, t, lo, hi, 0.f, lane);
+      for (int r = 0; r < 16; r++) s[t][r] = exp2_(fmaf(s[t][r], c, -s_lse[32 * t + 8 * (r / 4) + r % 4 + h4]));
+      if (masked) mask(s[t], t, lo, hi, 0.f, lane);
       if (DV) {
-        p[2 * t] = operand<T>(s, 0);
-        p[2 * t + 1] = operand<T>(s, 1);
+        p[2 * t] = operand<T>(s[t], 0);
+        p[2 * t + 1] = operand<T>(s[t], 1);
       }
       if (DK) {
-        acc16 dp = rows_product<T, DP>(s_g, t, v, L.rows, a);
 #pragma unroll
-        for (int r = 0; r < 16; r++) dp[r] = s[r] * (dp[r] - s_D[32 * t + 8 * (r / 4) + r % 4 + h4]);
-        if (masked) mask(dp, t, lo, hi, 0.f, lane);
-        ds[2 * t] = operand<T>(dp, 0);
-        ds[2 * t + 1] = operand<T>(dp, 1);
+        for (int r = 0; r < 16; r++) dp[t][r] = s[t][r] * (dp[t][r] - s_D[32 * t + 8 * (r / 4) + r % 4 + h4]);
+        if (masked) mask(dp[t], t, lo, hi, 0.f, lane);
+        ds[2 * t] = operand<T>(dp[t], 0);
+        ds[2 * t + 1] = operand<T>(dp[t], 1);
       }
     }
     if (DV) product<T, DP, DC, CAREFUL>(s_g, dv, p, L.cols, masked, lo, hi, lane, a);
