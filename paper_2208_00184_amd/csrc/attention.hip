@@ -200,14 +200,14 @@ __device__ inline uint32_t not_numbers(uint32_t x) {
 // times it would let in.  The products run on the tile's numbers, in the order
 // and to the bits of a tile without others; each row x's infinities and NaN
 // are a product of their own, added where the column sees x.
-template <class T, int DP, int DC>
-__device__ __forceinline__ void careful_product(const char *lds, acc16 (&acc)[DC / 32], const u32x4 (&b)[4], int cols,
+template <class T, int DP, int NB>
+__device__ __forceinline__ void careful_product(const char *lds, acc16 (&acc)[NB], const u32x4 (&b)[4], int cols,
                                                 int lo, int hi, int lane, int a0) {
   lane = fresh(lane, a0), cols = fresh(cols, a0);
 #pragma unroll
   for (int j = 0; j < 4; j++)
 #pragma unroll
-    for (int n = 0; n < DC / 32; n++) {
+    for (int n = 0; n < NB; n++) {
       u32x4 a = cols_at<DP>(lds, cols, n, j), off;
 #pragma unroll
       for (int w = 0; w < 4; w++) {
@@ -278,15 +278,15 @@ __device__ inline void load_rows(u32x4 (&f)[KK], const Rows &x, int head, int i,
     f[kk] = i < end && c < d ? *reinterpret_cast<const u32x4 *>(p + 2 * c) : u32x4{0, 0, 0, 0};
   }
 }
-// A transposed result, acc[n][r] times `by`: dimension 32 n + 8 (r / 4) + 4 (lane / 32) + r % 4 of row i.
+// A transposed result, acc[n][r] times `by`: dimension 32 (n0 + n) + 8 (r / 4) + 4 (lane / 32) + r % 4 of row i.
 template <class T, int N>
-__device__ inline void store_rows(const Rows &x, int head, int i, const acc16 (&acc)[N], float by, int d, int lane) {
+__device__ inline void store_rows(const Rows &x, int head, int i, const acc16 (&acc)[N], int n0, float by, int d, int lane) {
   char *p = x.p + 2 * ((int64_t)i * x.row + (int64_t)head * x.head);
 #pragma unroll
   for (int n = 0; n < N; n++)
 #pragma unroll
     for (int g = 0; g < 4; g++) {
-      const int c = 32 * n + 8 * g + 4 * (lane >> 5);
+      const int c = 32 * (n0 + n) + 8 * g + 4 * (lane >> 5);
       if (c < d)
         *reinterpret_cast<u32x2 *>(p + 2 * c) = u32x2{pack2<T>(acc[n][4 * g] * by, acc[n][4 * g + 1] * by),
                                                       pack2<T>(acc[n][4 * g + 2] * by, acc[n][4 * g + 3] * by)};
@@ -385,18 +385,18 @@ __device__ __forceinline__ void feed() {
   __builtin_amdgcn_sched_group_barrier(0x008, AHEAD, 0);
 }
 // acc += (columns of the staged tile)^T b, see careful_product.
-template <class T, int DP, int DC, bool CAREFUL>
-__device__ __forceinline__ void product(const char *lds, acc16 (&acc)[DC / 32], const u32x4 (&b)[4], int cols, bool masked,
+template <class T, int DP, bool CAREFUL, int NB>
+__device__ __forceinline__ void product(const char *lds, acc16 (&acc)[NB], const u32x4 (&b)[4], int cols, bool masked,
                                         int lo, int hi, int lane, int a) {
   if (CAREFUL && masked) {
-    careful_product<T, DP, DC>(lds, acc, b, cols, lo, hi, lane, a);
+    careful_product<T, DP, NB>(lds, acc, b, cols, lo, hi, lane, a);
   } else {
     cols = fresh(cols, a);
 #pragma unroll
     for (int j = 0; j < 4; j++)
 #pragma unroll
-      for (int n = 0; n < DC / 32; n++) acc[n] = Half<T>::mma(cols_at<DP>(lds, cols, n, j), b[j], acc[n]);
-    feed<4 * (DC / 32), 2, kAhead>();
+      for (int n = 0; n < NB; n++) acc[n] = Half<T>::mma(cols_at<DP>(lds, cols, n, j), b[j], acc[n]);
+    feed<4 * NB, 2, kAhead>();
   }
 }
 // x = rows 32 t .. of a staged tile times f, y = rows 32 u .. of another times g.
@@ -426,6 +426,7 @@ __device__ __forceinline__ void mask(acc16 &x, int t, int lo, int hi, float by, 
 template <class T, int DP, int DC, bool CAREFUL>
 __device__ __forceinline__ bool attention_tile(const AttnArgs &A, char *s_k0, char *s_k1, char *s_v0, char *s_v1,
                                                int (*s_reach)[kWaves]) {
+  constexpr int NB = CAREFUL ? 1 : DC / 32;  // sums a pass holds, see CEL_TILE_KERNEL
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int item = item_of(blockIdx.x, gridDim.x);
   const int head = item / A.tiles, tile = A.tiles - 1 - item % A.tiles, kvh = head / (A.H / A.K);
@@ -437,79 +438,94 @@ __device__ __forceinline__ bool attention_tile(const AttnArgs &A, char *s_k0, ch
   const Lane<DP> L(lane);
   const Stager<DP> ks(A.k, A.d, tid), vs(A.v, A.d, tid);
   const int64_t k_head = 2 * kvh * A.k.head, v_head = 2 * kvh * A.v.head;
-  acc16 o[DC / 32];
-  float m, mc, l;
-  auto load = [&](int t, auto buf) {
-    const int a = R.from + t * kStep;
-    ks.load(buf.at ? s_k1 : s_k0, k_head, a, R.to + 1, wave);
-    vs.load(buf.at ? s_v1 : s_v0, v_head, a, R.to + 1, wave);
-  };
-  auto step = [&](int t0, auto buf) {
-    const int a = R.from + t0 * kStep;
-    if (R.skips(a)) return;
-    const char *s_k = buf.at ? s_k1 : s_k0, *s_v = buf.at ? s_v1 : s_v0;
-    const bool masked = R.masks(a);
-    const int lo = R.lo - a, hi = R.hi - a;  // of the 64 keys, those that this row sees
-    acc16 s[2];
-    rows_products<T, DP>(s[0], s_k, 0, q, s[1], s_k, 1, q, L.rows, a);
-    if (masked) {
-      mask(s[0], 0, lo, hi, -INFINITY, lane);
-      mask(s[1], 1, lo, hi, -INFINITY, lane);
-    }
-    float top = s[0][0];
-#pragma unroll
-    for (int t = 0; t < 2; t++)
-#pragma unroll
-      for (int r = 0; r < 16; r++) top = fmaxf(top, s[t][r]);
-    top = half_max(top);
-    // The reference m of the exponents follows the maximum only once that is
-    // 2^8 above it: p stays below 2^8, and the sums are seldom rescaled.
-    if (__any(top > m + far)) {
-      const float to = fmaxf(m, top);
-      const float by = to == -INFINITY ? 1.f : exp2_((m - to) * c);
-      m = to;
-      mc = m == -INFINITY ? 0.f : m * c;
-      l *= by;
-#pragma unroll
-      for (int n = 0; n < DC / 32; n++) o[n] *= by;
-    }
-    u32x4 p[4];
-#pragma unroll
-    for (int t = 0; t < 2; t++) {
-#pragma unroll
-      for (int r = 0; r < 16; r++) {
-        s[t][r] = exp2_(fmaf(s[t][r], c, -mc));
-        l += s[t][r];
+  // from block n0 of 32 dimensions on
+  auto pass = [&](int n0) {
+    const int cols = L.cols ^ (n0 << 6);
+    acc16 o[NB];
+    float m, mc, l;
+    auto load = [&](int t, auto buf) {
+      const int a = R.from + t * kStep;
+      ks.load(buf.at ? s_k1 : s_k0, k_head, a, R.to + 1, wave);
+      vs.load(buf.at ? s_v1 : s_v0, v_head, a, R.to + 1, wave);
+    };
+    auto step = [&](int t0, auto buf) {
+      const int a = R.from + t0 * kStep;
+      if (R.skips(a)) return;
+      const char *s_k = buf.at ? s_k1 : s_k0, *s_v = buf.at ? s_v1 : s_v0;
+      const bool masked = R.masks(a);
+      const int lo = R.lo - a, hi = R.hi - a;  // of the 64 keys, those that this row sees
+      acc16 s[2];
+      // The products come first: matrix instructions take one issue slot in eight, so
+      // the other wave's vector instructions still find theirs.
+      __builtin_amdgcn_s_setprio(1);
+      rows_products<T, DP>(s[0], s_k, 0, q, s[1], s_k, 1, q, L.rows, a);
+      __builtin_amdgcn_s_setprio(0);
+      if (masked) {
+        mask(s[0], 0, lo, hi, -INFINITY, lane);
+        mask(s[1], 1, lo, hi, -INFINITY, lane);
       }
-      p[2 * t] = operand<T>(s[t], 0);
-      p[2 * t + 1] = operand<T>(s[t], 1);
-    }
-    product<T, DP, DC, CAREFUL>(s_v, o, p, L.cols, masked, lo, hi, lane, a);
-  };
-  auto clear = [&] {
+      float top = s[0][0];
 #pragma unroll
-    for (int n = 0; n < DC / 32; n++) o[n] = acc16{};
-    m = -INFINITY, mc = 0.f, l = 0.f;
-  };
-  clear();
-  through_tiles<CAREFUL>(R.steps(), load, step);
-  // An infinity or NaN may come from a value that the row does not see.
-  if (!CAREFUL && __syncthreads_or(R.real() && not_finite(o, 1.f))) return false;
-  l = half_sum(l);
-  if (i < A.T) {
-    if (!R.real()) {
+      for (int t = 0; t < 2; t++)
 #pragma unroll
-      for (int n = 0; n < DC / 32; n++) o[n] = acc16{};
+        for (int r = 0; r < 16; r++) top = fmaxf(top, s[t][r]);
+      top = half_max(top);
+      // The reference m of the exponents follows the maximum only once that is
+      // 2^8 above it: p stays below 2^8, and the sums are seldom rescaled.
+      if (__any(top > m + far)) {
+        const float to = fmaxf(m, top);
+        const float by = to == -INFINITY ? 1.f : exp2_((m - to) * c);
+        m = to;
+        mc = m == -INFINITY ? 0.f : m * c;
+        l *= by;
+#pragma unroll
+        for (int n = 0; n < NB; n++) o[n] *= by;
+      }
+      u32x4 p[4];
+#pragma unroll
+      for (int t = 0; t < 2; t++) {
+#pragma unroll
+        for (int r = 0; r < 16; r++) {
+          s[t][r] = exp2_(fmaf(s[t][r], c, -mc));
+          l += s[t][r];
+        }
+        p[2 * t] = operand<T>(s[t], 0);
+        p[2 * t + 1] = operand<T>(s[t], 1);
+      }
+      __builtin_amdgcn_s_setprio(1);
+      product<T, DP, CAREFUL>(s_v, o, p, cols, masked, lo, hi, lane, a);
+      __builtin_amdgcn_s_setprio(0);
+    };
+    auto clear = [&] {
+#pragma unroll
+      for (int n = 0; n < NB; n++) o[n] = acc16{};
+      m = -INFINITY, mc = 0.f, l = 0.f;
+    };
+    clear();
+    through_tiles<CAREFUL>(R.steps(), load, step);
+    // An infinity or NaN may come from a value that the row does not see.
+    if (!CAREFUL && __syncthreads_or(R.real() && not_finite(o, 1.f))) return false;
+    l = half_sum(l);
+    if (i < A.T) {
+      if (!R.real()) {
+#pragma unroll
+        for (int n = 0; n < NB; n++) o[n] = acc16{};
+      }
+      store_rows<T>(A.out, head, i, o, n0, R.real() ? 1.f / l : 0.f, A.d, lane);
+      if (lane < 32) A.lse[(int64_t)head * A.T + i] = R.real() ? (mc + __builtin_amdgcn_logf(l)) * kLn2 : -INFINITY;
     }
-    store_rows<T>(A.out, head, i, o, R.real() ? 1.f / l : 0.f, A.d, lane);
-    if (lane < 32) A.lse[(int64_t)head * A.T + i] = R.real() ? (mc + __builtin_amdgcn_logf(l)) * kLn2 : -INFINITY;
-  }
+    return true;
+  };
+  if constexpr (!CAREFUL) return pass(0);
+#pragma unroll 1
+  for (int n0 = 0; n0 < DC / 32; n0++) (void)pass(n0);
   return true;
 }
 
 // A workgroup runs its tile without regard to infinities and NaN, and where
 // the result has any, all of it again with: nothing of the first run is kept in
-// registers for the second.
+// registers for the second, which takes 32 dimensions at a time, so that it
+// needs fewer than the first.
 #define CEL_TILE_KERNEL(kernel, tile, a0, a1, b0, b1)                            \
   template <class T, int DP, int DC>                                             \
   __global__ void __launch_bounds__(kWaves * 64, 2) kernel(AttnArgs A) {         \
@@ -529,6 +545,7 @@ CEL_TILE_KERNEL(k_attention, attention_tile, s_k0, s_k1, s_v0, s_v1)
 template <class T, int DP, int DC, bool CAREFUL>
 __device__ __forceinline__ bool dq_tile(const AttnArgs &A, char *s_k0, char *s_k1, char *s_v0, char *s_v1,
                                         int (*s_reach)[kWaves]) {
+  constexpr int NB = CAREFUL ? 1 : DC / 32;  // sums a pass holds, see CEL_TILE_KERNEL
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int item = item_of(blockIdx.x, gridDim.x);
   const int head = item / A.tiles, tile = A.tiles - 1 - item % A.tiles, kvh = head / (A.H / A.K);
@@ -555,60 +572,68 @@ __device__ __forceinline__ bool dq_tile(const AttnArgs &A, char *s_k0, char *s_k
   const Lane<DP> L(lane);
   const Stager<DP> ks(A.k, A.d, tid), vs(A.v, A.d, tid);
   const int64_t k_head = 2 * kvh * A.k.head, v_head = 2 * kvh * A.v.head;
-  acc16 dq[DC / 32];
-  auto load = [&](int t, auto buf) {
-    const int a = R.from + t * kStep;
-    ks.load(buf.at ? s_k1 : s_k0, k_head, a, R.to + 1, wave);
-    vs.load(buf.at ? s_v1 : s_v0, v_head, a, R.to + 1, wave);
-  };
-  auto step = [&](int t0, auto buf) {
-    const int a = R.from + t0 * kStep;
-    if (R.skips(a)) return;
-    const char *s_k = buf.at ? s_k1 : s_k0, *s_v = buf.at ? s_v1 : s_v0;
-    const bool masked = R.masks(a);
-    const int lo = R.lo - a, hi = R.hi - a;
-    if (R.any_lo >= a && R.any_hi < a + kStep) {
-      D = 0.f;
+  // from block n0 of 32 dimensions on
+  auto pass = [&](int n0) {
+    const int cols = L.cols ^ (n0 << 6);
+    acc16 dq[NB];
+    auto load = [&](int t, auto buf) {
+      const int a = R.from + t * kStep;
+      ks.load(buf.at ? s_k1 : s_k0, k_head, a, R.to + 1, wave);
+      vs.load(buf.at ? s_v1 : s_v0, v_head, a, R.to + 1, wave);
+    };
+    auto step = [&](int t0, auto buf) {
+      const int a = R.from + t0 * kStep;
+      if (R.skips(a)) return;
+      const char *s_k = buf.at ? s_k1 : s_k0, *s_v = buf.at ? s_v1 : s_v0;
+      const bool masked = R.masks(a);
+      const int lo = R.lo - a, hi = R.hi - a;
+      if (R.any_lo >= a && R.any_hi < a + kStep) {
+        D = 0.f;
+#pragma unroll
+        for (int t = 0; t < 2; t++) {
+          acc16 s, dp;
+          rows_products<T, DP>(s, s_k, t, q, dp, s_v, t, g, L.rows, a);
+#pragma unroll
+          for (int r = 0; r < 16; r++) s[r] = exp2_(fmaf(s[r], c, -lse2)) * dp[r];
+          mask(s, t, lo, hi, 0.f, lane);
+#pragma unroll
+          for (int r = 0; r < 16; r++) D += s[r];
+        }
+        D = half_sum(D);
+      }
+      u32x4 ds[4];
 #pragma unroll
       for (int t = 0; t < 2; t++) {
         acc16 s, dp;
         rows_products<T, DP>(s, s_k, t, q, dp, s_v, t, g, L.rows, a);
 #pragma unroll
-        for (int r = 0; r < 16; r++) s[r] = exp2_(fmaf(s[r], c, -lse2)) * dp[r];
-        mask(s, t, lo, hi, 0.f, lane);
-#pragma unroll
-        for (int r = 0; r < 16; r++) D += s[r];
+        for (int r = 0; r < 16; r++) s[r] = exp2_(fmaf(s[r], c, -lse2)) * (dp[r] - D);
+        if (masked) mask(s, t, lo, hi, 0.f, lane);
+        ds[2 * t] = operand<T>(s, 0);
+        ds[2 * t + 1] = operand<T>(s, 1);
       }
-      D = half_sum(D);
-    }
-    u32x4 ds[4];
+      product<T, DP, CAREFUL>(s_k, dq, ds, cols, masked, lo, hi, lane, a);
+    };
+    auto clear = [&] {
 #pragma unroll
-    for (int t = 0; t < 2; t++) {
-      acc16 s, dp;
-      rows_products<T, DP>(s, s_k, t, q, dp, s_v, t, g, L.rows, a);
-#pragma unroll
-      for (int r = 0; r < 16; r++) s[r] = exp2_(fmaf(s[r], c, -lse2)) * (dp[r] - D);
-      if (masked) mask(s, t, lo, hi, 0.f, lane);
-      ds[2 * t] = operand<T>(s, 0);
-      ds[2 * t + 1] = operand<T>(s, 1);
+      for (int n = 0; n < NB; n++) dq[n] = acc16{};
+    };
+    clear();
+    through_tiles<CAREFUL>(R.steps(), load, step);
+    if (!CAREFUL && __syncthreads_or(R.real() && not_finite(dq, A.scale))) return false;
+    if (i < A.T) {
+      if (!R.real()) clear();
+      store_rows<T>(A.dq, head, i, dq, n0, A.scale, A.d, lane);
+      if (lane < 32) {
+        A.rows[(int64_t)head * A.T + i] = lse2;
+        A.rows[((int64_t)A.H + head) * A.T + i] = D;
+      }
     }
-    product<T, DP, DC, CAREFUL>(s_k, dq, ds, L.cols, masked, lo, hi, lane, a);
+    return true;
   };
-  auto clear = [&] {
-#pragma unroll
-    for (int n = 0; n < DC / 32; n++) dq[n] = acc16{};
-  };
-  clear();
-  through_tiles<CAREFUL>(R.steps(), load, step);
-  if (!CAREFUL && __syncthreads_or(R.real() && not_finite(dq, A.scale))) return false;
-  if (i < A.T) {
-    if (!R.real()) clear();
-    store_rows<T>(A.dq, head, i, dq, A.scale, A.d, lane);
-    if (lane < 32) {
-      A.rows[(int64_t)head * A.T + i] = lse2;
-      A.rows[((int64_t)A.H + head) * A.T + i] = D;
-    }
-  }
+  if constexpr (!CAREFUL) return pass(0);
+#pragma unroll 1
+  for (int n0 = 0; n0 < DC / 32; n0++) (void)pass(n0);
   return true;
 }
 CEL_TILE_KERNEL(k_attention_dq, dq_tile, s_k0, s_k1, s_v0, s_v1)
@@ -619,6 +644,7 @@ CEL_TILE_KERNEL(k_attention_dq, dq_tile, s_k0, s_k1, s_v0, s_v1)
 template <class T, int DP, int DC, bool DK, bool DV, bool CAREFUL>
 __device__ __forceinline__ bool dkv_tile(const AttnArgs &A, int kvh, int tile, char *s_q0, char *s_q1, char *s_g0,
                                          char *s_g1, float *s_r0, float *s_r1, int (*s_reach)[kWaves]) {
+  constexpr int NB = CAREFUL ? 1 : DC / 32;  // sums a pass holds, see CEL_TILE_KERNEL
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), h4 = 4 * (lane >> 5);
   const int group = A.H / A.K;
   const int j = tile * kBlock + wave * kRows + (lane & 31);  // this lane's key
@@ -645,52 +671,60 @@ __device__ __forceinline__ bool dkv_tile(const AttnArgs &A, int kvh, int tile, c
     l_a += kStep;
     if (l_a > R.to) l_a = R.from, l_head++;
   };
-  acc16 dk[DC / 32], dv[DC / 32];
-  auto step = [&](int, auto buf) {
-    const int a = s_a;
-    s_a = a + kStep > R.to ? R.from : a + kStep;
-    if (R.skips(a)) return;
-    const char *s_q = buf.at ? s_q1 : s_q0, *s_g = buf.at ? s_g1 : s_g0;
-    const float *s_lse = buf.at ? s_r1 : s_r0, *s_D = s_lse + kStep;
-    const bool masked = R.masks(a);
-    const int lo = R.lo - a, hi = R.hi - a;  // of the 64 rows, those that see this key
-    u32x4 p[4], ds[4];
-    acc16 s[2], dp[2];
-    if (!DK) rows_products<T, DP>(s[0], s_q, 0, k, s[1], s_q, 1, k, L.rows, a);
+  // from block n0 of 32 dimensions on
+  auto pass = [&](int n0) {
+    const int cols = L.cols ^ (n0 << 6);
+    acc16 dk[NB], dv[NB];
+    auto step = [&](int, auto buf) {
+      const int a = s_a;
+      s_a = a + kStep > R.to ? R.from : a + kStep;
+      if (R.skips(a)) return;
+      const char *s_q = buf.at ? s_q1 : s_q0, *s_g = buf.at ? s_g1 : s_g0;
+      const float *s_lse = buf.at ? s_r1 : s_r0, *s_D = s_lse + kStep;
+      const bool masked = R.masks(a);
+      const int lo = R.lo - a, hi = R.hi - a;  // of the 64 rows, those that see this key
+      u32x4 p[4], ds[4];
+      acc16 s[2], dp[2];
+      if (!DK) rows_products<T, DP>(s[0], s_q, 0, k, s[1], s_q, 1, k, L.rows, a);
 #pragma unroll
-    for (int t = 0; t < 2; t++) {
-      if (DK) rows_products<T, DP>(s[t], s_q, t, k, dp[t], s_g, t, v, L.rows, a);
+      for (int t = 0; t < 2; t++) {
+        if (DK) rows_products<T, DP>(s[t], s_q, t, k, dp[t], s_g, t, v, L.rows, a);
 #pragma unroll
-      for (int r = 0; r < 16; r++) s[t][r] = exp2_(fmaf(s[t][r], c, -s_lse[32 * t + 8 * (r / 4) + r % 4 + h4]));
-      if (masked) mask(s[t], t, lo, hi, 0.f, lane);
-      if (DV) {
-        p[2 * t] = operand<T>(s[t], 0);
-        p[2 * t + 1] = operand<T>(s[t], 1);
+        for (int r = 0; r < 16; r++) s[t][r] = exp2_(fmaf(s[t][r], c, -s_lse[32 * t + 8 * (r / 4) + r % 4 + h4]));
+        if (masked) mask(s[t], t, lo, hi, 0.f, lane);
+        if (DV) {
+          p[2 * t] = operand<T>(s[t], 0);
+          p[2 * t + 1] = operand<T>(s[t], 1);
+        }
+        if (DK) {
+#pragma unroll
+          for (int r = 0; r < 16; r++) dp[t][r] = s[t][r] * (dp[t][r] - s_D[32 * t + 8 * (r / 4) + r % 4 + h4]);
+          if (masked) mask(dp[t], t, lo, hi, 0.f, lane);
+          ds[2 * t] = operand<T>(dp[t], 0);
+          ds[2 * t + 1] = operand<T>(dp[t], 1);
+        }
       }
-      if (DK) {
+      if (DV) product<T, DP, CAREFUL>(s_g, dv, p, cols, masked, lo, hi, lane, a);
+      if (DK) product<T, DP, CAREFUL>(s_q, dk, ds, cols, masked, lo, hi, lane, a);
+    };
+    auto clear = [&] {
 #pragma unroll
-        for (int r = 0; r < 16; r++) dp[t][r] = s[t][r] * (dp[t][r] - s_D[32 * t + 8 * (r / 4) + r % 4 + h4]);
-        if (masked) mask(dp[t], t, lo, hi, 0.f, lane);
-        ds[2 * t] = operand<T>(dp[t], 0);
-        ds[2 * t + 1] = operand<T>(dp[t], 1);
-      }
+      for (int n = 0; n < NB; n++) dk[n] = dv[n] = acc16{};
+      l_head = kvh * group, l_a = s_a = R.from;
+    };
+    clear();
+    through_tiles<CAREFUL>(all, load, step);
+    if (!CAREFUL && __syncthreads_or(R.real() && ((DK && not_finite(dk, A.scale)) || (DV && not_finite(dv, 1.f))))) return false;
+    if (j < A.T) {
+      if (!R.real()) clear();
+      if (DK) store_rows<T>(A.dk, kvh, j, dk, n0, A.scale, A.d, lane);
+      if (DV) store_rows<T>(A.dv, kvh, j, dv, n0, 1.f, A.d, lane);
     }
-    if (DV) product<T, DP, DC, CAREFUL>(s_g, dv, p, L.cols, masked, lo, hi, lane, a);
-    if (DK) product<T, DP, DC, CAREFUL>(s_q, dk, ds, L.cols, masked, lo, hi, lane, a);
+    return true;
   };
-  auto clear = [&] {
-#pragma unroll
-    for (int n = 0; n < DC / 32; n++) dk[n] = dv[n] = acc16{};
-    l_head = kvh * group, l_a = s_a = R.from;
-  };
-  clear();
-  through_tiles<CAREFUL>(all, load, step);
-  if (!CAREFUL && __syncthreads_or(R.real() && ((DK && not_finite(dk, A.scale)) || (DV && not_finite(dv, 1.f))))) return false;
-  if (j < A.T) {
-    if (!R.real()) clear();
-    if (DK) store_rows<T>(A.dk, kvh, j, dk, A.scale, A.d, lane);
-    if (DV) store_rows<T>(A.dv, kvh, j, dv, 1.f, A.d, lane);
-  }
+  if constexpr (!CAREFUL) return pass(0);
+#pragma unroll 1
+  for (int n0 = 0; n0 < DC / 32; n0++) (void)pass(n0);
   return true;
 }
 
