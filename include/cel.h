@@ -379,12 +379,17 @@ int cel_attention(const cel_attn *a, const cel_rows *out, float *lse, hipStream_
  *   dq_i = scale sum_j ds_ij k_j;  dk_j = scale sum_i ds_ij q_i;  dv_j = sum_i p_ij dout_i
  * dk and dv sum over the query heads of their key/value head, in a fixed
  * order: the same inputs give the same bits.  A token of no sequence has
- * gradients of 0.  scratch: float [2][heads][tokens].
+ * gradients of 0.  scratch: cel_attention_grad_scratch(a)
+ * bytes, aligned to 256.
  * Outputs: dq (heads), dk, dv (kv_heads); they overlap no input nor each other.
  * Errors: CEL_E_ARG, CEL_E_HIP. */
 int cel_attention_grad(const cel_attn *a, const cel_rows *out, const float *lse, const cel_rows *dout,
-                       float *scratch, const cel_rows *dq, const cel_rows *dk, const cel_rows *dv,
+                       void *scratch, const cel_rows *dq, const cel_rows *dk, const cel_rows *dv,
                        hipStream_t stream);
+
+/* Bytes of scratch that cel_attention_grad takes for a (its type, sizes and
+ * scale are looked at), or CEL_E_ARG. */
+int64_t cel_attention_grad_scratch(const cel_attn *a);
 
 /* Rows of an embedding table by token id.  An id outside 0 .. vocab - 1 is
  * padding: its row is zero and it gives no gradient. */

@@ -25,7 +25,7 @@ EXPORTS = ("cel_topo_levels", "cel_blevel", "cel_cpd_order", "cel_dfs_order", "c
            "cel_makespan_info", "cel_makespan_blocks_info", "cel_makespan_relax", "cel_blevel_info", "cel_policy_iteration",
            "cel_topo_levels_info", "cel_cluster_info",
            "cel_order_place", "cel_comm_sums", "cel_makespan_model", "cel_colocate",
-           "cel_attention", "cel_attention_grad", "cel_embed", "cel_embed_grad", "cel_embed_grad_scratch", "cel_step_latency", "cel_timing", "cel_kernel_stats", "cel_last_error", "cel_version")
+           "cel_attention", "cel_attention_grad", "cel_attention_grad_scratch", "cel_embed", "cel_embed_grad", "cel_embed_grad_scratch", "cel_step_latency", "cel_timing", "cel_kernel_stats", "cel_last_error", "cel_version")
 
 
 class CelError(RuntimeError):
@@ -97,6 +97,8 @@ def lib() -> C.CDLL:
         L.cel_colocate.argtypes = [G, vp, vp, i32, i32, vp, vp]
         At, Ro = C.POINTER(_Attn), C.POINTER(_Rows)
         L.cel_attention.argtypes = [At, Ro, vp, vp]
+        L.cel_attention_grad_scratch.argtypes = [At]
+        L.cel_attention_grad_scratch.restype = i64
         L.cel_attention_grad.argtypes = [At, Ro, vp, Ro, vp, Ro, Ro, Ro, vp]
         Em = C.POINTER(_Embed)
         L.cel_embed.argtypes = [Em, vp, vp, vp]
@@ -593,7 +595,10 @@ def attention_grad(dout, q, k, v, out, lse, seq_ptr, scale=None, grads=None):
             for name, t, x in zip(("dq", "dk", "dv"), grads, (q, k, v)):
                 if t.shape != x.shape or t.dtype != q.dtype or (t.numel() and not _aligned(t)):
                     _refuse(f"{fn}: {name} cannot be written in place: {tuple(t.shape)} {t.dtype}, strides {t.stride()}")
-        scratch = torch.empty((2, H, T), dtype=torch.float32, device=q.device)
+        size = lib().cel_attention_grad_scratch(C.byref(a))
+        if size < 0:
+            _check(int(size))
+        scratch = torch.empty(size, dtype=torch.uint8, device=q.device)
         views = [_view(t) for t in grads]
         _check(lib().cel_attention_grad(C.byref(a), C.byref(_view(out)), _p(lse), C.byref(_view(dout)), _p(scratch),
                                         *(C.byref(x) for x in views), _stream()))

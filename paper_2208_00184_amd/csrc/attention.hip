@@ -22,6 +22,7 @@
 // are rounded to the inputs' 16-bit type as operands, since the matrix cores
 // take 16-bit operands only at their full rate; the sum under p's quotient
 // adds the unrounded values.
+#include <algorithm>
 #include <cmath>
 #include <type_traits>
 
@@ -39,6 +40,7 @@ constexpr float kLog2e = 1.4426950408889634f;
 constexpr float kLn2 = 0.6931471805599453f;
 
 typedef __attribute__((ext_vector_type(16))) float acc16;
+typedef __attribute__((ext_vector_type(4))) float acc4;
 typedef __attribute__((ext_vector_type(4))) uint32_t u32x4;
 typedef __attribute__((ext_vector_type(2))) uint32_t u32x2;
 typedef __attribute__((ext_vector_type(2))) float f32x2;
@@ -95,20 +97,25 @@ struct AttnArgs {
   int32_t S, T, H, K, d, tiles;
   float *lse;
   float *rows;  // the backward pass's scratch: lse in units of log 2, D, each [heads][tokens]
+  float *part;  // and behind it, where a key/value head's query heads are dealt out to `parts` workgroups, dk
+                // and dv of each part, [parts][2][tokens][kv_heads][dim]
+  int32_t parts;
   float scale;
 };
 
 // A staged tile: kStep rows of DP 16-bit values, in 16-byte chunks.  Chunk c
-// of row r lies at position c ^ swz(r) of its row: the 16 rows that a wave's
+// of row r lies at position c ^ Swz::of(r) of its row: the 16 rows that a wave's
 // plain 16-byte reads touch at once, and the four rows of a transposed read,
 // then lie in different banks.
 template <int DP>
-__device__ inline int swz(int r) {
-  return DP == 128 ? ((r & 3) << 2) | ((r >> 2) & 3) : (((r >> 1) & 1) << 2) | ((r >> 2) & 3);
-}
+struct Swz {
+  static __device__ int of(int r) {
+    return DP == 128 ? ((r & 3) << 2) | ((r >> 2) & 3) : (((r >> 1) & 1) << 2) | ((r >> 2) & 3);
+  }
+};
 template <int DP>
 __device__ inline int chunk_at(int r, int c) {  // byte offset
-  return r * (DP * 2) + ((c ^ swz<DP>(r)) << 4);
+  return r * (DP * 2) + ((c ^ Swz<DP>::of(r)) << 4);
 }
 // x, as far as the compiler knows made from the loop's variable `by`: what is
 // made from it inside the loop is not kept in registers across the loop.
@@ -120,13 +127,14 @@ __device__ __forceinline__ int fresh(int x, int by) {
 // bytes a lane; rows at or past `end`, and values past d, become zeros: they
 // lie beyond the buffer descriptor's size.  The copy is in order with the
 // wave's other loads and done once vmcnt says so.
-template <int DP>
+template <int DP, class Order = Swz<DP>>
 struct Stager {
   static constexpr int C = DP / 8, kLoads = kStep * C / (kWaves * 64), kRowsApart = kWaves * 64 / C;
+  static_assert(kLoads >= 1 && kRowsApart % 16 == 0, "whole loads, and the order repeats after 16 rows");
   const char *base;
   uint32_t at, row;  // this lane's offset in a tile; bytes between rows
   __device__ Stager(const Rows &x, int d, int tid) : base(x.p), row((uint32_t)(2 * x.row)) {
-    const int r = tid / C, c = (tid % C) ^ swz<DP>(r);  // the rows of a lane's loads share swz: 16 divides kRowsApart
+    const int r = tid / C, c = (tid % C) ^ Order::of(r);
     at = c * 8 < d ? (uint32_t)r * row + 16 * c : 0x80000000u;
   }
   __device__ void load(char *lds, int64_t head_bytes, int r0, int end, int wave) const {
@@ -140,7 +148,6 @@ struct Stager {
           at + (uint32_t)i * kRowsApart * row, 0, 0, 0);
   }
 };
-static_assert(Stager<64>::kRowsApart % 16 == 0 && Stager<128>::kRowsApart % 16 == 0, "swz repeats after 16 rows");
 // Between tiles: this wave's copies have landed and its reads of LDS are
 // done; after it, every wave's are.
 __device__ inline void next_tile() {
@@ -194,18 +201,18 @@ __device__ inline uint32_t not_numbers(uint32_t x) {
   return ((x & e) == e ? 0xffffu : 0u) | ((x >> 16 & e) == e ? 0xffff0000u : 0u);
 }
 
-// acc[n] += (columns of the staged tile)^T b[j], where entry x of the 64 that b
+// acc[n] += (columns of the staged tile)^T b[j], where entry x of the 16 J that b
 // holds counts only for lo <= x <= hi of its column.  b's other entries are 0,
 // which is enough unless the tile holds an infinity or NaN there, which 0
 // times it would let in.  The products run on the tile's numbers, in the order
 // and to the bits of a tile without others; each row x's infinities and NaN
 // are a product of their own, added where the column sees x.
-template <class T, int DP, int NB>
-__device__ __forceinline__ void careful_product(const char *lds, acc16 (&acc)[NB], const u32x4 (&b)[4], int cols,
+template <class T, int DP, int NB, int J>
+__device__ __forceinline__ void careful_product(const char *lds, acc16 (&acc)[NB], const u32x4 (&b)[J], int cols,
                                                 int lo, int hi, int lane, int a0) {
   lane = fresh(lane, a0), cols = fresh(cols, a0);
 #pragma unroll
-  for (int j = 0; j < 4; j++)
+  for (int j = 0; j < J; j++)
 #pragma unroll
     for (int n = 0; n < NB; n++) {
       u32x4 a = cols_at<DP>(lds, cols, n, j), off;
@@ -311,6 +318,7 @@ struct Reach {
   int all_lo, all_hi;    // this wave's intersection
   int from, to;          // the workgroup's union
   __device__ bool real() const { return lo <= hi; }
+  // of the tile [a, a + kStep): whether the wave has no part in it, or only some of its tokens with some of it
   __device__ bool skips(int a) const { return a > any_hi || a + kStep <= any_lo; }
   __device__ bool masks(int a) const { return a < all_lo || a + kStep - 1 > all_hi; }
   __device__ int steps() const { return to < from ? 0 : (to - from) / kStep + 1; }
@@ -385,18 +393,18 @@ __device__ __forceinline__ void feed() {
   __builtin_amdgcn_sched_group_barrier(0x008, AHEAD, 0);
 }
 // acc += (columns of the staged tile)^T b, see careful_product.
-template <class T, int DP, bool CAREFUL, int NB>
-__device__ __forceinline__ void product(const char *lds, acc16 (&acc)[NB], const u32x4 (&b)[4], int cols, bool masked,
+template <class T, int DP, bool CAREFUL, int NB, int J>
+__device__ __forceinline__ void product(const char *lds, acc16 (&acc)[NB], const u32x4 (&b)[J], int cols, bool masked,
                                         int lo, int hi, int lane, int a) {
   if (CAREFUL && masked) {
-    careful_product<T, DP, NB>(lds, acc, b, cols, lo, hi, lane, a);
+    careful_product<T, DP, NB, J>(lds, acc, b, cols, lo, hi, lane, a);
   } else {
     cols = fresh(cols, a);
 #pragma unroll
-    for (int j = 0; j < 4; j++)
+    for (int j = 0; j < J; j++)
 #pragma unroll
       for (int n = 0; n < NB; n++) acc[n] = Half<T>::mma(cols_at<DP>(lds, cols, n, j), b[j], acc[n]);
-    feed<4 * NB, 2, kAhead>();
+    feed<J * NB, 2, (kAhead < J * NB ? kAhead : J * NB)>();
   }
 }
 // x = rows 32 t .. of a staged tile times f, y = rows 32 u .. of another times g.
@@ -638,87 +646,256 @@ __device__ __forceinline__ bool dq_tile(const AttnArgs &A, char *s_k0, char *s_k
 }
 CEL_TILE_KERNEL(k_attention_dq, dq_tile, s_k0, s_k1, s_v0, s_v1)
 
-// dk, dv or both of a tile of 128 tokens of one key/value head: each wave 32
-// of them, over the query heads that share it and the rows up to the end of the
-// last token's sequence, in that order whatever the launch.
-template <class T, int DP, int DC, bool DK, bool DV, bool CAREFUL>
-__device__ __forceinline__ bool dkv_tile(const AttnArgs &A, int kvh, int tile, char *s_q0, char *s_q1, char *s_g0,
-                                         char *s_g1, float *s_r0, float *s_r1, int (*s_reach)[kWaves]) {
-  constexpr int NB = CAREFUL ? 1 : DC / 32;  // sums a pass holds, see CEL_TILE_KERNEL
-  const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), h4 = 4 * (lane >> 5);
-  const int group = A.H / A.K;
-  const int j = tile * kBlock + wave * kRows + (lane & 31);  // this lane's key
-  const Reach R = reach_of(A, j, false, s_reach, wave);
-  u32x4 k[DC / 16], v[DC / 16];
-  load_rows(k, A.k, kvh, j, A.T, A.d, lane);
-  if (DK) load_rows(v, A.v, kvh, j, A.T, A.d, lane);
-  const float c = A.scale * kLog2e;
-  const Lane<DP> L(lane);
-  const Stager<DP> qs(A.q, A.d, tid), gs(A.dout, A.d, tid);
-  const int steps = R.steps(), all = steps * group;
-  int l_head, l_a, s_a;  // where the copies and the steps stand
-  auto load = [&](int, auto buf) {
-    qs.load(buf.at ? s_q1 : s_q0, 2 * l_head * A.q.head, l_a, R.to + 1, wave);
-    gs.load(buf.at ? s_g1 : s_g0, 2 * l_head * A.dout.head, l_a, R.to + 1, wave);
-    if (wave < 2) {  // 64 rows' lse by wave 0, their D by wave 1
-      const float *from = A.rows + ((int64_t)wave * A.H + l_head) * A.T + l_a;
-      const int rows = min(R.to + 1 - l_a, kStep);
-      const __amdgpu_buffer_rsrc_t buffer =
-          __builtin_amdgcn_make_buffer_rsrc(const_cast<float *>(from), 0, 4 * rows, 0x00020000);
-      __builtin_amdgcn_raw_ptr_buffer_load_lds(
-          buffer, (__attribute__((address_space(3))) void *)((buf.at ? s_r1 : s_r0) + wave * kStep), 4, 4 * lane, 0, 0, 0);
+// lse (which = 0) or D (1) of rows [a, a + kStep) to LDS, one behind the other; 0 at or past `end`.
+__device__ __forceinline__ void load_row_values(float *lds, const AttnArgs &A, int which, int head, int a, int end,
+                                                int lane) {
+  const float *from = A.rows + ((int64_t)which * A.H + head) * A.T + a;
+  const int rows = min(end - a, kStep);
+  const __amdgpu_buffer_rsrc_t buf =
+      __builtin_amdgcn_make_buffer_rsrc(const_cast<float *>(from), 0, rows > 0 ? 4 * rows : 0, 0x00020000);
+  __builtin_amdgcn_raw_ptr_buffer_load_lds(buf, (__attribute__((address_space(3))) void *)(lds + which * kStep), 4, 4 * lane,
+                                           0, 0, 0);
+}
+// The same as load_rows for 16 columns: dimensions 32 kk + 8 (lane / 16) + 0..7.
+template <int KK>
+__device__ inline void load_rows16(u32x4 (&f)[KK], const Rows &x, int head, int i, int end, int d, int lane) {
+  const char *p = x.p + 2 * ((int64_t)i * x.row + (int64_t)head * x.head);
+#pragma unroll
+  for (int kk = 0; kk < KK; kk++) {
+    const int c = 32 * kk + 8 * (lane >> 4);
+    f[kk] = i < end && c < d ? *reinterpret_cast<const u32x4 *>(p + 2 * c) : u32x4{0, 0, 0, 0};
+  }
+}
+// Sums of a key's gradients, dimensions 32 n0 + 16 n + 4 (lane / 16) + r: in the
+// rows' type, or in 32 bits in A.part where several workgroups share a
+// key/value head's query heads.
+template <class T, int N>
+__device__ __forceinline__ void store_sums(const AttnArgs &A, const Rows &x, int which, int kvh, int part, int j,
+                                           const acc4 (&acc)[N], int n0, float by, int lane) {
+  char *p = x.p + 2 * ((int64_t)j * x.row + (int64_t)kvh * x.head);
+  float *q = A.part + ((((int64_t)part * 2 + which) * A.T + j) * A.K + kvh) * A.d;
+#pragma unroll
+  for (int n = 0; n < N; n++) {
+    const int c = 32 * n0 + 16 * n + 4 * (lane >> 4);
+    const acc4 y = acc[n] * by;
+    if (c >= A.d) continue;
+    if (A.parts == 1) *reinterpret_cast<u32x2 *>(p + 2 * c) = u32x2{pack2<T>(y[0], y[1]), pack2<T>(y[2], y[3])};
+    else *reinterpret_cast<acc4 *>(q + c) = y;
+  }
+}
+// Where a workgroup's walk over its query heads and their rows stands.
+struct Walk {
+  int head, a;
+  __device__ void next(const Reach &R) {
+    a += kStep;
+    if (a > R.to) a = R.from, head++;
+  }
+};
+// The query heads of a workgroup: part `part` of those that share head kvh.
+__device__ inline void heads_of(const AttnArgs &A, int kvh, int part, int &first, int &count) {
+  const int group = A.H / A.K, per = (group + A.parts - 1) / A.parts;
+  first = kvh * group + part * per;
+  count = min(per, group - part * per);
+}
+
+// dk and dv: a wave owns 16 keys, on 16x16x32 matrix instructions.  Their sums
+// and operands take half the registers that 32 keys would, so that two waves
+// share a SIMD and every product is made once; the reads of LDS a product are
+// twice as many, 256 bytes a cycle at the matrix cores' full rate, which is what
+// LDS gives.
+//   A result tile D[m][n] puts column n = lane % 16 and rows 4 (lane / 16) + r in
+//   register r; two of them are a right operand of 32 rows, in the order
+//   16 u + 4 (lane / 16) + r for its value 4 u + r.
+constexpr int kKeys = 16, kKeyBlock = kWaves * kKeys;
+template <class T>
+__device__ inline acc4 mma16(u32x4 a, u32x4 b, acc4 c) {
+  typedef typename Half<T>::v8 v8;
+  if constexpr (__is_same(T, __bf16))
+    return __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(v8, a), __builtin_bit_cast(v8, b), c, 0, 0, 0);
+  else
+    return __builtin_amdgcn_mfma_f32_16x16x32_f16(__builtin_bit_cast(v8, a), __builtin_bit_cast(v8, b), c, 0, 0, 0);
+}
+// The chunks' order for 16 columns of eight rows at once.
+template <int DP>
+struct Swz16 {
+  static __device__ int of(int r) {
+    return DP == 128 ? ((r & 7) << 1) | ((r >> 3) & 1) : (((r >> 1) & 3) << 1) | ((r >> 3) & 1);
+  }
+};
+template <int DP>
+struct Lane16 {
+  static constexpr int RB = 2 * DP;
+  int rows, cols;
+  __device__ explicit Lane16(int lane) {
+    const int i = lane & 15, g = lane >> 4, r = 4 * g + (i >> 2);
+    rows = i * RB + ((g ^ Swz16<DP>::of(i)) << 4);
+    cols = r * RB + ((((i & 3) >> 1) ^ Swz16<DP>::of(r)) << 4) + 8 * (i & 1);
+  }
+};
+// Rows 16 t + lane % 16, columns 32 kk + 8 (lane / 16) + 0..7.
+template <int DP>
+__device__ inline u32x4 rows16_at(const char *lds, int rows, int t, int kk) {
+  return *reinterpret_cast<const u32x4 *>(lds + (rows ^ (kk << 6)) + t * 16 * Lane16<DP>::RB);
+}
+// The transpose: column 16 n + lane % 16 as a row, its k the rows 32 j + 16 u + 4 (lane / 16) + 0..3.
+template <int DP>
+__device__ inline u32x4 cols16_at(const char *lds, int cols, int n, int j) {
+  typedef __attribute__((ext_vector_type(4))) short s16x4;
+  typedef __attribute__((address_space(3))) s16x4 *lds_ptr;
+  u32x4 a;
+#pragma unroll
+  for (int u = 0; u < 2; u++) {
+    const s16x4 x =
+        __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_ptr)(lds + (cols ^ (n << 5)) + (32 * j + 16 * u) * Lane16<DP>::RB));
+    const u32x2 y = __builtin_bit_cast(u32x2, x);
+    a[2 * u] = y[0];
+    a[2 * u + 1] = y[1];
+  }
+  return a;
+}
+// x[t] = rows 16 t .. of a staged tile times f, y[t] of another times g.
+template <class T, int DP, int KK>
+__device__ __forceinline__ void rows16_products(acc4 (&x)[4], const char *lds, const u32x4 (&f)[KK], acc4 (&y)[4],
+                                                const char *lds2, const u32x4 (&g)[KK], int rows, int a) {
+  rows = fresh(rows, a);
+#pragma unroll
+  for (int kk = 0; kk < KK; kk++)
+#pragma unroll
+    for (int t = 0; t < 4; t++) x[t] = mma16<T>(rows16_at<DP>(lds, rows, t, kk), f[kk], kk ? x[t] : acc4{});
+#pragma unroll
+  for (int kk = 0; kk < KK; kk++)
+#pragma unroll
+    for (int t = 0; t < 4; t++) y[t] = mma16<T>(rows16_at<DP>(lds2, rows, t, kk), g[kk], kk ? y[t] : acc4{});
+  feed<8 * KK, 1, kAhead>();
+}
+// acc[n] += (columns of the staged tile)^T b, and its careful form: see product and careful_product.
+template <class T, int DP, bool CAREFUL, int NB>
+__device__ __forceinline__ void product16(const char *lds, acc4 (&acc)[NB], const u32x4 (&b)[2], int cols, bool masked,
+                                          int lo, int hi, int lane, int a0) {
+  cols = fresh(cols, a0);
+  if (!CAREFUL || !masked) {
+#pragma unroll
+    for (int j = 0; j < 2; j++)
+#pragma unroll
+      for (int n = 0; n < NB; n++) acc[n] = mma16<T>(cols16_at<DP>(lds, cols, n, j), b[j], acc[n]);
+    feed<2 * NB, 2, (kAhead < 2 * NB ? kAhead : 2 * NB)>();
+    return;
+  }
+#pragma unroll
+  for (int j = 0; j < 2; j++)
+#pragma unroll
+    for (int n = 0; n < NB; n++) {
+      u32x4 a = cols16_at<DP>(lds, cols, n, j), off;
+#pragma unroll
+      for (int w = 0; w < 4; w++) {
+        const uint32_t m = not_numbers<T>(a[w]);
+        off[w] = a[w] & m;
+        a[w] &= ~m;
+      }
+      acc[n] = mma16<T>(a, b[j], acc[n]);
+      if (!__any((off[0] | off[1] | off[2] | off[3]) != 0)) continue;
+#pragma unroll 1
+      for (int k = 0; k < 32; k++) {
+        const int e = (k >> 4) * 4 + (k & 3), x = 32 * j + k;
+        const uint32_t keep = (lane >> 4) == ((k >> 2) & 3) ? (e & 1 ? 0xffff0000u : 0xffffu) : 0u;
+        u32x4 only;
+#pragma unroll
+        for (int w = 0; w < 4; w++) only[w] = w == (e >> 1) ? off[w] & keep : 0u;
+        const acc4 one = mma16<T>(only, b[j], acc4{});
+#pragma unroll
+        for (int r = 0; r < 4; r++) acc[n][r] = x >= lo && x <= hi ? acc[n][r] + one[r] : acc[n][r];
+      }
     }
-    l_a += kStep;
-    if (l_a > R.to) l_a = R.from, l_head++;
+}
+
+// dk and dv of a tile of 64 tokens of one key/value head: each wave 16 of them,
+// over the query heads and the rows up to the end of the last token's sequence,
+// in that order whatever the launch.
+template <class T, int DP, int DC, bool CAREFUL>
+__device__ __forceinline__ bool dkv_tile(const AttnArgs &A, char *s_q0, char *s_q1, char *s_g0, char *s_g1, float *s_r0,
+                                         float *s_r1, int (*s_reach)[kWaves]) {
+  constexpr int NB = CAREFUL ? 2 : DC / 16, KK = DC / 32;  // sums a pass holds, see CEL_TILE_KERNEL
+  const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), g4 = 4 * (lane >> 4);
+  const int tiles = (A.T + kKeyBlock - 1) / kKeyBlock;
+  const int item = item_of(blockIdx.x, gridDim.x), kvh = item / tiles / A.parts, part = item / tiles % A.parts;
+  const int j = item % tiles * kKeyBlock + wave * kKeys + (lane & 15);  // this lane's key
+  int head0, heads;
+  heads_of(A, kvh, part, head0, heads);
+  const Reach R = reach_of(A, j, false, s_reach, wave);
+  u32x4 k[KK], v[KK];
+  load_rows16(k, A.k, kvh, j, A.T, A.d, lane);
+  load_rows16(v, A.v, kvh, j, A.T, A.d, lane);
+  const float c = A.scale * kLog2e;
+  const Lane16<DP> L(lane);
+  const Stager<DP, Swz16<DP>> qs(A.q, A.d, tid), gs(A.dout, A.d, tid);
+  const int all = R.steps() * heads;
+  Walk copies, steps;
+  auto load = [&](int, auto buf) {
+    qs.load(buf.at ? s_q1 : s_q0, 2 * copies.head * A.q.head, copies.a, R.to + 1, wave);
+    gs.load(buf.at ? s_g1 : s_g0, 2 * copies.head * A.dout.head, copies.a, R.to + 1, wave);
+    if (wave < 2) load_row_values(buf.at ? s_r1 : s_r0, A, wave, copies.head, copies.a, R.to + 1, lane);
+    copies.next(R);
   };
-  // from block n0 of 32 dimensions on
   auto pass = [&](int n0) {
     const int cols = L.cols ^ (n0 << 6);
-    acc16 dk[NB], dv[NB];
+    acc4 dk[NB], dv[NB];
     auto step = [&](int, auto buf) {
-      const int a = s_a;
-      s_a = a + kStep > R.to ? R.from : a + kStep;
+      const int a = steps.a;
+      steps.next(R);
       if (R.skips(a)) return;
       const char *s_q = buf.at ? s_q1 : s_q0, *s_g = buf.at ? s_g1 : s_g0;
       const float *s_lse = buf.at ? s_r1 : s_r0, *s_D = s_lse + kStep;
       const bool masked = R.masks(a);
       const int lo = R.lo - a, hi = R.hi - a;  // of the 64 rows, those that see this key
-      u32x4 p[4], ds[4];
-      acc16 s[2], dp[2];
-      if (!DK) rows_products<T, DP>(s[0], s_q, 0, k, s[1], s_q, 1, k, L.rows, a);
+      acc4 s[4], dp[4];
+      rows16_products<T, DP>(s, s_q, k, dp, s_g, v, L.rows, a);
 #pragma unroll
-      for (int t = 0; t < 2; t++) {
-        if (DK) rows_products<T, DP>(s[t], s_q, t, k, dp[t], s_g, t, v, L.rows, a);
+      for (int t = 0; t < 4; t++)
 #pragma unroll
-        for (int r = 0; r < 16; r++) s[t][r] = exp2_(fmaf(s[t][r], c, -s_lse[32 * t + 8 * (r / 4) + r % 4 + h4]));
-        if (masked) mask(s[t], t, lo, hi, 0.f, lane);
-        if (DV) {
-          p[2 * t] = operand<T>(s[t], 0);
-          p[2 * t + 1] = operand<T>(s[t], 1);
+        for (int r = 0; r < 4; r++) {
+          s[t][r] = exp2_(fmaf(s[t][r], c, -s_lse[16 * t + g4 + r]));
+          dp[t][r] = s[t][r] * (dp[t][r] - s_D[16 * t + g4 + r]);
         }
-        if (DK) {
+      if (masked) {
+        asm volatile("");
 #pragma unroll
-          for (int r = 0; r < 16; r++) dp[t][r] = s[t][r] * (dp[t][r] - s_D[32 * t + 8 * (r / 4) + r % 4 + h4]);
-          if (masked) mask(dp[t], t, lo, hi, 0.f, lane);
-          ds[2 * t] = operand<T>(dp[t], 0);
-          ds[2 * t + 1] = operand<T>(dp[t], 1);
-        }
+        for (int t = 0; t < 4; t++)
+#pragma unroll
+          for (int r = 0; r < 4; r++) {
+            const int x = 16 * t + g4 + r;
+            const bool seen = x >= lo && x <= hi;
+            s[t][r] = seen ? s[t][r] : 0.f;
+            dp[t][r] = seen ? dp[t][r] : 0.f;
+          }
       }
-      if (DV) product<T, DP, CAREFUL>(s_g, dv, p, cols, masked, lo, hi, lane, a);
-      if (DK) product<T, DP, CAREFUL>(s_q, dk, ds, cols, masked, lo, hi, lane, a);
+      u32x4 p[2], ds[2];
+#pragma unroll
+      for (int t = 0; t < 4; t++)
+#pragma unroll
+        for (int w = 0; w < 2; w++) {
+          p[t / 2][2 * (t % 2) + w] = pack2<T>(s[t][2 * w], s[t][2 * w + 1]);
+          ds[t / 2][2 * (t % 2) + w] = pack2<T>(dp[t][2 * w], dp[t][2 * w + 1]);
+        }
+      product16<T, DP, CAREFUL>(s_g, dv, p, cols, masked, lo, hi, lane, a);
+      product16<T, DP, CAREFUL>(s_q, dk, ds, cols, masked, lo, hi, lane, a);
     };
     auto clear = [&] {
 #pragma unroll
-      for (int n = 0; n < NB; n++) dk[n] = dv[n] = acc16{};
-      l_head = kvh * group, l_a = s_a = R.from;
+      for (int n = 0; n < NB; n++) dk[n] = dv[n] = acc4{};
     };
     clear();
+    copies = steps = Walk{head0, R.from};
     through_tiles<CAREFUL>(all, load, step);
-    if (!CAREFUL && __syncthreads_or(R.real() && ((DK && not_finite(dk, A.scale)) || (DV && not_finite(dv, 1.f))))) return false;
+    bool odd = false;
+#pragma unroll
+    for (int n = 0; n < NB; n++)
+#pragma unroll
+      for (int r = 0; r < 4; r++) odd |= !(fabsf(dk[n][r] * A.scale) < INFINITY) || !(fabsf(dv[n][r]) < INFINITY);
+    if (!CAREFUL && __syncthreads_or(R.real() && odd)) return false;
     if (j < A.T) {
       if (!R.real()) clear();
-      if (DK) store_rows<T>(A.dk, kvh, j, dk, n0, A.scale, A.d, lane);
-      if (DV) store_rows<T>(A.dv, kvh, j, dv, n0, 1.f, A.d, lane);
+      store_sums<T>(A, A.dk, 0, kvh, part, j, dk, n0, A.scale, lane);
+      store_sums<T>(A, A.dv, 1, kvh, part, j, dv, n0, 1.f, lane);
     }
     return true;
   };
@@ -727,26 +904,30 @@ __device__ __forceinline__ bool dkv_tile(const AttnArgs &A, int kvh, int tile, c
   for (int n0 = 0; n0 < DC / 32; n0++) (void)pass(n0);
   return true;
 }
-
-// Up to 64 dimensions a wave holds both sums (4 products a tile).  Beyond,
-// both would take more than the 256 registers that let two waves share a SIMD:
-// a workgroup takes dv (2 products) or dk (3), which computes the scores twice.
 template <class T, int DP, int DC>
 __global__ void __launch_bounds__(kWaves * 64, 2) k_attention_dkv(AttnArgs A) {
   constexpr int kTile = kStep * DP * 2;
   __shared__ __align__(16) char s_q0[kTile], s_q1[kTile], s_g0[kTile], s_g1[kTile];
   __shared__ __align__(16) float s_r0[2 * kStep], s_r1[2 * kStep];  // lse and D of the rows
   __shared__ int s_reach[2][kWaves];
-  auto run = [&](auto dk, auto dv, int item) {
-    constexpr bool DK = decltype(dk)::value, DV = decltype(dv)::value;
-    const int kvh = item / A.tiles, tile = item % A.tiles;
-    if (!dkv_tile<T, DP, DC, DK, DV, false>(A, kvh, tile, s_q0, s_q1, s_g0, s_g1, s_r0, s_r1, s_reach))
-      (void)dkv_tile<T, DP, DC, DK, DV, true>(A, kvh, tile, s_q0, s_q1, s_g0, s_g1, s_r0, s_r1, s_reach);
-  };
-  const int item = item_of(blockIdx.x, gridDim.x);
-  if constexpr (DC <= 64) run(std::true_type{}, std::true_type{}, item);
-  else if (item & 1) run(std::true_type{}, std::false_type{}, item >> 1);
-  else run(std::false_type{}, std::true_type{}, item >> 1);
+  if (!dkv_tile<T, DP, DC, false>(A, s_q0, s_q1, s_g0, s_g1, s_r0, s_r1, s_reach))
+    (void)dkv_tile<T, DP, DC, true>(A, s_q0, s_q1, s_g0, s_g1, s_r0, s_r1, s_reach);
+}
+
+// dk and dv as the sums of their parts, in the order of the query heads.
+template <class T>
+__global__ void __launch_bounds__(256) k_attention_join(AttnArgs A) {
+  const int64_t n = (int64_t)A.T * A.K * A.d, at = ((int64_t)blockIdx.x * 256 + threadIdx.x) * 4;
+  if (at >= n) return;
+  const int c = (int)(at % A.d), kvh = (int)(at / A.d % A.K);
+  const int64_t t = at / A.d / A.K;
+#pragma unroll
+  for (int which = 0; which < 2; which++) {
+    acc4 sum = {0, 0, 0, 0};
+    for (int p = 0; p < A.parts; p++) sum += *reinterpret_cast<const acc4 *>(A.part + (p * 2 + which) * n + at);
+    const Rows &x = which ? A.dv : A.dk;
+    *reinterpret_cast<u32x2 *>(x.p + 2 * (t * x.row + kvh * x.head + c)) = u32x2{pack2<T>(sum[0], sum[1]), pack2<T>(sum[2], sum[3])};
+  }
 }
 
 // ------------------------------------------------------------- entry points
@@ -770,10 +951,19 @@ int check_attn(const cel_attn *a, const char *fn) {
     return set_error(CEL_E_ARG, "%s: dim %d is not a multiple of 8 in 8..128", fn, a->dim);
   if (!(a->scale > 0.f) || !std::isfinite(a->scale) || !std::isfinite(8.f / (a->scale * kLog2e)))
     return set_error(CEL_E_ARG, "%s: scale %g is not positive and finite", fn, (double)a->scale);
-  if (((int64_t)a->tokens + kBlock - 1) / kBlock * a->heads > INT32_MAX)
+  if (((int64_t)a->tokens + kKeyBlock - 1) / kKeyBlock * a->heads > INT32_MAX)
     return set_error(CEL_E_ARG, "%s: %d tokens of %d heads", fn, a->tokens, a->heads);
   if (!a->seq_ptr) return set_error(CEL_E_ARG, "%s: seq_ptr is NULL", fn);
   return CEL_OK;
+}
+// Into how many workgroups a tile of keys deals out the query heads that share
+// them: as many as bring eight workgroups to each of the 256 compute units (the
+// tiles at a long sequence's beginning take many times the average), each with the
+// same number of heads but the last.
+int parts_of(const cel_attn *a) {
+  const int64_t group = a->heads / a->kv_heads, tiles = ((int64_t)a->tokens + kKeyBlock - 1) / kKeyBlock;
+  const int64_t per = std::max<int64_t>(1, group * tiles * a->kv_heads / 2048);
+  return per >= group ? 1 : (int)((group + per - 1) / per);
 }
 Rows rows_of(const cel_rows *x) { return Rows{static_cast<char *>(x->p), x->row, x->head}; }
 AttnArgs args_of(const cel_attn *a) {
@@ -786,27 +976,39 @@ AttnArgs args_of(const cel_attn *a) {
   return A;
 }
 
-// f<T, DP, DC> for the call's type and dimension: rows are staged DP wide (a
-// power of two, for the chunks' order), products run over DC dimensions.
-#define CEL_BY_DIM(T, kernel, grid)                                                     \
-  do {                                                                                  \
-    if (A.d <= 32) kernel<T, 64, 32><<<grid, kWaves * 64, 0, s>>>(A);                   \
-    else if (A.d <= 64) kernel<T, 64, 64><<<grid, kWaves * 64, 0, s>>>(A);              \
-    else if (A.d <= 96) kernel<T, 128, 96><<<grid, kWaves * 64, 0, s>>>(A);             \
-    else kernel<T, 128, 128><<<grid, kWaves * 64, 0, s>>>(A);                           \
+// kernel<T, DP, DC> for the call's type and dimension: rows are staged DP wide
+// (a power of two, for the chunks' order), products run over DC dimensions.
+#define CEL_LAUNCH(kernel, T, DP, DC) kernel<T, DP, DC><<<grid, kWaves * 64, 0, s>>>(A)
+#define CEL_SMALL(kernel, T)                        \
+  do {                                                     \
+    if (A.d <= 32) CEL_LAUNCH(kernel, T, 64, 32);   \
+    else CEL_LAUNCH(kernel, T, 64, 64);             \
   } while (0)
-#define CEL_BY_TYPE(kernel, grid)                                                       \
-  do {                                                                                  \
-    KTimer kt(s, #kernel);                                                              \
-    if (a->type == CEL_BF16) CEL_BY_DIM(__bf16, kernel, grid);                          \
-    else CEL_BY_DIM(_Float16, kernel, grid);                                            \
-    CEL_HIP(hipGetLastError());                                                         \
+#define CEL_LARGE(kernel, T)                        \
+  do {                                                     \
+    if (A.d <= 96) CEL_LAUNCH(kernel, T, 128, 96);  \
+    else CEL_LAUNCH(kernel, T, 128, 128);           \
+  } while (0)
+#define CEL_BY_TYPE(which, kernel)                  \
+  do {                                                     \
+    KTimer kt(s, #kernel);                                 \
+    if (a->type == CEL_BF16) which(kernel, __bf16); \
+    else which(kernel, _Float16);                   \
+    CEL_HIP(hipGetLastError());                            \
   } while (0)
 
 }  // namespace
 }  // namespace cel
 
 using namespace cel;
+
+extern "C" int64_t cel_attention_grad_scratch(const cel_attn *a) {
+  const int rc = check_attn(a, "cel_attention_grad_scratch");
+  if (rc) return rc;
+  const int parts = parts_of(a);
+  const int64_t rows = 2 * (int64_t)a->heads * a->tokens;
+  return 4 * (rows + (parts > 1 ? 2 * (int64_t)parts * a->tokens * a->kv_heads * a->dim : 0));
+}
 
 extern "C" int cel_attention(const cel_attn *a, const cel_rows *out, float *lse, hipStream_t s) {
   const char *fn = "cel_attention";
@@ -820,12 +1022,14 @@ extern "C" int cel_attention(const cel_attn *a, const cel_rows *out, float *lse,
   AttnArgs A = args_of(a);
   A.out = rows_of(out);
   A.lse = lse;
-  CEL_BY_TYPE(k_attention, A.tiles * A.H);
+  const int grid = A.tiles * A.H;
+  if (a->dim <= 64) CEL_BY_TYPE(CEL_SMALL, k_attention);
+  else CEL_BY_TYPE(CEL_LARGE, k_attention);
   return CEL_OK;
 }
 
 extern "C" int cel_attention_grad(const cel_attn *a, const cel_rows *out, const float *lse, const cel_rows *dout,
-                                  float *scratch, const cel_rows *dq, const cel_rows *dk, const cel_rows *dv,
+                                  void *scratch_, const cel_rows *dq, const cel_rows *dk, const cel_rows *dv,
                                   hipStream_t s) {
   const char *fn = "cel_attention_grad";
   int rc = check_attn(a, fn);
@@ -836,12 +1040,26 @@ extern "C" int cel_attention_grad(const cel_attn *a, const cel_rows *out, const 
       (rc = check_rows(dout, a, fn, "dout")) || (rc = check_rows(dq, a, fn, "dq")) ||
       (rc = check_rows(dk, a, fn, "dk")) || (rc = check_rows(dv, a, fn, "dv")))
     return rc;
+  float *scratch = static_cast<float *>(scratch_);
   if (!lse || !scratch) return set_error(CEL_E_ARG, "%s: lse or scratch is NULL", fn);
   AttnArgs A = args_of(a);
   A.out = rows_of(out), A.dout = rows_of(dout), A.dq = rows_of(dq), A.dk = rows_of(dk), A.dv = rows_of(dv);
   A.lse = const_cast<float *>(lse);
   A.rows = scratch;
-  CEL_BY_TYPE(k_attention_dq, A.tiles * A.H);
-  CEL_BY_TYPE(k_attention_dkv, A.tiles * A.K * (A.d <= 64 ? 1 : 2));
+  int grid = A.tiles * A.H;
+  if (a->dim <= 64) CEL_BY_TYPE(CEL_SMALL, k_attention_dq);
+  else CEL_BY_TYPE(CEL_LARGE, k_attention_dq);
+  A.parts = parts_of(a);
+  A.part = scratch + 2 * (int64_t)a->heads * a->tokens;
+  grid = (A.T + kKeyBlock - 1) / kKeyBlock * A.K * A.parts;
+  if (a->dim <= 64) CEL_BY_TYPE(CEL_SMALL, k_attention_dkv);
+  else CEL_BY_TYPE(CEL_LARGE, k_attention_dkv);
+  if (A.parts > 1) {
+    KTimer kt(s, "k_attention_join");
+    const int64_t blocks = ((int64_t)A.T * A.K * A.d / 4 + 255) / 256;
+    if (a->type == CEL_BF16) k_attention_join<__bf16><<<(unsigned)blocks, 256, 0, s>>>(A);
+    else k_attention_join<_Float16><<<(unsigned)blocks, 256, 0, s>>>(A);
+    CEL_HIP(hipGetLastError());
+  }
   return CEL_OK;
 }
