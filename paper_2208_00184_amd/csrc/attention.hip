@@ -715,11 +715,16 @@ __device__ inline acc4 mma16(u32x4 a, u32x4 b, acc4 c) {
   else
     return __builtin_amdgcn_mfma_f32_16x16x32_f16(__builtin_bit_cast(v8, a), __builtin_bit_cast(v8, b), c, 0, 0, 0);
 }
-// The chunks' order for 16 columns of eight rows at once.
+// The chunks' order here.  A transposed read takes two chunks each of eight
+// rows at once (0..7, 8..15), which have to differ in their upper bits.  A plain
+// read takes one chunk of rows 0..3 and 12..15 with the next chunk of rows 4..11
+// (that is how a wave's 16-byte reads are grouped), or the other way round:
+// each of these halves fills whole pairs of chunks.
 template <int DP>
 struct Swz16 {
   static __device__ int of(int r) {
-    return DP == 128 ? ((r & 7) << 1) | ((r >> 3) & 1) : (((r >> 1) & 3) << 1) | ((r >> 3) & 1);
+    return DP == 128 ? (((r & 7) ^ ((r >> 1) & 4)) << 1) | ((r >> 3) & 1)
+                     : ((((r >> 1) & 3) ^ ((r >> 2) & 2)) << 1) | ((r >> 3) & 1);
   }
 };
 template <int DP>
