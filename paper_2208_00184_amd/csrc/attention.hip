@@ -380,17 +380,20 @@ __device__ __forceinline__ void through_tiles(int n, Load load, Step step) {
     step(t + 1, Buffer<1>{});
   }
 }
-// Orders what the compiler schedules here: N matrix instructions, each fed by
-// READS reads of LDS, with the reads AHEAD instructions before their use.
-template <int N, int READS, int AHEAD>
-__device__ __forceinline__ void feed() {
-  __builtin_amdgcn_sched_group_barrier(0x100, AHEAD * READS, 0);
+// N matrix instructions, instruction x fed by read(x) from LDS kAhead instructions
+// before: left to itself, or asked for this order as a preference, the compiler reads each
+// operand right before its use where it runs short of registers, and waits.
+template <int N, class Read, class Use>
+__device__ __forceinline__ void feed(Read read, Use use) {
+  u32x4 ring[kAhead + 1];
 #pragma unroll
-  for (int i = 0; i < N - AHEAD; i++) {
-    __builtin_amdgcn_sched_group_barrier(0x008, 1, 0);
-    __builtin_amdgcn_sched_group_barrier(0x100, READS, 0);
+  for (int x = 0; x < kAhead && x < N; x++) ring[x] = read(x);
+#pragma unroll
+  for (int x = 0; x < N; x++) {
+    if (x + kAhead < N) ring[(x + kAhead) % (kAhead + 1)] = read(x + kAhead);
+    use(x, ring[x % (kAhead + 1)]);
+    __builtin_amdgcn_sched_barrier(0x6);  // vector and scalar arithmetic may still move
   }
-  __builtin_amdgcn_sched_group_barrier(0x008, AHEAD, 0);
 }
 // acc += (columns of the staged tile)^T b, see careful_product.
 template <class T, int DP, bool CAREFUL, int NB, int J>
@@ -400,11 +403,8 @@ __device__ __forceinline__ void product(const char *lds, acc16 (&acc)[NB], const
     careful_product<T, DP, NB, J>(lds, acc, b, cols, lo, hi, lane, a);
   } else {
     cols = fresh(cols, a);
-#pragma unroll
-    for (int j = 0; j < J; j++)
-#pragma unroll
-      for (int n = 0; n < NB; n++) acc[n] = Half<T>::mma(cols_at<DP>(lds, cols, n, j), b[j], acc[n]);
-    feed<J * NB, 2, (kAhead < J * NB ? kAhead : J * NB)>();
+    feed<J * NB>([&](int x) { return cols_at<DP>(lds, cols, x % NB, x / NB); },
+                 [&](int x, u32x4 f) { acc[x % NB] = Half<T>::mma(f, b[x / NB], acc[x % NB]); });
   }
 }
 // x = rows 32 t .. of a staged tile times f, y = rows 32 u .. of another times g.
@@ -412,15 +412,15 @@ template <class T, int DP, int KK>
 __device__ __forceinline__ void rows_products(acc16 &x, const char *lds, int t, const u32x4 (&f)[KK], acc16 &y,
                                               const char *lds2, int u, const u32x4 (&g)[KK], int rows, int a) {
   rows = fresh(rows, a);
-  x = y = acc16{};
-#pragma unroll
-  for (int kk = 0; kk < KK; kk++) {
-    x = Half<T>::mma(rows_at<DP>(lds, rows, t, kk), f[kk], x);
-    y = Half<T>::mma(rows_at<DP>(lds2, rows, u, kk), g[kk], y);
-  }
-  feed<2 * KK, 1, kAhead>();
+  feed<2 * KK>([&](int n) { return rows_at<DP>(n & 1 ? lds2 : lds, rows, n & 1 ? u : t, n / 2); },
+               [&](int n, u32x4 z) {
+                 if (n & 1) y = Half<T>::mma(z, g[n / 2], n > 1 ? y : acc16{});
+                 else x = Half<T>::mma(z, f[n / 2], n > 1 ? x : acc16{});
+               });
 }
-// x's entries at 32 t .. of a tile outside lo .. hi, replaced.
+// x's entries at 32 t .. of a tile outside lo .. hi, replaced.  The empty
+// statement hides where the bounds come from: they are compared with constants, not
+// with 16 numbers of each lane's that would stay in registers across the loop.
 __device__ __forceinline__ void mask(acc16 &x, int t, int lo, int hi, float by, int lane) {
 #pragma unroll
   for (int r = 0; r < 16; r++) {
@@ -761,15 +761,12 @@ template <class T, int DP, int KK>
 __device__ __forceinline__ void rows16_products(acc4 (&x)[4], const char *lds, const u32x4 (&f)[KK], acc4 (&y)[4],
                                                 const char *lds2, const u32x4 (&g)[KK], int rows, int a) {
   rows = fresh(rows, a);
-#pragma unroll
-  for (int kk = 0; kk < KK; kk++)
-#pragma unroll
-    for (int t = 0; t < 4; t++) x[t] = mma16<T>(rows16_at<DP>(lds, rows, t, kk), f[kk], kk ? x[t] : acc4{});
-#pragma unroll
-  for (int kk = 0; kk < KK; kk++)
-#pragma unroll
-    for (int t = 0; t < 4; t++) y[t] = mma16<T>(rows16_at<DP>(lds2, rows, t, kk), g[kk], kk ? y[t] : acc4{});
-  feed<8 * KK, 1, kAhead>();
+  feed<8 * KK>([&](int n) { return rows16_at<DP>(n < 4 * KK ? lds : lds2, rows, n % 4, n / 4 % KK); },
+               [&](int n, u32x4 z) {
+                 const int t = n % 4, kk = n / 4 % KK;
+                 if (n < 4 * KK) x[t] = mma16<T>(z, f[kk], kk ? x[t] : acc4{});
+                 else y[t] = mma16<T>(z, g[kk], kk ? y[t] : acc4{});
+               });
 }
 // acc[n] += (columns of the staged tile)^T b, and its careful form: see product and careful_product.
 template <class T, int DP, bool CAREFUL, int NB>
@@ -777,11 +774,8 @@ __device__ __forceinline__ void product16(const char *lds, acc4 (&acc)[NB], cons
                                           int lo, int hi, int lane, int a0) {
   cols = fresh(cols, a0);
   if (!CAREFUL || !masked) {
-#pragma unroll
-    for (int j = 0; j < 2; j++)
-#pragma unroll
-      for (int n = 0; n < NB; n++) acc[n] = mma16<T>(cols16_at<DP>(lds, cols, n, j), b[j], acc[n]);
-    feed<2 * NB, 2, (kAhead < 2 * NB ? kAhead : 2 * NB)>();
+    feed<2 * NB>([&](int x) { return cols16_at<DP>(lds, cols, x % NB, x / NB); },
+                 [&](int x, u32x4 f) { acc[x % NB] = mma16<T>(f, b[x / NB], acc[x % NB]); });
     return;
   }
 #pragma unroll
@@ -860,8 +854,8 @@ __device__ __forceinline__ bool dkv_tile(const AttnArgs &A, char *s_q0, char *s_
           dp[t][r] = s[t][r] * (dp[t][r] - s_D[16 * t + g4 + r]);
         }
       if (masked) {
-        asm volatile("");  // as in mask
-        const int from = lo - g4, to = hi - g4;
+        int from = lo - g4, to = hi - g4;
+        asm volatile("" : "+v"(from), "+v"(to));  // as in mask
 #pragma unroll
         for (int t = 0; t < 4; t++)
 #pragma unroll
