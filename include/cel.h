@@ -411,8 +411,8 @@ int cel_embed(const cel_embed_args *a, const void *table, void *out, hipStream_t
 /* The gradient of cel_embed's table at dx, the gradient of its rows:
  * grad_v = scale * sum over t with ids_t = v of dx_t, 0 for a word that does
  * not occur (every element of grad is written).  Tokens are sorted by id and
- * added in 32 bits in the batch's order, with every aligned 64 sorted tokens
- * of one word added up first: the same inputs give the same bits.
+ * added in 32 bits in the batch's order, every 32 tokens of a word summed first:
+ * the same inputs give the same bits.
  * Inputs: dx [tokens] rows of `hidden` values, `stride` apart; scratch of
  * cel_embed_grad_scratch(tokens, vocab, hidden) bytes, aligned to 256.
  * Outputs: grad [vocab][hidden], of grad_type: the rows' type or CEL_F32.

@@ -11,9 +11,8 @@
 // stand together in the order of the batch, and then gives each table row to
 // one wave (of each slice of columns), which adds its tokens in 32 bits in that
 // order: no atomics, the same bits every time.  Words follow Zipf's law, so one may
-// have a tenth of all tokens: every aligned chunk of kChunk sorted tokens that
-// is one word through and through is summed beforehand by a wave of its own,
-// and the row adds the chunks' sums.
+// have a tenth of all tokens: every kChunk tokens of a word are summed beforehand
+// by a wave of their own, and the row adds these sums and what is left.
 #include <algorithm>
 #include <cmath>
 
@@ -22,84 +21,93 @@
 namespace cel {
 namespace {
 
-constexpr int kChunk = 64;       // sorted tokens of one partial sum
+constexpr int kChunk = 32;       // sorted tokens of one partial sum
 constexpr int kDigit = 9;        // bits of an id sorted at once: two passes up to 262,143 words
 constexpr int kBins = 1 << kDigit;
 constexpr int kSortB = 1024, kSortW = kSortB / 64;
-constexpr int kOne = 8;          // tokens a thread holds in the sort by one workgroup
-constexpr int kSegs = 4;         // 16-byte chunks a lane handles of a row slice
+constexpr int kRankMost = 16384; // tokens that are ranked against each other
+constexpr int kRankB = 256, kRankEach = 8, kRankTokens = kRankB / kRankEach;  // threads, threads a token, tokens
+constexpr int kSlice = 1024;     // columns a wave handles
+constexpr int kTogether = 4;     // rows of the lookup that a wave has on their way at once
 constexpr int kRowsAt = 4;       // table rows a wave writes one behind the other
 
-// 16 bytes at any address of the element type.
-struct __attribute__((packed, aligned(2))) Raw16 {
-  uint32_t w[4];
+// BYTES at any address of the element type, as one access.
+template <int BYTES>
+struct __attribute__((packed, aligned(2))) Raw {
+  uint32_t w[BYTES / 4];
 };
-template <class T>
-struct Vec {
-  static constexpr int N = 16 / sizeof(T);
+// A wave's kSlice columns are S chunks of 64 lanes with E values each; E values
+// of the rows written are 16 bytes.
+template <class O>
+struct Shape {
+  static constexpr int E = 16 / sizeof(O), S = kSlice / 64 / E;
 };
-template <class T>
-__device__ inline void load_vec(float (&f)[Vec<T>::N], const T *p, int count) {
-  if (count == Vec<T>::N) {
-    const Raw16 r = *reinterpret_cast<const Raw16 *>(p);
-    T x[Vec<T>::N];
-    __builtin_memcpy(x, &r, 16);
-#pragma unroll
-    for (int e = 0; e < Vec<T>::N; e++) f[e] = (float)x[e];
+template <class T, int E>
+__device__ inline Raw<E * sizeof(T)> load_raw(const T *p, int64_t left) {
+  Raw<E * sizeof(T)> r{};
+  if (left >= E) {
+    r = *reinterpret_cast<const Raw<E * sizeof(T)> *>(p);
   } else {
+    T x[E];
 #pragma unroll
-    for (int e = 0; e < Vec<T>::N; e++) f[e] = e < count ? (float)p[e] : 0.f;
+    for (int e = 0; e < E; e++) x[e] = e < left ? p[e] : (T)0.f;
+    __builtin_memcpy(&r, x, sizeof r);
   }
+  return r;
 }
-// N values rounded to O, 16 bytes at a time.
-template <class O, int N>
-__device__ inline void store_vec(O *p, const float (&f)[N], int count) {
-  O x[N];
+template <class T, int E>
+__device__ inline void values(float (&f)[E], const Raw<E * sizeof(T)> &r) {
+  T x[E];
+  __builtin_memcpy(x, &r, sizeof r);
 #pragma unroll
-  for (int e = 0; e < N; e++) x[e] = (O)f[e];
-  if (count == N) {
+  for (int e = 0; e < E; e++) f[e] = (float)x[e];
+}
+template <class O, int E>
+__device__ inline void store_values(O *p, const float (&f)[E], float by, int64_t left) {
+  O x[E];
 #pragma unroll
-    for (int b = 0; b < (int)(N * sizeof(O)) / 16; b++) {
-      Raw16 r;
-      __builtin_memcpy(&r, x + b * Vec<O>::N, 16);
-      *reinterpret_cast<Raw16 *>(p + b * Vec<O>::N) = r;
-    }
-    if constexpr (N * sizeof(O) % 16 != 0) {
-#pragma unroll
-      for (int e = N * sizeof(O) / 16 * Vec<O>::N; e < N; e++) p[e] = x[e];
-    }
+  for (int e = 0; e < E; e++) x[e] = (O)(f[e] * by);
+  if (left >= E) {
+    Raw<E * sizeof(O)> r;
+    __builtin_memcpy(&r, x, sizeof r);
+    *reinterpret_cast<Raw<E * sizeof(O)> *>(p) = r;
   } else {
 #pragma unroll
-    for (int e = 0; e < N; e++)
-      if (e < count) p[e] = x[e];
+    for (int e = 0; e < E; e++)
+      if (e < left) p[e] = x[e];
   }
 }
 
-// A wave takes one token and kSegs * 64 chunks of its row.
+// A wave takes kTogether tokens and kSlice columns of their rows: every load is
+// on its way before the first store.
 template <class T, class I>
 __global__ void __launch_bounds__(256) k_embed(const T *table, int64_t stride, int64_t vocab, const I *ids, int64_t tokens,
                                                int64_t h, int slices, float scale, T *out) {
-  constexpr int N = Vec<T>::N;
-  const int lane = threadIdx.x & 63;
-  const int64_t task = (int64_t)blockIdx.x * 4 + (threadIdx.x >> 6);
-  const int64_t t = task / slices;
-  if (t >= tokens) return;
-  const int64_t id = ids[t], c0 = (task % slices) * (kSegs * 64 * N) + lane * N;
-  const bool in = id >= 0 && id < vocab;
-  float f[kSegs][N];
+  constexpr int E = Shape<T>::E, S = Shape<T>::S;
+  const int64_t task = (int64_t)blockIdx.x * 4 + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int64_t t0 = task / slices * kTogether, c0 = (task % slices) * kSlice + (threadIdx.x & 63) * E;
+  if (t0 >= tokens) return;
+  Raw<16> r[kTogether][S];
 #pragma unroll
-  for (int u = 0; u < kSegs; u++) {
-    const int64_t c = c0 + u * 64 * N;
+  for (int k = 0; k < kTogether; k++) {
+    const int64_t id = t0 + k < tokens ? (int64_t)ids[t0 + k] : -1;
+    const bool in = id >= 0 && id < vocab;
 #pragma unroll
-    for (int e = 0; e < N; e++) f[u][e] = 0.f;
-    if (in && c < h) load_vec<T>(f[u], table + id * stride + c, (int)min((int64_t)N, h - c));
+    for (int u = 0; u < S; u++) {
+      const int64_t c = c0 + u * 64 * E;
+      r[k][u] = in && c < h ? load_raw<T, E>(table + id * stride + c, h - c) : Raw<16>{};
+    }
   }
 #pragma unroll
-  for (int u = 0; u < kSegs; u++) {
-    const int64_t c = c0 + u * 64 * N;
+  for (int k = 0; k < kTogether; k++) {
+    if (t0 + k >= tokens) break;
 #pragma unroll
-    for (int e = 0; e < N; e++) f[u][e] *= scale;
-    if (c < h) store_vec<T, N>(out + t * h + c, f[u], (int)min((int64_t)N, h - c));
+    for (int u = 0; u < S; u++) {
+      const int64_t c = c0 + u * 64 * E;
+      float f[E];
+      values<T, E>(f, r[k][u]);
+      if (c < h) store_values<T, E>(out + (t0 + k) * h + c, f, scale, h - c);
+    }
   }
 }
 
@@ -124,7 +132,7 @@ __device__ inline uint64_t same_digit(uint32_t digit, bool in) {
 }
 // Counts this lane's digit in its wave's column of counters and returns how
 // many tokens before it, in the wave's order, had the same.
-__device__ inline uint32_t rank_in_wave(uint32_t (*count)[kSortW], int wave, int lane, uint32_t digit, bool in) {
+__device__ inline uint32_t rank_in_wave(uint32_t (*count)[kSortW + 1], int wave, int lane, uint32_t digit, bool in) {
   const uint64_t m = same_digit(digit, in);
   uint32_t before = 0;
   if (in) before = count[digit][wave];
@@ -133,89 +141,47 @@ __device__ inline uint32_t rank_in_wave(uint32_t (*count)[kSortW], int wave, int
   lds_order();
   return before + (uint32_t)__builtin_popcountll(m & ((uint64_t(1) << lane) - 1));
 }
-// Exclusive sums over the digits, and inside a digit over the waves; base:
-// what each digit starts from besides, or NULL.  Called by the whole workgroup.
-__device__ inline void start_counts(uint32_t (*count)[kSortW], uint32_t *s_sum, const uint32_t *base, int tid) {
-  const int lane = tid & 63, wave = tid >> 6;
-  uint32_t all = 0;
+// Turns every digit's counts into where each wave's tokens of it begin: base, and the waves before.
+__device__ inline void start_counts(uint32_t (*count)[kSortW + 1], const uint32_t *base, int tid) {
   if (tid < kBins) {
+    uint32_t at = base[tid];
 #pragma unroll
     for (int w = 0; w < kSortW; w++) {
       const uint32_t x = count[tid][w];
-      count[tid][w] = all;
-      all += x;
+      count[tid][w] = at;
+      at += x;
     }
-  }
-  if (!base) {
-    uint32_t up = all;
-    for (int o = 1; o < 64; o <<= 1) {
-      const uint32_t y = __shfl_up(up, o);
-      if (lane >= o) up += y;
-    }
-    if (tid < kBins && lane == 63) s_sum[wave] = up;
-    __syncthreads();
-    if (tid < kBins) {
-      uint32_t b = up - all;
-      for (int w = 0; w < wave; w++) b += s_sum[w];
-      all = b;
-    }
-  } else if (tid < kBins) {
-    all = base[tid];
-  }
-  if (tid < kBins) {
-#pragma unroll
-    for (int w = 0; w < kSortW; w++) count[tid][w] += all;
   }
   __syncthreads();
 }
 
-// Up to kOne * kSortB tokens by one workgroup, every pass through LDS.
+// Few tokens: every token's place is the number of tokens that come before it,
+// counted against all of them, kRankEach threads a token.  Tokens squared
+// comparisons, but one launch and no dependent passes.
 template <class I>
-__global__ void __launch_bounds__(kSortB) k_embed_sort_one(const I *ids, int tokens, int64_t vocab, int bits, uint32_t *keys,
-                                                           uint32_t *order) {
-  __shared__ uint32_t count[kBins][kSortW];
-  __shared__ uint32_t s_key[kOne * kSortB], s_pos[kOne * kSortB], s_sum[kSortW];
-  const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
-  uint32_t key[kOne], pos[kOne];
-  const int mine = wave * kOne * 64 + lane;  // a wave's tokens stand together
-#pragma unroll
-  for (int u = 0; u < kOne; u++) {
-    pos[u] = mine + u * 64;
-    key[u] = (int)pos[u] < tokens ? key_of(ids, pos[u], vocab) : 0;
-  }
-  for (int shift = 0; shift < bits; shift += kDigit) {
-    for (int i = tid; i < kBins * kSortW; i += kSortB) (&count[0][0])[i] = 0;
-    __syncthreads();
-    uint32_t rank[kOne];
-#pragma unroll
-    for (int u = 0; u < kOne; u++) rank[u] = rank_in_wave(count, wave, lane, digit_of(key[u], shift), mine + u * 64 < tokens);
-    __syncthreads();
-    start_counts(count, s_sum, nullptr, tid);
-#pragma unroll
-    for (int u = 0; u < kOne; u++) {
-      if (mine + u * 64 >= tokens) continue;
-      const uint32_t to = count[digit_of(key[u], shift)][wave] + rank[u];
-      s_key[to] = key[u];
-      s_pos[to] = pos[u];
-    }
-    __syncthreads();
-#pragma unroll
-    for (int u = 0; u < kOne; u++) {
-      if (mine + u * 64 >= tokens) continue;
-      key[u] = s_key[mine + u * 64];
-      pos[u] = s_pos[mine + u * 64];
-    }
+__global__ void __launch_bounds__(kRankB) k_embed_rank(const I *ids, int tokens, int64_t vocab, uint32_t *keys,
+                                                       uint32_t *order) {
+  __shared__ __align__(16) uint32_t s_key[kRankMost];
+  const int tid = threadIdx.x;
+  for (int t = tid; t < (tokens + 3) / 4 * 4; t += kRankB) s_key[t] = t < tokens ? key_of(ids, t, vocab) : ~0u;
+  __syncthreads();
+  const int t = blockIdx.x * kRankTokens + tid / kRankEach, part = tid % kRankEach;
+  const uint32_t key = t < tokens ? s_key[t] : 0;
+  uint32_t before = 0;
+  for (int i = 4 * part; i < tokens; i += 4 * kRankEach) {
+    const uint4 k = *reinterpret_cast<const uint4 *>(&s_key[i]);
+    before += (k.x < key + (i < t)) + (k.y < key + (i + 1 < t)) + (k.z < key + (i + 2 < t)) + (k.w < key + (i + 3 < t));
   }
 #pragma unroll
-  for (int u = 0; u < kOne; u++) {
-    if (mine + u * 64 >= tokens) continue;
-    keys[mine + u * 64] = key[u];
-    order[mine + u * 64] = pos[u];
+  for (int o = 1; o < kRankEach; o <<= 1) before += __shfl_xor(before, o);
+  if (t < tokens && part == 0) {
+    keys[before] = key;
+    order[before] = t;
   }
 }
 
-// The same by several workgroups, each of which holds `tile` tokens (a
-// multiple of kSortB): a pass counts digits per tile (table [tiles][kBins]),
+// Many tokens: a radix sort by several workgroups, each of which holds `tile`
+// tokens (a multiple of 2 kSortB): a pass counts digits per tile (table [tiles][kBins]),
 // and then puts every token in its place.  first: from ids, else from keys.
 template <class I>
 __global__ void __launch_bounds__(kSortB) k_embed_count(const I *ids, const uint32_t *keys, bool first, int64_t tokens,
@@ -234,7 +200,7 @@ template <class I>
 __global__ void __launch_bounds__(kSortB) k_embed_move(const I *ids, const uint32_t *keys, const uint32_t *order, bool first,
                                                        int64_t tokens, int64_t vocab, int64_t tile, int shift,
                                                        const uint32_t *table, uint32_t *keys_to, uint32_t *order_to) {
-  __shared__ uint32_t count[kBins][kSortW];
+  __shared__ uint32_t count[kBins][kSortW + 1];  // one more: a digit's counters start in different banks
   __shared__ uint32_t s_base[kBins], s_sum[kSortW];
   const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
   uint32_t all = 0, before = 0;
@@ -258,7 +224,7 @@ __global__ void __launch_bounds__(kSortB) k_embed_move(const I *ids, const uint3
   }
   const int64_t t0 = blockIdx.x * tile, t1 = min(tokens, t0 + tile);
   for (int64_t at = t0; at < t1; at += 2 * kSortB) {  // two tokens a thread at once, in the waves' order
-    for (int i = tid; i < kBins * kSortW; i += kSortB) (&count[0][0])[i] = 0;
+    for (int i = tid; i < kBins * (kSortW + 1); i += kSortB) (&count[0][0])[i] = 0;
     __syncthreads();
     uint32_t key[2] = {0, 0}, pos[2] = {0, 0}, rank[2];
 #pragma unroll
@@ -278,7 +244,7 @@ __global__ void __launch_bounds__(kSortB) k_embed_move(const I *ids, const uint3
 #pragma unroll
       for (int w = 0; w < kSortW; w++) sum += count[tid][w];
     }
-    start_counts(count, s_sum, s_base, tid);
+    start_counts(count, s_base, tid);
 #pragma unroll
     for (int u = 0; u < 2; u++) {
       if (at + wave * 128 + u * 64 + lane >= t1) continue;
@@ -292,32 +258,44 @@ __global__ void __launch_bounds__(kSortB) k_embed_move(const I *ids, const uint3
 }
 
 // ------------------------------------------------------------ sums by word
-// Sorted tokens [a, b), added in order to the lane's columns; a row or a
-// partial sum alike.
-template <class T>
-__device__ inline void add_tokens(float (&f)[kSegs][Vec<T>::N], const T *dx, int64_t stride, const uint32_t *order, int64_t a,
+// Sorted tokens [a, b), added in order to the lane's columns, kAtOnce rows on
+// their way at a time.
+template <class T, int E, int S>
+__device__ inline void add_tokens(float (&f)[S][E], const T *dx, int64_t stride, const uint32_t *__restrict__ order, int64_t a,
                                   int64_t b, int64_t c0, int64_t h) {
-  constexpr int N = Vec<T>::N;
-  for (int64_t t = a; t < b; t++) {
-    const T *row = dx + (int64_t)order[t] * stride;
+  constexpr int kAtOnce = 8;
+  for (int64_t t = a; t < b; t += kAtOnce) {
+    Raw<E * sizeof(T)> r[kAtOnce][S];
 #pragma unroll
-    for (int u = 0; u < kSegs; u++) {
-      const int64_t c = c0 + u * 64 * N;
-      if (c >= h) continue;
-      float x[N];
-      load_vec<T>(x, row + c, (int)min((int64_t)N, h - c));
+    for (int k = 0; k < kAtOnce; k++) {
+      const T *row = dx + (int64_t)order[t + k < b ? t + k : b - 1] * stride;
 #pragma unroll
-      for (int e = 0; e < N; e++) f[u][e] += x[e];
+      for (int u = 0; u < S; u++) {
+        const int64_t c = c0 + u * 64 * E;
+        if (t + k < b && c < h) r[k][u] = load_raw<T, E>(row + c, h - c);
+      }
     }
+#pragma unroll
+    for (int k = 0; k < kAtOnce; k++)
+#pragma unroll
+      for (int u = 0; u < S; u++) {
+        if (t + k >= b || c0 + u * 64 * E >= h) continue;
+        float x[E];
+        values<T, E>(x, r[k][u]);
+#pragma unroll
+        for (int e = 0; e < E; e++) f[u][e] += x[e];
+      }
   }
 }
 
 // Blocks below `searches`: where each word's tokens begin (start [vocab + 1]).
-// The others: the sums of the chunks that hold one word only (part [chunks][h]).
+// The others: the sums of the words' full chunks (part [tokens / kChunk][h]; a
+// word's chunks are counted from its first token, so that its sum depends on no
+// other word, and chunk p of a word that begins at a lies at a / kChunk + p).
 template <class T>
-__global__ void __launch_bounds__(256) k_embed_parts(const uint32_t *keys, const uint32_t *order, int64_t tokens, int64_t vocab,
-                                                     int searches, uint32_t *start, const T *dx, int64_t stride, int64_t h,
-                                                     int slices, float *part) {
+__global__ void __launch_bounds__(256) k_embed_parts(const uint32_t *__restrict__ keys, const uint32_t *__restrict__ order,
+                                                     int64_t tokens, int64_t vocab, int searches, uint32_t *start, const T *dx,
+                                                     int64_t stride, int64_t h, int slices, float *part) {
   if ((int)blockIdx.x < searches) {
     const int64_t v = (int64_t)blockIdx.x * 256 + threadIdx.x;
     if (v > vocab) return;
@@ -330,61 +308,66 @@ __global__ void __launch_bounds__(256) k_embed_parts(const uint32_t *keys, const
     start[v] = (uint32_t)lo;
     return;
   }
-  constexpr int N = Vec<T>::N;
-  const int lane = threadIdx.x & 63;
-  const int64_t task = (int64_t)(blockIdx.x - searches) * 4 + (threadIdx.x >> 6);
-  const int64_t chunk = task / slices, t0 = chunk * kChunk;
-  if (t0 + kChunk > tokens) return;
-  const uint32_t key = keys[t0];
-  if (key != keys[t0 + kChunk - 1] || key >= (uint32_t)vocab) return;
-  const int64_t c0 = (task % slices) * (kSegs * 64 * N) + lane * N;
-  float f[kSegs][N] = {};
-  add_tokens<T>(f, dx, stride, order, t0, t0 + kChunk, c0, h);
+  constexpr int E = Shape<float>::E, S = Shape<float>::S;
+  const int64_t task = (int64_t)(blockIdx.x - searches) * 4 + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  // The chunk that begins among the kChunk tokens from w on, if there is one,
+  // reaches past the last of them, and holds one kChunk / 2 further or nearer too.
+  const int64_t chunk = task / slices, w = chunk * kChunk;
+  if (w + kChunk > tokens) return;
+  const uint32_t key = keys[w + kChunk - 1];
+  if (key >= (uint32_t)vocab || (keys[w + kChunk / 2 - 1] != key &&
+                                 (w + kChunk * 3 / 2 > tokens || keys[w + kChunk * 3 / 2 - 1] != key)))
+    return;
+  int64_t a = 0, hi = w + kChunk - 1;  // where the word begins
+  while (a < hi) {
+    const int64_t mid = (a + hi) >> 1;
+    if (keys[mid] < key) a = mid + 1;
+    else hi = mid;
+  }
+  const int64_t t0 = a >= w ? a : w + (a - w) % kChunk + (((a - w) % kChunk) ? kChunk : 0);
+  if (t0 + kChunk > tokens || keys[t0 + kChunk - 1] != key) return;
+  const int64_t c0 = (task % slices) * kSlice + (threadIdx.x & 63) * E;
+  float f[S][E] = {};
+  add_tokens<T, E, S>(f, dx, stride, order, t0, t0 + kChunk, c0, h);
 #pragma unroll
-  for (int u = 0; u < kSegs; u++) {
-    const int64_t c = c0 + u * 64 * N;
-    if (c < h) store_vec<float, N>(part + chunk * h + c, f[u], (int)min((int64_t)N, h - c));
+  for (int u = 0; u < S; u++) {
+    const int64_t c = c0 + u * 64 * E;
+    if (c < h) store_values<float, E>(part + chunk * h + c, f[u], 1.f, h - c);
   }
 }
 
-// A wave takes kRowsAt rows of the table and kSegs * 64 chunks of their columns.
+// A wave takes kRowsAt rows of the table and kSlice of their columns.
 template <class T, class O>
-__global__ void __launch_bounds__(256) k_embed_grad(const uint32_t *start, const uint32_t *order, int64_t vocab, const T *dx,
-                                                    int64_t stride, int64_t h, int slices, const float *part, float scale,
-                                                    O *grad) {
-  constexpr int N = Vec<T>::N;
+__global__ void __launch_bounds__(256) k_embed_grad(const uint32_t *start, const uint32_t *__restrict__ order, int64_t vocab,
+                                                    const T *dx, int64_t stride, int64_t h, int slices,
+                                                    const float *__restrict__ part, float scale, O *grad) {
+  constexpr int E = Shape<O>::E, S = Shape<O>::S;
   const int lane = threadIdx.x & 63;
-  const int64_t task = (int64_t)blockIdx.x * 4 + (threadIdx.x >> 6);
+  const int64_t task = (int64_t)blockIdx.x * 4 + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int64_t v0 = task / slices * kRowsAt;
   if (v0 >= vocab) return;
-  const int64_t c0 = (task % slices) * (kSegs * 64 * N) + lane * N;
+  const int64_t c0 = (task % slices) * kSlice + lane * E;
   const uint32_t at = lane <= kRowsAt && v0 + lane <= vocab ? start[v0 + lane] : 0;
+#pragma unroll 1
   for (int r = 0; r < kRowsAt && v0 + r < vocab; r++) {
     const int64_t a = (uint32_t)__builtin_amdgcn_readlane(at, r), b = (uint32_t)__builtin_amdgcn_readlane(at, r + 1);
-    float f[kSegs][N] = {};
+    float f[S][E] = {};
     if (a < b) {
-      const int64_t first = (a + kChunk - 1) / kChunk, last = b / kChunk;  // chunks inside [a, b)
-      if (first < last) {
-        add_tokens<T>(f, dx, stride, order, a, first * kChunk, c0, h);
-        for (int64_t p = first; p < last; p++)
+      const int64_t chunks = (b - a) / kChunk;
+      for (int64_t p = a / kChunk; p < a / kChunk + chunks; p++)
 #pragma unroll
-          for (int u = 0; u < kSegs; u++) {
-            const int64_t c = c0 + u * 64 * N;
+        for (int u = 0; u < S; u++) {
+          const int64_t c = c0 + u * 64 * E;
 #pragma unroll
-            for (int e = 0; e < N; e++)
-              if (c + e < h) f[u][e] += part[p * h + c + e];
-          }
-        add_tokens<T>(f, dx, stride, order, last * kChunk, b, c0, h);
-      } else {
-        add_tokens<T>(f, dx, stride, order, a, b, c0, h);
-      }
+          for (int e = 0; e < E; e++)
+            if (c + e < h) f[u][e] += part[p * h + c + e];
+        }
+      add_tokens<T, E, S>(f, dx, stride, order, a + chunks * kChunk, b, c0, h);
     }
 #pragma unroll
-    for (int u = 0; u < kSegs; u++) {
-      const int64_t c = c0 + u * 64 * N;
-#pragma unroll
-      for (int e = 0; e < N; e++) f[u][e] *= scale;
-      if (c < h) store_vec<O, N>(grad + (v0 + r) * h + c, f[u], (int)min((int64_t)N, h - c));
+    for (int u = 0; u < S; u++) {
+      const int64_t c = c0 + u * 64 * E;
+      if (c < h) store_values<O, E>(grad + (v0 + r) * h + c, f[u], scale, h - c);
     }
   }
 }
@@ -431,8 +414,7 @@ int check_embed(const cel_embed_args *a, const char *fn) {
   return CEL_OK;
 }
 int slices_of(const cel_embed_args *a) {
-  const int64_t per = kSegs * 64 * (a->type == CEL_F32 ? 4 : 8);
-  return (int)((a->hidden + per - 1) / per);
+  return (int)((a->hidden + kSlice - 1) / kSlice);
 }
 int blocks_of(int64_t waves, const char *fn, unsigned *blocks) {
   const int64_t b = (waves + 3) / 4;
@@ -445,7 +427,7 @@ template <class T>
 int embed(const cel_embed_args *a, const void *table, void *out, hipStream_t s) {
   const int slices = slices_of(a);
   unsigned blocks;
-  CEL_TRY(blocks_of(a->tokens * slices, "cel_embed", &blocks));
+  CEL_TRY(blocks_of((a->tokens + kTogether - 1) / kTogether * slices, "cel_embed", &blocks));
   KTimer kt(s, "k_embed");
   if (a->id_bytes == 4)
     k_embed<T, int32_t><<<blocks, 256, 0, s>>>((const T *)table, a->stride, a->vocab, (const int32_t *)a->ids, a->tokens,
@@ -462,9 +444,11 @@ int sort_tokens(const cel_embed_args *a, const Plan &p, char *w, int *in, hipStr
   const I *ids = (const I *)a->ids;
   auto u32 = [&](int64_t at) { return reinterpret_cast<uint32_t *>(w + at); };
   *in = 0;
-  if (a->tokens <= kOne * kSortB) {
-    KTimer kt(s, "k_embed_sort_one");
-    k_embed_sort_one<I><<<1, kSortB, 0, s>>>(ids, (int)a->tokens, a->vocab, p.bits, u32(p.keys[0]), u32(p.order[0]));
+  if (a->tokens == 0) return CEL_OK;
+  if (a->tokens <= kRankMost) {
+    KTimer kt(s, "k_embed_rank");
+    k_embed_rank<I><<<(unsigned)((a->tokens + kRankTokens - 1) / kRankTokens), kRankB, 0, s>>>(
+        ids, (int)a->tokens, a->vocab, u32(p.keys[0]), u32(p.order[0]));
     CEL_HIP(hipGetLastError());
     return CEL_OK;
   }
