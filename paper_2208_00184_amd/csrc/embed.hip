@@ -15,6 +15,7 @@
 // by a wave of their own, and the row adds these sums and what is left.
 #include <algorithm>
 #include <cmath>
+#include <type_traits>
 
 #include "cel_internal.h"
 
@@ -26,8 +27,8 @@ constexpr int kDigit = 9;        // bits of an id sorted at once: two passes up 
 constexpr int kBins = 1 << kDigit;
 constexpr int kSortB = 1024, kSortW = kSortB / 64;
 constexpr int kRankMost = 16384; // tokens that are ranked against each other
-constexpr int kRankB = 256, kRankEach = 8, kRankTokens = kRankB / kRankEach;  // threads, threads a token, tokens
-constexpr int kSlice = 1024;     // columns a wave handles
+constexpr int kRankB = 256, kRankEach = 16, kRankTokens = kRankB / kRankEach;  // threads, threads a token, tokens
+constexpr int kSlice = 512;      // columns a wave handles
 constexpr int kTogether = 4;     // rows of the lookup that a wave has on their way at once
 constexpr int kRowsAt = 4;       // table rows a wave writes one behind the other
 
@@ -62,7 +63,12 @@ __device__ inline void values(float (&f)[E], const Raw<E * sizeof(T)> &r) {
 #pragma unroll
   for (int e = 0; e < E; e++) f[e] = (float)x[e];
 }
-template <class O, int E>
+// NT: past the caches.  An output larger than the memory-side cache (256 MiB)
+// would only push out what is read again (lookup of 32,768 rows of 8,192: 126 us
+// against 221); a smaller one is still there when it is used next (gradient of
+// 50,001 rows of 1,024 in 32 bits: 55 us against 65).
+constexpr int64_t kCached = int64_t(256) << 20;
+template <class O, int E, bool NT>
 __device__ inline void store_values(O *p, const float (&f)[E], float by, int64_t left) {
   O x[E];
 #pragma unroll
@@ -70,7 +76,14 @@ __device__ inline void store_values(O *p, const float (&f)[E], float by, int64_t
   if (left >= E) {
     Raw<E * sizeof(O)> r;
     __builtin_memcpy(&r, x, sizeof r);
-    *reinterpret_cast<Raw<E * sizeof(O)> *>(p) = r;
+    if constexpr (NT) {
+      typedef __attribute__((ext_vector_type(4))) uint32_t u32x4;
+      typedef __attribute__((ext_vector_type(4), aligned(2))) uint32_t any_u32x4;
+      static_assert(sizeof r == 16, "whole stores");
+      __builtin_nontemporal_store(__builtin_bit_cast(u32x4, r), reinterpret_cast<any_u32x4 *>(p));
+    } else {
+      *reinterpret_cast<Raw<E * sizeof(O)> *>(p) = r;
+    }
   } else {
 #pragma unroll
     for (int e = 0; e < E; e++)
@@ -80,7 +93,7 @@ __device__ inline void store_values(O *p, const float (&f)[E], float by, int64_t
 
 // A wave takes kTogether tokens and kSlice columns of their rows: every load is
 // on its way before the first store.
-template <class T, class I>
+template <class T, class I, bool NT>
 __global__ void __launch_bounds__(256) k_embed(const T *table, int64_t stride, int64_t vocab, const I *ids, int64_t tokens,
                                                int64_t h, int slices, float scale, T *out) {
   constexpr int E = Shape<T>::E, S = Shape<T>::S;
@@ -106,7 +119,7 @@ __global__ void __launch_bounds__(256) k_embed(const T *table, int64_t stride, i
       const int64_t c = c0 + u * 64 * E;
       float f[E];
       values<T, E>(f, r[k][u]);
-      if (c < h) store_values<T, E>(out + (t0 + k) * h + c, f, scale, h - c);
+      if (c < h) store_values<T, E, NT>(out + (t0 + k) * h + c, f, scale, h - c);
     }
   }
 }
@@ -163,11 +176,20 @@ __global__ void __launch_bounds__(kRankB) k_embed_rank(const I *ids, int tokens,
                                                        uint32_t *order) {
   __shared__ __align__(16) uint32_t s_key[kRankMost];
   const int tid = threadIdx.x;
-  for (int t = tid; t < (tokens + 3) / 4 * 4; t += kRankB) s_key[t] = t < tokens ? key_of(ids, t, vocab) : ~0u;
+  for (int t0 = tid; t0 < (tokens + 3) / 4 * 4; t0 += 8 * kRankB) {
+    uint32_t k[8];
+#pragma unroll
+    for (int u = 0; u < 8; u++) k[u] = t0 + u * kRankB < tokens ? key_of(ids, t0 + u * kRankB, vocab) : ~0u;
+#pragma unroll
+    for (int u = 0; u < 8; u++)
+      if (t0 + u * kRankB < kRankMost) s_key[t0 + u * kRankB] = k[u];
+  }
   __syncthreads();
   const int t = blockIdx.x * kRankTokens + tid / kRankEach, part = tid % kRankEach;
   const uint32_t key = t < tokens ? s_key[t] : 0;
   uint32_t before = 0;
+  // up to three entries behind the last token are read, larger than any key
+#pragma unroll 8
   for (int i = 4 * part; i < tokens; i += 4 * kRankEach) {
     const uint4 k = *reinterpret_cast<const uint4 *>(&s_key[i]);
     before += (k.x < key + (i < t)) + (k.y < key + (i + 1 < t)) + (k.z < key + (i + 2 < t)) + (k.w < key + (i + 3 < t));
@@ -258,17 +280,17 @@ __global__ void __launch_bounds__(kSortB) k_embed_move(const I *ids, const uint3
 }
 
 // ------------------------------------------------------------ sums by word
-// Sorted tokens [a, b), added in order to the lane's columns, kAtOnce rows on
-// their way at a time.
-template <class T, int E, int S>
-__device__ inline void add_tokens(float (&f)[S][E], const T *dx, int64_t stride, const uint32_t *__restrict__ order, int64_t a,
-                                  int64_t b, int64_t c0, int64_t h) {
-  constexpr int kAtOnce = 8;
+// Rows row_of(t) of dx for t in [a, b), added in order to the lane's columns,
+// kAtOnce of them on their way at a time.
+template <class T, int E, int S, class Row>
+__device__ inline void add_rows(float (&f)[S][E], const T *dx, int64_t stride, int64_t a, int64_t b, int64_t c0, int64_t h,
+                                Row row_of) {
+  constexpr int kAtOnce = 4;
   for (int64_t t = a; t < b; t += kAtOnce) {
     Raw<E * sizeof(T)> r[kAtOnce][S];
 #pragma unroll
     for (int k = 0; k < kAtOnce; k++) {
-      const T *row = dx + (int64_t)order[t + k < b ? t + k : b - 1] * stride;
+      const T *row = dx + row_of(t + k < b ? t + k : b - 1) * stride;
 #pragma unroll
       for (int u = 0; u < S; u++) {
         const int64_t c = c0 + u * 64 * E;
@@ -328,16 +350,16 @@ __global__ void __launch_bounds__(256) k_embed_parts(const uint32_t *__restrict_
   if (t0 + kChunk > tokens || keys[t0 + kChunk - 1] != key) return;
   const int64_t c0 = (task % slices) * kSlice + (threadIdx.x & 63) * E;
   float f[S][E] = {};
-  add_tokens<T, E, S>(f, dx, stride, order, t0, t0 + kChunk, c0, h);
+  add_rows<T, E, S>(f, dx, stride, t0, t0 + kChunk, c0, h, [&](int64_t t) { return (int64_t)order[t]; });
 #pragma unroll
   for (int u = 0; u < S; u++) {
     const int64_t c = c0 + u * 64 * E;
-    if (c < h) store_values<float, E>(part + chunk * h + c, f[u], 1.f, h - c);
+    if (c < h) store_values<float, E, false>(part + chunk * h + c, f[u], 1.f, h - c);
   }
 }
 
 // A wave takes kRowsAt rows of the table and kSlice of their columns.
-template <class T, class O>
+template <class T, class O, bool NT>
 __global__ void __launch_bounds__(256) k_embed_grad(const uint32_t *start, const uint32_t *__restrict__ order, int64_t vocab,
                                                     const T *dx, int64_t stride, int64_t h, int slices,
                                                     const float *__restrict__ part, float scale, O *grad) {
@@ -354,20 +376,13 @@ __global__ void __launch_bounds__(256) k_embed_grad(const uint32_t *start, const
     float f[S][E] = {};
     if (a < b) {
       const int64_t chunks = (b - a) / kChunk;
-      for (int64_t p = a / kChunk; p < a / kChunk + chunks; p++)
-#pragma unroll
-        for (int u = 0; u < S; u++) {
-          const int64_t c = c0 + u * 64 * E;
-#pragma unroll
-          for (int e = 0; e < E; e++)
-            if (c + e < h) f[u][e] += part[p * h + c + e];
-        }
-      add_tokens<T, E, S>(f, dx, stride, order, a + chunks * kChunk, b, c0, h);
+      add_rows<float, E, S>(f, part, h, a / kChunk, a / kChunk + chunks, c0, h, [](int64_t p) { return p; });
+      add_rows<T, E, S>(f, dx, stride, a + chunks * kChunk, b, c0, h, [&](int64_t t) { return (int64_t)order[t]; });
     }
 #pragma unroll
     for (int u = 0; u < S; u++) {
       const int64_t c = c0 + u * 64 * E;
-      if (c < h) store_values<O, E>(grad + (v0 + r) * h + c, f[u], scale, h - c);
+      if (c < h) store_values<O, E, NT>(grad + (v0 + r) * h + c, f[u], scale, h - c);
     }
   }
 }
@@ -429,12 +444,14 @@ int embed(const cel_embed_args *a, const void *table, void *out, hipStream_t s) 
   unsigned blocks;
   CEL_TRY(blocks_of((a->tokens + kTogether - 1) / kTogether * slices, "cel_embed", &blocks));
   KTimer kt(s, "k_embed");
-  if (a->id_bytes == 4)
-    k_embed<T, int32_t><<<blocks, 256, 0, s>>>((const T *)table, a->stride, a->vocab, (const int32_t *)a->ids, a->tokens,
-                                               a->hidden, slices, a->scale, (T *)out);
-  else
-    k_embed<T, int64_t><<<blocks, 256, 0, s>>>((const T *)table, a->stride, a->vocab, (const int64_t *)a->ids, a->tokens,
-                                               a->hidden, slices, a->scale, (T *)out);
+  auto go = [&](auto id, auto nt) {
+    typedef decltype(id) I;
+    k_embed<T, I, decltype(nt)::value><<<blocks, 256, 0, s>>>((const T *)table, a->stride, a->vocab, (const I *)a->ids,
+                                                              a->tokens, a->hidden, slices, a->scale, (T *)out);
+  };
+  const bool nt = a->tokens * a->hidden * (int64_t)sizeof(T) > kCached;
+  if (a->id_bytes == 4) nt ? go(int32_t{}, std::true_type{}) : go(int32_t{}, std::false_type{});
+  else nt ? go(int64_t{}, std::true_type{}) : go(int64_t{}, std::false_type{});
   CEL_HIP(hipGetLastError());
   return CEL_OK;
 }
@@ -487,12 +504,14 @@ int embed_grad(const cel_embed_args *a, const void *dx, void *work, int grad_typ
   }
   CEL_TRY(blocks_of((a->vocab + kRowsAt - 1) / kRowsAt * slices, "cel_embed_grad", &blocks));
   KTimer kt(s, "k_embed_grad");
-  if (grad_type == CEL_F32)
-    k_embed_grad<T, float><<<blocks, 256, 0, s>>>(start, order, a->vocab, (const T *)dx, a->stride, a->hidden, slices, part,
-                                                  a->scale, (float *)grad);
-  else
-    k_embed_grad<T, T><<<blocks, 256, 0, s>>>(start, order, a->vocab, (const T *)dx, a->stride, a->hidden, slices, part,
-                                              a->scale, (T *)grad);
+  auto go = [&](auto out, auto nt) {
+    typedef decltype(out) O;
+    k_embed_grad<T, O, decltype(nt)::value><<<blocks, 256, 0, s>>>(start, order, a->vocab, (const T *)dx, a->stride, a->hidden,
+                                                                   slices, part, a->scale, (O *)grad);
+  };
+  const bool f32 = grad_type == CEL_F32, nt = a->vocab * a->hidden * (f32 ? 4 : (int64_t)sizeof(T)) > kCached;
+  if (f32) nt ? go(float{}, std::true_type{}) : go(float{}, std::false_type{});
+  else nt ? go(T{}, std::true_type{}) : go(T{}, std::false_type{});
   CEL_HIP(hipGetLastError());
   return CEL_OK;
 }
