@@ -8,8 +8,8 @@ stream.  There is no CPU fallback: a missing library or a failed call raises.
 from __future__ import annotations
 
 import ctypes as C
-import math
 import os
+from contextlib import nullcontext
 from dataclasses import dataclass
 
 import numpy as np
@@ -508,50 +508,70 @@ def _refuse(what):
     raise CelError(E_ARG, what)
 
 
-def _on(t):
-    """The tensor's device as the current one for the launches of a call."""
-    return torch.cuda.device(t.device)
+def _on(index):
+    """The device as the current one for the launches of a call."""
+    return nullcontext() if index == torch.cuda.current_device() else torch.cuda.device(index)
 
 
-def _same_device(fn, **tensors):
-    dev = None
+def _raw_stream(index):
+    """The handle of the device's current stream."""
+    return torch._C._cuda_getCurrentRawStream(index)
+
+
+def _device_of(fn, **tensors):
+    """The index of the ROCm device that all of them are on."""
+    index = -1
     for name, t in tensors.items():
         if not isinstance(t, torch.Tensor) or not t.is_cuda:
             _refuse(f"{fn}: {name} is not a tensor on a ROCm device")
-        if dev is not None and t.device != dev:
-            _refuse(f"{fn}: {name} is on {t.device}, not on {dev}")
-        dev = t.device
-
-
-def _aligned(t):
-    return t.stride(2) == 1 and t.stride(0) % 8 == 0 and t.stride(1) % 8 == 0 and \
-        t.shape[2] <= t.stride(0) <= 1 << 23 and t.data_ptr() % 16 == 0
+        at = t.get_device()
+        if index >= 0 and at != index:
+            _refuse(f"{fn}: {name} is on device {at}, not on {index}")
+        index = at
+    return index
 
 
 def _view(t):
-    return _Rows(t.data_ptr(), t.stride(0), t.stride(1))
+    """t [tokens, heads, dim] as the kernels read and write it, or None where its values are not
+    contiguous or its address or strides are off 16 bytes."""
+    row, head, one = t.stride()
+    p = t.data_ptr()
+    if one != 1 or row & 7 or head & 7 or p & 15 or not t.shape[2] <= row <= 1 << 23:
+        return None
+    return _Rows(p, row, head)
+
+
+def _views(*tensors):
+    """Views to read, of copies where need be -> (views, tensors to keep alive)."""
+    views, keep = [], []
+    for t in tensors:
+        x = _view(t)
+        if x is None:
+            t = t.clone(memory_format=torch.contiguous_format)
+            x = _Rows(t.data_ptr(), t.shape[1] * t.shape[2], t.shape[2])
+        views.append(x)
+        keep.append(t)
+    return views, keep
 
 
 def _attn(fn, q, k, v, seq_ptr, scale):
-    """-> (descriptor, tensors to keep alive).  Views that the kernels cannot read as they are
-    (values not contiguous, addresses or strides off 16 bytes) are copied."""
-    _same_device(fn, q=q, k=k, v=v, seq_ptr=seq_ptr)
-    for name, t in (("q", q), ("k", k), ("v", v)):
-        if t.dim() != 3 or t.dtype != q.dtype or t.dtype not in (torch.bfloat16, torch.float16):
-            _refuse(f"{fn}: {name} is not [tokens, heads, dim] in bfloat16 or float16 as q is")
+    """-> (descriptor, tensors to keep alive)"""
+    if q.dim() != 3 or k.dim() != 3 or v.dim() != 3 or q.dtype not in (torch.bfloat16, torch.float16) or \
+            k.dtype != q.dtype or v.dtype != q.dtype:
+        _refuse(f"{fn}: q, k and v are not [tokens, heads, dim] in bfloat16 or in float16")
     T, H, d = q.shape
-    if k.shape != v.shape or k.shape[0] != T or k.shape[2] != d:
+    shape = k.shape
+    if v.shape != shape or shape[0] != T or shape[2] != d:
         _refuse(f"{fn}: shapes q {tuple(q.shape)}, k {tuple(k.shape)}, v {tuple(v.shape)}")
     if seq_ptr.dim() != 1 or seq_ptr.dtype != torch.int32 or seq_ptr.numel() < 1:
         _refuse(f"{fn}: seq_ptr is not int32 [sequences + 1]")
     if T >= 1 << 31:
         _refuse(f"{fn}: {T} tokens")
-    q, k, v = (t if _aligned(t) else t.clone(memory_format=torch.contiguous_format) for t in (q, k, v))
-    ptr = seq_ptr.contiguous()
-    a = _Attn(_TYPES[q.dtype], T, ptr.numel() - 1, H, k.shape[1], d,
-              1.0 / math.sqrt(max(d, 1)) if scale is None else float(scale), ptr.data_ptr(),
-              _view(q), _view(k), _view(v))
-    return a, (q, k, v, ptr)
+    (qv, kv, vv), keep = _views(q, k, v)
+    seq_ptr = seq_ptr.contiguous()
+    keep.append(seq_ptr)
+    return _Attn(_TYPES[q.dtype], T, seq_ptr.numel() - 1, H, shape[1], d,
+                 (d or 1) ** -0.5 if scale is None else scale, seq_ptr.data_ptr(), qv, kv, vv), keep
 
 
 def attention(q, k, v, seq_ptr, scale=None):
@@ -561,11 +581,13 @@ def attention(q, k, v, seq_ptr, scale=None):
     (views of a fused projection are read in place); heads a multiple of kv_heads, dim a multiple
     of 8 up to 128; scale: of the scores, 1 / sqrt(dim) by default.
     -> (out [T, heads, dim], lse float32 [heads, T]); tokens of no sequence have 0 and -inf."""
-    a, keep = _attn("attention", q, k, v, seq_ptr, scale)
-    with _on(q):
+    index = _device_of("attention", q=q, k=k, v=v, seq_ptr=seq_ptr)
+    with _on(index):
+        a, keep = _attn("attention", q, k, v, seq_ptr, scale)
         out = torch.empty(q.shape, dtype=q.dtype, device=q.device)
-        lse = torch.empty((q.shape[1], q.shape[0]), dtype=torch.float32, device=q.device)
-        _check(lib().cel_attention(C.byref(a), C.byref(_view(out)), _p(lse), _stream()))
+        lse = torch.empty((a.heads, a.tokens), dtype=torch.float32, device=q.device)
+        rows = _Rows(out.data_ptr(), a.heads * a.dim, a.dim)
+        _check(lib().cel_attention(C.byref(a), C.byref(rows), lse.data_ptr(), _raw_stream(index)))
     return out, lse
 
 
@@ -575,48 +597,50 @@ def attention_grad(dout, q, k, v, out, lse, seq_ptr, scale=None, grads=None):
     of one fused gradient; values contiguous, addresses and strides multiples of 16 bytes).  The same
     inputs give the same bits."""
     fn = "attention_grad"
-    a, keep = _attn(fn, q, k, v, seq_ptr, scale)
-    _same_device(fn, q=q, dout=dout, out=out, lse=lse)
-    T, H, d = q.shape
-    for name, t in (("dout", dout), ("out", out)):
-        if t.shape != q.shape or t.dtype != q.dtype:
-            _refuse(f"{fn}: {name} is {tuple(t.shape)} {t.dtype}, not as q")
-    if lse.shape != (H, T) or lse.dtype != torch.float32:
-        _refuse(f"{fn}: lse is not float32 [heads, tokens]")
-    with _on(q):
-        dout, out = (t if _aligned(t) else t.clone(memory_format=torch.contiguous_format) for t in (dout, out))
+    index = _device_of(fn, q=q, k=k, v=v, seq_ptr=seq_ptr, dout=dout, out=out, lse=lse)
+    with _on(index):
+        a, keep = _attn(fn, q, k, v, seq_ptr, scale)
+        for name, t in (("dout", dout), ("out", out)):
+            if t.shape != q.shape or t.dtype != q.dtype:
+                _refuse(f"{fn}: {name} is {tuple(t.shape)} {t.dtype}, not as q")
+        if lse.shape != (a.heads, a.tokens) or lse.dtype != torch.float32:
+            _refuse(f"{fn}: lse is not float32 [heads, tokens]")
+        (gv, ov), keep2 = _views(dout, out)
         lse = lse.contiguous()
         if grads is None:
             grads = tuple(torch.empty(t.shape, dtype=q.dtype, device=q.device) for t in (q, k, v))
+        elif len(grads) != 3:
+            _refuse(f"{fn}: grads are not three tensors")
         else:
-            _same_device(fn, q=q, **{f"grads[{i}]": t for i, t in enumerate(grads)})
-            if len(grads) != 3:
-                _refuse(f"{fn}: grads are not three tensors")
-            for name, t, x in zip(("dq", "dk", "dv"), grads, (q, k, v)):
-                if t.shape != x.shape or t.dtype != q.dtype or (t.numel() and not _aligned(t)):
-                    _refuse(f"{fn}: {name} cannot be written in place: {tuple(t.shape)} {t.dtype}, strides {t.stride()}")
+            _device_of(fn, q=q, dq=grads[0], dk=grads[1], dv=grads[2])
+        views = []
+        for name, t, x in zip(("dq", "dk", "dv"), grads, (q, k, v)):
+            view = _view(t) if t.shape == x.shape and t.dtype == q.dtype else None
+            if view is None and t.numel():
+                _refuse(f"{fn}: {name} cannot be written in place: {tuple(t.shape)} {t.dtype}, strides {t.stride()}")
+            views.append(C.byref(view or _Rows()))
         size = lib().cel_attention_grad_scratch(C.byref(a))
         if size < 0:
-            _check(int(size))
+            _check(size)
         scratch = torch.empty(size, dtype=torch.uint8, device=q.device)
-        views = [_view(t) for t in grads]
-        _check(lib().cel_attention_grad(C.byref(a), C.byref(_view(out)), _p(lse), C.byref(_view(dout)), _p(scratch),
-                                        *(C.byref(x) for x in views), _stream()))
+        _check(lib().cel_attention_grad(C.byref(a), C.byref(ov), lse.data_ptr(), C.byref(gv), scratch.data_ptr(), *views,
+                                        _raw_stream(index)))
     return tuple(grads)
 
 
 def _embed(fn, what, rows, ids, vocab, scale):
     """-> (descriptor, rows with contiguous values, ids): checks that embed and embed_grad share."""
-    _same_device(fn, **{what: rows, "ids": ids})
     if rows.dim() != 2 or rows.dtype not in _TYPES:
         _refuse(f"{fn}: {what} is not [rows, hidden] in bfloat16, float16 or float32")
     if ids.dim() != 1 or ids.dtype not in (torch.int32, torch.int64):
         _refuse(f"{fn}: ids are not int32 or int64 [tokens]")
     h = rows.shape[1]
-    if (h > 1 and rows.stride(1) != 1) or (rows.shape[0] > 1 and rows.stride(0) < h):
-        rows = rows.clone(memory_format=torch.contiguous_format)
+    stride, one = rows.stride()
+    if rows.shape[0] <= 1:
+        stride = h
+    if (h > 1 and one != 1) or stride < h:
+        rows, stride = rows.clone(memory_format=torch.contiguous_format), h
     ids = ids.contiguous()
-    stride = rows.stride(0) if rows.shape[0] > 1 else h
     return _Embed(_TYPES[rows.dtype], ids.element_size(), ids.numel(), vocab, h, stride, ids.data_ptr(),
                   float(scale)), rows, ids
 
@@ -625,10 +649,11 @@ def embed(table, ids, scale=1.0):
     """scale * table[ids]: rows of table [vocab, hidden] (bfloat16, float16 or float32, rows any
     stride apart) by token id (int32 or int64 [tokens]); an id outside [0, vocab) is padding, a row
     of zeros. -> [tokens, hidden] in the table's type."""
-    a, table, ids = _embed("embed", "table", table, ids, table.shape[0] if isinstance(table, torch.Tensor) else 0, scale)
-    with _on(table):
-        out = torch.empty((ids.numel(), table.shape[1]), dtype=table.dtype, device=table.device)
-        _check(lib().cel_embed(C.byref(a), _p(table), _p(out), _stream()))
+    index = _device_of("embed", table=table, ids=ids)
+    with _on(index):
+        a, table, ids = _embed("embed", "table", table, ids, table.shape[0], scale)
+        out = torch.empty((a.tokens, a.hidden), dtype=table.dtype, device=table.device)
+        _check(lib().cel_embed(C.byref(a), table.data_ptr(), out.data_ptr(), _raw_stream(index)))
     return out
 
 
@@ -638,17 +663,19 @@ def embed_grad(dx, ids, vocab, scale=1.0, dtype=None):
     The tokens are sorted by id and added in 32 bits in a fixed order: the same inputs give the
     same bits."""
     fn = "embed_grad"
-    a, dx, ids = _embed(fn, "dx", dx, ids, int(vocab), scale)
-    if ids.numel() != dx.shape[0]:
-        _refuse(f"{fn}: {ids.numel()} ids of {dx.shape[0]} rows")
-    dtype = dx.dtype if dtype is None else dtype
-    if dtype not in (dx.dtype, torch.float32):
-        _refuse(f"{fn}: a gradient in {dtype} of rows in {dx.dtype}")
-    with _on(dx):
-        size = lib().cel_embed_grad_scratch(ids.numel(), int(vocab), dx.shape[1])
+    index = _device_of(fn, dx=dx, ids=ids)
+    with _on(index):
+        a, dx, ids = _embed(fn, "dx", dx, ids, int(vocab), scale)
+        if a.tokens != dx.shape[0]:
+            _refuse(f"{fn}: {a.tokens} ids of {dx.shape[0]} rows")
+        dtype = dx.dtype if dtype is None else dtype
+        if dtype not in (dx.dtype, torch.float32):
+            _refuse(f"{fn}: a gradient in {dtype} of rows in {dx.dtype}")
+        size = lib().cel_embed_grad_scratch(a.tokens, int(vocab), a.hidden)
         if size < 0:
-            _check(int(size))
+            _check(size)
         work = torch.empty(size, dtype=torch.uint8, device=dx.device)
-        grad = torch.empty((int(vocab), dx.shape[1]), dtype=dtype, device=dx.device)
-        _check(lib().cel_embed_grad(C.byref(a), _p(dx), _p(work), _TYPES[dtype], _p(grad), _stream()))
+        grad = torch.empty((int(vocab), a.hidden), dtype=dtype, device=dx.device)
+        _check(lib().cel_embed_grad(C.byref(a), dx.data_ptr(), work.data_ptr(), _TYPES[dtype], grad.data_ptr(),
+                                    _raw_stream(index)))
     return grad
