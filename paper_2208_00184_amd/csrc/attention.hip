@@ -964,12 +964,12 @@ int check_attn(const cel_attn *a, const char *fn) {
   return CEL_OK;
 }
 // Into how many workgroups a tile of keys deals out the query heads that share
-// them: as many as bring eight workgroups to each of the 256 compute units (the
+// them: as many as bring six workgroups to each of the 256 compute units (the
 // tiles at a long sequence's beginning take many times the average), each with the
 // same number of heads but the last.
 int parts_of(const cel_attn *a) {
   const int64_t group = a->heads / a->kv_heads, tiles = ((int64_t)a->tokens + kKeyBlock - 1) / kKeyBlock;
-  const int64_t per = std::max<int64_t>(1, group * tiles * a->kv_heads / 2048);
+  const int64_t per = std::max<int64_t>(1, group * tiles * a->kv_heads / 1536);
   return per >= group ? 1 : (int)((group + per - 1) / per);
 }
 Rows rows_of(const cel_rows *x) { return Rows{static_cast<char *>(x->p), x->row, x->head}; }
