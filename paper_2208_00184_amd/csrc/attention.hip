@@ -436,15 +436,17 @@ __device__ __forceinline__ void mask(acc16 &x, int t, int lo, int hi, float by, 
 
 // One tile of 128 tokens of one query head: each wave 32 of them, over the
 // keys from the first row's sequence on.
-template <class T, int DP, int DC, bool CAREFUL>
+template <class T, int DP, int DC, int G, bool CAREFUL>
 __device__ __forceinline__ bool attention_tile(const AttnArgs &A, char *s_k0, char *s_k1, char *s_v0, char *s_v1,
                                                int (*s_reach)[kWaves]) {
+  constexpr int kTile = kStep * DP * 2;
   constexpr int NB = CAREFUL ? 1 : DC / 32;  // sums a pass holds, see CEL_TILE_KERNEL
-  const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+  const int tid = threadIdx.x % (kWaves * 64), lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+  const int group = G > 1 ? __builtin_amdgcn_readfirstlane(threadIdx.x / (kWaves * 64)) : 0;
   const int item = item_of(blockIdx.x, gridDim.x);
   const int head = item / A.tiles, tile = A.tiles - 1 - item % A.tiles, kvh = head / (A.H / A.K);
   const int i = tile * kBlock + wave * kRows + (lane & 31);  // this lane's row
-  const Reach R = reach_of(A, i, true, s_reach, wave);
+  const Reach R = reach_of(A, i, true, s_reach + 2 * group, wave);
   u32x4 q[DC / 16];
   load_rows(q, A.q, head, i, A.T, A.d, lane);
   const float c = A.scale * kLog2e, far = 8.f / c;
@@ -457,14 +459,14 @@ __device__ __forceinline__ bool attention_tile(const AttnArgs &A, char *s_k0, ch
     acc16 o[NB];
     float m, mc, l;
     auto load = [&](int t, auto buf) {
-      const int a = R.from + t * kStep;
-      ks.load(buf.at ? s_k1 : s_k0, k_head, a, R.to + 1, wave);
-      vs.load(buf.at ? s_v1 : s_v0, v_head, a, R.to + 1, wave);
+      const int a = R.from + (t * G + group) * kStep;
+      ks.load((buf.at ? s_k1 : s_k0) + group * kTile, k_head, a, R.to + 1, wave);
+      vs.load((buf.at ? s_v1 : s_v0) + group * kTile, v_head, a, R.to + 1, wave);
     };
     auto step = [&](int t0, auto buf) {
-      const int a = R.from + t0 * kStep;
+      const int a = R.from + (t0 * G + group) * kStep;
       if (R.skips(a)) return;
-      const char *s_k = buf.at ? s_k1 : s_k0, *s_v = buf.at ? s_v1 : s_v0;
+      const char *s_k = (buf.at ? s_k1 : s_k0) + group * kTile, *s_v = (buf.at ? s_v1 : s_v0) + group * kTile;
       const bool masked = R.masks(a);
       const int lo = R.lo - a, hi = R.hi - a;  // of the 64 keys, those that this row sees
       acc16 s[2];
@@ -515,11 +517,34 @@ __device__ __forceinline__ bool attention_tile(const AttnArgs &A, char *s_k0, ch
       m = -INFINITY, mc = 0.f, l = 0.f;
     };
     clear();
-    through_tiles<CAREFUL>(R.steps(), load, step);
+    through_tiles<CAREFUL>((R.steps() + G - 1) / G, load, step);
     // An infinity or NaN may come from a value that the row does not see.
     if (!CAREFUL && __syncthreads_or(R.real() && not_finite(o, 1.f))) return false;
     l = half_sum(l);
-    if (i < A.T) {
+    if constexpr (G > 1) {  // the first group's sums and the second's, over the larger maximum
+      float *theirs = reinterpret_cast<float *>((wave & 2 ? s_k1 : s_k0) + (wave & 1) * kTile) + lane;
+      float *stats = reinterpret_cast<float *>(s_v0) + wave * 128 + lane;
+      if (CAREFUL) __syncthreads();
+      if (group) {
+#pragma unroll
+        for (int n = 0; n < NB; n++)
+#pragma unroll
+          for (int r = 0; r < 16; r++) theirs[(16 * n + r) * 64] = o[n][r];
+        stats[0] = m, stats[64] = l;
+      }
+      __syncthreads();
+      if (!group) {
+        const float m1 = stats[0], to = fmaxf(m, m1);
+        const float a0 = to == -INFINITY ? 1.f : exp2_((m - to) * c), a1 = to == -INFINITY ? 1.f : exp2_((m1 - to) * c);
+        l = l * a0 + stats[64] * a1;
+        mc = to == -INFINITY ? 0.f : to * c;
+#pragma unroll
+        for (int n = 0; n < NB; n++)
+#pragma unroll
+          for (int r = 0; r < 16; r++) o[n][r] = o[n][r] * a0 + theirs[(16 * n + r) * 64] * a1;
+      }
+    }
+    if (i < A.T && group == 0) {
       if (!R.real()) {
 #pragma unroll
         for (int n = 0; n < NB; n++) o[n] = acc16{};
@@ -539,14 +564,19 @@ __device__ __forceinline__ bool attention_tile(const AttnArgs &A, char *s_k0, ch
 // the result has any, all of it again with: nothing of the first run is kept in
 // registers for the second, which takes 32 dimensions at a time, so that it
 // needs fewer than the first.
-#define CEL_TILE_KERNEL(kernel, tile, a0, a1, b0, b1)                            \
-  template <class T, int DP, int DC>                                             \
-  __global__ void __launch_bounds__(kWaves * 64, 2) kernel(AttnArgs A) {         \
-    constexpr int kTile = kStep * DP * 2;                                        \
-    __shared__ __align__(16) char a0[kTile], a1[kTile], b0[kTile], b1[kTile];    \
-    __shared__ int s_reach[2][kWaves];                                           \
-    if (!tile<T, DP, DC, false>(A, a0, a1, b0, b1, s_reach))                     \
-      (void)tile<T, DP, DC, true>(A, a0, a1, b0, b1, s_reach);                   \
+// G = 2: two groups of waves share the rows and take their keys' tiles in turn,
+// each with buffers of its own, and join their sums at the end.  A tile's chain of
+// steps, each of which waits for the one before, is then half as long, with the
+// same two waves on every SIMD; it is taken where each workgroup has a compute unit
+// to itself, so that the longest chain is the time (see split_keys).
+#define CEL_TILE_KERNEL(kernel, tile, a0, a1, b0, b1)                                                      \
+  template <class T, int DP, int DC, int G>                                                                \
+  __global__ void __launch_bounds__(G *kWaves * 64, 2) kernel(AttnArgs A) {                                \
+    constexpr int kTile = G * kStep * DP * 2;                                                              \
+    __shared__ __align__(16) char a0[kTile], a1[kTile], b0[kTile], b1[kTile];                              \
+    __shared__ int s_reach[2 * G][kWaves];                                                                 \
+    if (!tile<T, DP, DC, G, false>(A, a0, a1, b0, b1, s_reach))                                            \
+      (void)tile<T, DP, DC, G, true>(A, a0, a1, b0, b1, s_reach);                                          \
   }
 CEL_TILE_KERNEL(k_attention, attention_tile, s_k0, s_k1, s_v0, s_v1)
 
@@ -555,15 +585,17 @@ CEL_TILE_KERNEL(k_attention, attention_tile, s_k0, s_k1, s_v0, s_v1)
 // wave's keys all lie in one tile: there, where o_i is large (few values
 // averaged) and its rounding would weigh as much as that of ds, it is the sum of
 // p_ij <do_i, v_j> in 32 bits, at the price of that tile's products twice.
-template <class T, int DP, int DC, bool CAREFUL>
+template <class T, int DP, int DC, int G, bool CAREFUL>
 __device__ __forceinline__ bool dq_tile(const AttnArgs &A, char *s_k0, char *s_k1, char *s_v0, char *s_v1,
                                         int (*s_reach)[kWaves]) {
+  constexpr int kTile = kStep * DP * 2;
   constexpr int NB = CAREFUL ? 1 : DC / 32;  // sums a pass holds, see CEL_TILE_KERNEL
-  const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+  const int tid = threadIdx.x % (kWaves * 64), lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+  const int group = G > 1 ? __builtin_amdgcn_readfirstlane(threadIdx.x / (kWaves * 64)) : 0;
   const int item = item_of(blockIdx.x, gridDim.x);
   const int head = item / A.tiles, tile = A.tiles - 1 - item % A.tiles, kvh = head / (A.H / A.K);
   const int i = tile * kBlock + wave * kRows + (lane & 31);
-  const Reach R = reach_of(A, i, true, s_reach, wave);
+  const Reach R = reach_of(A, i, true, s_reach + 2 * group, wave);
   u32x4 q[DC / 16], g[DC / 16];
   load_rows(q, A.q, head, i, A.T, A.d, lane);
   load_rows(g, A.dout, head, i, A.T, A.d, lane);
@@ -590,14 +622,14 @@ __device__ __forceinline__ bool dq_tile(const AttnArgs &A, char *s_k0, char *s_k
     const int cols = L.cols ^ (n0 << 6);
     acc16 dq[NB];
     auto load = [&](int t, auto buf) {
-      const int a = R.from + t * kStep;
-      ks.load(buf.at ? s_k1 : s_k0, k_head, a, R.to + 1, wave);
-      vs.load(buf.at ? s_v1 : s_v0, v_head, a, R.to + 1, wave);
+      const int a = R.from + (t * G + group) * kStep;
+      ks.load((buf.at ? s_k1 : s_k0) + group * kTile, k_head, a, R.to + 1, wave);
+      vs.load((buf.at ? s_v1 : s_v0) + group * kTile, v_head, a, R.to + 1, wave);
     };
     auto step = [&](int t0, auto buf) {
-      const int a = R.from + t0 * kStep;
+      const int a = R.from + (t0 * G + group) * kStep;
       if (R.skips(a)) return;
-      const char *s_k = buf.at ? s_k1 : s_k0, *s_v = buf.at ? s_v1 : s_v0;
+      const char *s_k = (buf.at ? s_k1 : s_k0) + group * kTile, *s_v = (buf.at ? s_v1 : s_v0) + group * kTile;
       const bool masked = R.masks(a);
       const int lo = R.lo - a, hi = R.hi - a;
       if (R.any_lo >= a && R.any_hi < a + kStep) {
@@ -630,9 +662,30 @@ __device__ __forceinline__ bool dq_tile(const AttnArgs &A, char *s_k0, char *s_k
       for (int n = 0; n < NB; n++) dq[n] = acc16{};
     };
     clear();
-    through_tiles<CAREFUL>(R.steps(), load, step);
+    through_tiles<CAREFUL>((R.steps() + G - 1) / G, load, step);
     if (!CAREFUL && __syncthreads_or(R.real() && not_finite(dq, A.scale))) return false;
-    if (i < A.T) {
+    if constexpr (G > 1) {
+      float *theirs = reinterpret_cast<float *>((wave & 2 ? s_k1 : s_k0) + (wave & 1) * kTile) + lane;
+      float *their_D = reinterpret_cast<float *>(s_v0) + wave * 64 + lane;
+      if (CAREFUL) __syncthreads();
+      if (group) {
+#pragma unroll
+        for (int n = 0; n < NB; n++)
+#pragma unroll
+          for (int r = 0; r < 16; r++) theirs[(16 * n + r) * 64] = dq[n][r];
+        *their_D = D;
+      }
+      __syncthreads();
+      if (!group) {
+#pragma unroll
+        for (int n = 0; n < NB; n++)
+#pragma unroll
+          for (int r = 0; r < 16; r++) dq[n][r] += theirs[(16 * n + r) * 64];
+        const int t = (R.any_lo - R.from) / kStep;  // the tile with all of the wave's keys, if there is one
+        if (R.any_lo <= R.any_hi && (R.any_hi - R.from) / kStep == t && t & 1) D = *their_D;
+      }
+    }
+    if (i < A.T && group == 0) {
       if (!R.real()) clear();
       store_rows<T>(A.dq, head, i, dq, n0, A.scale, A.d, lane);
       if (lane < 32) {
@@ -983,26 +1036,64 @@ AttnArgs args_of(const cel_attn *a) {
   return A;
 }
 
-// kernel<T, DP, DC> for the call's type and dimension: rows are staged DP wide
-// (a power of two, for the chunks' order), products run over DC dimensions.
-#define CEL_LAUNCH(kernel, T, DP, DC) kernel<T, DP, DC><<<grid, kWaves * 64, 0, s>>>(A)
-#define CEL_SMALL(kernel, T)                        \
-  do {                                                     \
-    if (A.d <= 32) CEL_LAUNCH(kernel, T, 64, 32);   \
-    else CEL_LAUNCH(kernel, T, 64, 64);             \
-  } while (0)
-#define CEL_LARGE(kernel, T)                        \
-  do {                                                     \
-    if (A.d <= 96) CEL_LAUNCH(kernel, T, 128, 96);  \
-    else CEL_LAUNCH(kernel, T, 128, 128);           \
-  } while (0)
-#define CEL_BY_TYPE(which, kernel)                  \
-  do {                                                     \
-    KTimer kt(s, #kernel);                                 \
-    if (a->type == CEL_BF16) which(kernel, __bf16); \
-    else which(kernel, _Float16);                   \
-    CEL_HIP(hipGetLastError());                            \
-  } while (0)
+// Whether a kernel's workgroups share their keys between two groups of waves: where
+// there are no more of them than the GPU's 256 compute units, each then with as many
+// waves as two workgroups would give it, and tokens enough for the join, about 1 us,
+// to be won back.  One head of 64 over a sequence of 2,048 tokens: forward
+// 33.0 -> 26.7 us, dq 41.9 -> 35.2; of 128: forward 45.3 -> 36.1; 8 heads of 64 over 4,096:
+// 57.5 -> 45.2 and 73.1 -> 59.4; but at 512 workgroups (4 sequences of 1,024, 16 heads of
+// 64) 23.9 -> 32.3 and 31.6 -> 43.6, and at 64 tokens 7.4 -> 8.6.
+bool split_keys(const AttnArgs &A) { return (int64_t)A.tiles * A.H <= 256 && A.T >= 512; }
+
+// kernel<T, DP, DC, ...> for the call's type and dimension: rows are staged DP
+// wide (a power of two, for the chunks' order), products run over DC dimensions.
+template <class F>
+void by_dim(int d, F f) {
+  typedef std::integral_constant<int, 32> c32;
+  typedef std::integral_constant<int, 64> c64;
+  typedef std::integral_constant<int, 96> c96;
+  typedef std::integral_constant<int, 128> c128;
+  if (d <= 32) f(c64{}, c32{});
+  else if (d <= 64) f(c64{}, c64{});
+  else if (d <= 96) f(c128{}, c96{});
+  else f(c128{}, c128{});
+}
+template <class T>
+void launch_attention(const AttnArgs &A, hipStream_t s) {
+  KTimer kt(s, "k_attention");
+  by_dim(A.d, [&](auto dp, auto dc) {
+    constexpr int DP = decltype(dp)::value, DC = decltype(dc)::value;
+    const int grid = A.tiles * A.H;
+    if (split_keys(A)) k_attention<T, DP, DC, 2><<<grid, 2 * kWaves * 64, 0, s>>>(A);
+    else k_attention<T, DP, DC, 1><<<grid, kWaves * 64, 0, s>>>(A);
+  });
+}
+template <class T>
+void launch_dq(const AttnArgs &A, hipStream_t s) {
+  KTimer kt(s, "k_attention_dq");
+  by_dim(A.d, [&](auto dp, auto dc) {
+    constexpr int DP = decltype(dp)::value, DC = decltype(dc)::value;
+    const int grid = A.tiles * A.H;
+    if constexpr (DC <= 64) {  // beyond, two groups' dq does not fit in the registers (60 -> 126 us at 2,048 tokens)
+      if (split_keys(A)) return k_attention_dq<T, DP, DC, 2><<<grid, 2 * kWaves * 64, 0, s>>>(A);
+    }
+    k_attention_dq<T, DP, DC, 1><<<grid, kWaves * 64, 0, s>>>(A);
+  });
+}
+template <class T>
+void launch_dkv(const AttnArgs &A, hipStream_t s) {
+  {
+    KTimer kt(s, "k_attention_dkv");
+    by_dim(A.d, [&](auto dp, auto dc) {
+      k_attention_dkv<T, decltype(dp)::value, decltype(dc)::value>
+          <<<(A.T + kKeyBlock - 1) / kKeyBlock * A.K * A.parts, kWaves * 64, 0, s>>>(A);
+    });
+  }
+  if (A.parts > 1) {
+    KTimer kt(s, "k_attention_join");
+    k_attention_join<T><<<(unsigned)(((int64_t)A.T * A.K * A.d / 4 + 255) / 256), 256, 0, s>>>(A);
+  }
+}
 
 }  // namespace
 }  // namespace cel
@@ -1029,9 +1120,9 @@ extern "C" int cel_attention(const cel_attn *a, const cel_rows *out, float *lse,
   AttnArgs A = args_of(a);
   A.out = rows_of(out);
   A.lse = lse;
-  const int grid = A.tiles * A.H;
-  if (a->dim <= 64) CEL_BY_TYPE(CEL_SMALL, k_attention);
-  else CEL_BY_TYPE(CEL_LARGE, k_attention);
+  if (a->type == CEL_BF16) launch_attention<__bf16>(A, s);
+  else launch_attention<_Float16>(A, s);
+  CEL_HIP(hipGetLastError());
   return CEL_OK;
 }
 
@@ -1053,20 +1144,17 @@ extern "C" int cel_attention_grad(const cel_attn *a, const cel_rows *out, const 
   A.out = rows_of(out), A.dout = rows_of(dout), A.dq = rows_of(dq), A.dk = rows_of(dk), A.dv = rows_of(dv);
   A.lse = const_cast<float *>(lse);
   A.rows = scratch;
-  int grid = A.tiles * A.H;
-  if (a->dim <= 64) CEL_BY_TYPE(CEL_SMALL, k_attention_dq);
-  else CEL_BY_TYPE(CEL_LARGE, k_attention_dq);
   A.parts = parts_of(a);
   A.part = scratch + 2 * (int64_t)a->heads * a->tokens;
-  grid = (A.T + kKeyBlock - 1) / kKeyBlock * A.K * A.parts;
-  if (a->dim <= 64) CEL_BY_TYPE(CEL_SMALL, k_attention_dkv);
-  else CEL_BY_TYPE(CEL_LARGE, k_attention_dkv);
-  if (A.parts > 1) {
-    KTimer kt(s, "k_attention_join");
-    const int64_t blocks = ((int64_t)A.T * A.K * A.d / 4 + 255) / 256;
-    if (a->type == CEL_BF16) k_attention_join<__bf16><<<(unsigned)blocks, 256, 0, s>>>(A);
-    else k_attention_join<_Float16><<<(unsigned)blocks, 256, 0, s>>>(A);
+  if (a->type == CEL_BF16) {
+    launch_dq<__bf16>(A, s);
     CEL_HIP(hipGetLastError());
+    launch_dkv<__bf16>(A, s);
+  } else {
+    launch_dq<_Float16>(A, s);
+    CEL_HIP(hipGetLastError());
+    launch_dkv<_Float16>(A, s);
   }
+  CEL_HIP(hipGetLastError());
   return CEL_OK;
 }

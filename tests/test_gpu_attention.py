@@ -308,3 +308,54 @@ def test_refusals():
     refused(cel.attention_grad, g, q, k, v, out, lse, ptr, grads=(q[:, :, ::2], k, v))
     odd = torch.empty(q.numel() + 1, dtype=q.dtype, device=DEV)[1:].view(q.shape)
     refused(cel.attention_grad, g, q, k, v, out, lse, ptr, grads=(odd, torch.empty_like(k), torch.empty_like(v)))
+
+
+@pytest.mark.parametrize("lengths", [[512], [513], [640], [1100], [1000, 24], [0, 511, 1], [1] * 600, [30] * 20,
+                                     [70, 40, 500, 64, 130]])
+@pytest.mark.parametrize("d,dtype", [(32, torch.float16), (64, torch.bfloat16), (96, torch.bfloat16), (128, torch.float16)])
+def test_few_tiles_of_many_keys(lengths, d, dtype):
+    """Few rows' tiles over 512 tokens and more: a tile's keys are dealt out and joined."""
+    check(*batch(sum(lengths), 2, 1, d, dtype, d + len(lengths)), lengths)
+
+
+def test_few_tiles_with_tokens_of_no_sequence():
+    for T, first, lengths in [(700, 0, []), (700, 650, [3]), (900, 130, [260, 0, 300])]:
+        check(*batch(T, 2, 2, 64, torch.bfloat16, T), lengths, first)
+
+
+@pytest.mark.parametrize("bad", [float("nan"), float("inf"), -float("inf")])
+@pytest.mark.parametrize("at", [150, 250, 380])
+def test_few_tiles_and_what_a_row_does_not_see(bad, at):
+    """Infinities and NaN in one token's k and v, in either half of the keys' tiles."""
+    lengths = [100, 400, 200]
+    q, k, v, g = batch(700, 2, 1, 64, torch.bfloat16, 6)
+    ptr = ptr_of(lengths)
+    out0, lse0 = cel.attention(q, k, v, ptr)
+    g0 = cel.attention_grad(g, q, k, v, out0, lse0, ptr)
+    k2, v2 = k.clone(), v.clone()
+    k2[at], v2[at] = bad, bad
+    out, lse = cel.attention(q, k2, v2, ptr)
+    dq, dk, dv = cel.attention_grad(g, q, k2, v2, out, lse, ptr)
+    for rows in (slice(0, at), slice(500, 700)):
+        assert torch.equal(out[rows], out0[rows]) and torch.equal(lse[:, rows], lse0[:, rows])
+        assert torch.equal(dq[rows], g0[0][rows])
+    assert torch.equal(dk[500:], g0[1][500:]) and torch.equal(dv[500:], g0[2][500:])
+    assert not torch.isfinite(out[at:500].float()).all()
+
+
+def test_views_of_a_buffer_beyond_32_bits():
+    """Rows 2^23 values apart: the last of them lie past 2^32 bytes."""
+    T, d, lengths = 600, 64, [90, 510]
+    q, k, v, g = batch(T, 2, 1, d, torch.bfloat16, 12)
+    plain = check(q, k, v, g, lengths)
+    wide = torch.empty(T * 2 ** 23, dtype=q.dtype, device=DEV)
+    views = [wide.as_strided((T, x.shape[1], d), (2 ** 23, d, 1), 64 * 1000 * n) for n, x in enumerate((q, k, v, g))]
+    for view, x in zip(views, (q, k, v, g)):
+        view.copy_(x)
+    into = [wide.as_strided((T, x.shape[1], d), (2 ** 23, d, 1), 64 * 1000 * n + 64 * 500) for n, x in enumerate((q, k, v))]
+    ptr = ptr_of(lengths)
+    out, lse = cel.attention(*views[:3], ptr)
+    got = cel.attention_grad(views[3], *views[:3], out, lse, ptr, grads=into)
+    assert torch.equal(out, plain[0]) and torch.equal(lse, plain[1])
+    for a, b in zip(got, plain[2]):
+        assert torch.equal(a, b)

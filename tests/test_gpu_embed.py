@@ -223,3 +223,17 @@ def test_refusals():
     refused(cel.embed_grad, dx, ids, 10, dtype=torch.bfloat16)
     refused(cel.embed_grad, dx.double(), ids, 10)
     refused(cel.embed_grad, dx, ids, 10, scale=float("inf"))
+
+
+def test_views_of_a_buffer_beyond_32_bits():
+    """Rows 2^22 and 2^23 values apart: the last of them lie past 2^32 bytes."""
+    V, T, h = 600, 700, 72
+    table, dx, ids = randn(V, h, seed=40).bfloat16(), randn(T, h, seed=41).bfloat16(), zipf(T, V, 42)
+    wide = torch.empty(T * 2 ** 22 + V * 2 ** 22, dtype=torch.bfloat16, device=DEV)
+    far = wide.as_strided((V, h), (2 ** 23, 1))
+    far.copy_(table)
+    ids[-3:] = torch.tensor([V - 1, V, V - 2])
+    assert torch.equal(cel.embed(far, ids.to(DEV)).cpu(), ref_embed(table, ids, 1.0))
+    far = wide.as_strided((T, h), (2 ** 22, 1))
+    far.copy_(dx)
+    check_grad(far, ids.to(DEV), V, 1.0, None)
