@@ -26,7 +26,7 @@ constexpr int kChunk = 32;       // sorted tokens of one partial sum
 constexpr int kDigit = 9;        // bits of an id sorted at once: two passes up to 262,143 words
 constexpr int kBins = 1 << kDigit;
 constexpr int kSortB = 1024, kSortW = kSortB / 64;
-constexpr int kRankMost = 16384; // tokens that are ranked against each other
+constexpr int kRankMost = 8192;  // tokens that are ranked against each other, at most
 constexpr int kRankB = 256, kRankEach = 16, kRankTokens = kRankB / kRankEach;  // threads, threads a token, tokens
 constexpr int kSlice = 512;      // columns a wave handles
 constexpr int kTogether = 4;     // rows of the lookup that a wave has on their way at once
@@ -172,8 +172,9 @@ __device__ inline void start_counts(uint32_t (*count)[kSortW + 1], const uint32_
 
 // Few tokens: every token's place is the number of tokens that come before it,
 // counted against all of them, kRankEach threads a token.  Tokens squared
-// comparisons, but one launch and no dependent passes: 4,096 tokens in 11 us, where
-// the sort below takes four launches, about 30 us.  Bound by the reads of LDS.
+// comparisons, but one launch and no dependent passes: 4,096 tokens in 11 us and 8,192
+// in 21, where the sort below takes 25 and 26 us; 8,193 in 33 and 16,384 in 69, where it
+// takes 28 and 29 us.  Bound by the reads of LDS.
 template <class I>
 __global__ void __launch_bounds__(kRankB) k_embed_rank(const I *ids, int tokens, int64_t vocab, uint32_t *keys,
                                                        uint32_t *order) {

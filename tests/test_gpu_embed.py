@@ -237,3 +237,8 @@ def test_views_of_a_buffer_beyond_32_bits():
     far = wide.as_strided((T, h), (2 ** 22, 1))
     far.copy_(dx)
     check_grad(far, ids.to(DEV), V, 1.0, None)
+
+
+@pytest.mark.parametrize("T", [8191, 8192, 8193])
+def test_gradient_where_the_sort_changes(T):
+    check_grad(randn(T, 24, seed=T).bfloat16().to(DEV), zipf(T, 9000, T).to(DEV), 9000, 1.0, None)
