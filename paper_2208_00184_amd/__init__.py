@@ -1,4 +1,5 @@
-"""MI355X (gfx950) implementation of the Celeritas placement hot path.
+"""MI355X (gfx950) implementation of the Celeritas placement hot path, and of
+attention and the embedding of a training step whose costs it places.
 
 The computation lives in libcel.so (HIP kernels behind the C ABI of
 include/cel.h); this package is its thin Python binding.
