@@ -266,17 +266,27 @@ __device__ inline int wave_max(int x) {
   return x;
 }
 
-// Work items in an order that gives each of the 8 dies, which take
-// workgroups in turn, a stretch of neighbouring items: tiles of one head
-// share its keys and values in that die's L2.  Where a die's 32 compute units
-// take all of its items at once, two each, the second half comes backwards: the
-// longest of a head's tiles then share their unit with the shortest (4,096
-// tokens in 4 sequences, 16 heads of 64: forward 29 -> 26 us, dq 39 -> 32).
-__device__ inline int item_of(int block, int blocks) {
-  const int x = block & 7, per = blocks >> 3, more = blocks & 7, all = per + (x < more);
+// Workgroups in an order that deals with the tiles of all heads (units) in turn,
+// tile 0 first, so that a head's short tiles do not leave another's long ones to the
+// end.  The 8 dies take workgroups in turn: a power of two of them share
+// neighbouring heads, whose keys and values are then in those dies' L2 caches.
+// Against one head after the other, 4 sequences of 1,024 tokens, 64 heads of 128: forward
+// 131 -> 112 us, dk and dv 236 -> 217, dq 214 -> 203; 61 ragged ones, 32 heads of 128 over 8: 299
+// -> 252; one of 16,384, 4 heads of 128: dk and dv 740 -> 592.  Slower where more
+// heads at once mean more keys than L2 holds (8,192 tokens, 64 heads of 128: dk and dv 2.31 -> 2.39
+// ms, but forward 1.10 -> 1.07) and where no tile is long (64 sequences of 256: 32.5 -> 34.3).
+// Where a die's 32 compute units take all of its workgroups at once, two each, the second
+// half comes backwards: the longest of a head's tiles then share their unit with
+// the shortest (4,096 tokens in 4 sequences, 16 heads of 64: forward 29 -> 26 us, dq 39 -> 32).
+struct Item {
+  int unit, tile;
+};
+__device__ inline Item item_of(int block, int blocks, int units) {
+  const int x = block & 7, all = (blocks >> 3) + (x < (blocks & 7));
   int s = block >> 3;
   if (all <= 64 && s >= 32) s = 32 + all - 1 - s;
-  return x * per + min(x, more) + s;
+  const int at = 8 * s + x, u = at % units, share = min(units & -units, 8);
+  return {u % share * (units / share) + u / share, at / units};
 }
 
 // Right operand from global memory: column lane % 32 is a token, its k the
@@ -453,8 +463,8 @@ __device__ __forceinline__ bool attention_tile(const AttnArgs &A, char *s_k0, ch
   constexpr int NB = CAREFUL ? 1 : DC / 32;  // sums a pass holds, see CEL_TILE_KERNEL
   const int tid = threadIdx.x % (kWaves * 64), lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int group = G > 1 ? __builtin_amdgcn_readfirstlane(threadIdx.x / (kWaves * 64)) : 0;
-  const int item = item_of(blockIdx.x, gridDim.x);
-  const int head = item / A.tiles, tile = A.tiles - 1 - item % A.tiles, kvh = head / (A.H / A.K);
+  const Item item = item_of(blockIdx.x, gridDim.x, A.H);
+  const int head = item.unit, tile = A.tiles - 1 - item.tile, kvh = head / (A.H / A.K);
   const int i = tile * kBlock + wave * kRows + (lane & 31);  // this lane's row
   const Reach R = reach_of(A, i, true, s_reach + 2 * group, wave);
   u32x4 q[DC / 16];
@@ -608,8 +618,8 @@ __device__ __forceinline__ bool dq_tile(const AttnArgs &A, char *s_k0, char *s_k
   constexpr int NB = CAREFUL ? 1 : DC / 32;  // sums a pass holds, see CEL_TILE_KERNEL
   const int tid = threadIdx.x % (kWaves * 64), lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int group = G > 1 ? __builtin_amdgcn_readfirstlane(threadIdx.x / (kWaves * 64)) : 0;
-  const int item = item_of(blockIdx.x, gridDim.x);
-  const int head = item / A.tiles, tile = A.tiles - 1 - item % A.tiles, kvh = head / (A.H / A.K);
+  const Item item = item_of(blockIdx.x, gridDim.x, A.H);
+  const int head = item.unit, tile = A.tiles - 1 - item.tile, kvh = head / (A.H / A.K);
   const int i = tile * kBlock + wave * kRows + (lane & 31);
   const Reach R = reach_of(A, i, true, s_reach + 2 * group, wave);
   u32x4 q[DC / 16], g[DC / 16];
@@ -889,9 +899,9 @@ __device__ __forceinline__ bool dkv_tile(const AttnArgs &A, char *s_q0, char *s_
                                          float *s_r1, int (*s_reach)[kWaves]) {
   constexpr int NB = CAREFUL ? 2 : DC / 16, KK = DC / 32;  // sums a pass holds, see CEL_TILE_KERNEL
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), g4 = 4 * (lane >> 4);
-  const int tiles = (A.T + kKeyBlock - 1) / kKeyBlock;
-  const int item = item_of(blockIdx.x, gridDim.x), kvh = item / tiles / A.parts, part = item / tiles % A.parts;
-  const int j = item % tiles * kKeyBlock + wave * kKeys + (lane & 15);  // this lane's key
+  const Item item = item_of(blockIdx.x, gridDim.x, A.K * A.parts);
+  const int kvh = item.unit / A.parts, part = item.unit % A.parts;
+  const int j = item.tile * kKeyBlock + wave * kKeys + (lane & 15);  // this lane's key
   int head0, heads;
   heads_of(A, kvh, part, head0, heads);
   const Reach R = reach_of(A, j, false, s_reach, wave);
