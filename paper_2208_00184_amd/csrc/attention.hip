@@ -451,9 +451,9 @@ __device__ __forceinline__ void mask(acc16 &x, int t, int lo, int hi, float by, 
 // vector unit, which two waves on a SIMD overlap.  A tile of 128 rows reads each
 // staged key and value four times from LDS, which then gives what the products
 // take; more rows would not fit two waves' registers.  16,384 tokens in one sequence,
-// 16 heads of 128 over 4: 1.03 ms, 1.07 PFLOP/s, where a large library product
+// 16 heads of 128 over 4: 1.04 ms, 1.06 PFLOP/s, where a large library product
 // reaches 1.36 and this kernel without its softmax 1.25; 8,192 tokens, 32 heads
-// over 8: 0.55 ms, 0.99 PFLOP/s, matrix cores 54 % busy, no bank conflicts.
+// over 8: 0.53 ms, 1.04 PFLOP/s, matrix cores 56 % busy, no bank conflicts.
 // 4 sequences of 1,024, 16 heads of 64: 23 us, the 16 steps of a sequence's last
 // tile (0.8 us each at 64 dimensions, 1.1 at 128) behind some 7 us of start and end.
 template <class T, int DP, int DC, int G, bool CAREFUL>
@@ -607,7 +607,7 @@ CEL_TILE_KERNEL(k_attention, attention_tile, s_k0, s_k1, s_v0, s_v1)
 // p_ij <do_i, v_j> in 32 bits, at the price of that tile's products twice.
 // Tiles and bounds are the forward pass's, with three products a step and 32 keys'
 // scores in registers at a time: 8,192 tokens in one sequence, 32 heads of 128 over
-// 8: 0.79 ms, 1.04 PFLOP/s, matrix cores 59 % busy.  dq has a kernel of its own since
+// 8: 0.75 ms, 1.10 PFLOP/s, matrix cores 61 % busy.  dq has a kernel of its own since
 // its sums run over the other axis than dk's and dv's: joined, one side would be
 // added up in memory, by atomics in no fixed order.  The price is that scores and
 // their gradients are made twice, 7 products where 5 would do.
@@ -785,7 +785,7 @@ __device__ inline void heads_of(const AttnArgs &A, int kvh, int part, int &first
 // share a SIMD and every product is made once; the reads of LDS a product are
 // twice as many, 256 bytes a cycle at the matrix cores' full rate, which is what
 // LDS gives.  8,192 tokens in one sequence, 32 heads of 128 over 8: 1.12 ms for four
-// products, 0.98 PFLOP/s, matrix cores 49 % busy (32 keys a wave and a launch each for
+// products, 0.99 PFLOP/s, matrix cores 49 % busy (32 keys a wave and a launch each for
 // dk and dv, five products: 1.55 ms; pairs of waves that hand p over in LDS: 1.62 ms).
 //   A result tile D[m][n] puts column n = lane % 16 and rows 4 (lane / 16) + r in
 //   register r; two of them are a right operand of 32 rows, in the order
@@ -1048,7 +1048,9 @@ int check_attn(const cel_attn *a, const char *fn) {
 // Into how many workgroups a tile of keys deals out the query heads that share
 // them: as many as bring six workgroups to each of the 256 compute units (the
 // tiles at a long sequence's beginning take many times the average), each with the
-// same number of heads but the last.
+// same number of heads but the last.  (Against four: 37 ragged sequences, 24 heads of 80
+// over 4: 184 us with the join against 208; 8,192 tokens, 32 heads of 128 over 8: 1.15 ms against
+// 1.20; but 4 sequences of 1,024, 32 heads over 8: 145 against 131 us.)
 int parts_of(const cel_attn *a) {
   const int64_t group = a->heads / a->kv_heads, tiles = ((int64_t)a->tokens + kKeyBlock - 1) / kKeyBlock;
   const int64_t per = std::max<int64_t>(1, group * tiles * a->kv_heads / 1536);
