@@ -1042,7 +1042,6 @@ int check_attn(const cel_attn *a, const char *fn) {
     return set_error(CEL_E_ARG, "%s: scale %g is not positive and finite", fn, (double)a->scale);
   if (((int64_t)a->tokens + kKeyBlock - 1) / kKeyBlock * a->heads > INT32_MAX)
     return set_error(CEL_E_ARG, "%s: %d tokens of %d heads", fn, a->tokens, a->heads);
-  if (!a->seq_ptr) return set_error(CEL_E_ARG, "%s: seq_ptr is NULL", fn);
   return CEL_OK;
 }
 // Into how many workgroups a tile of keys deals out the query heads that share
@@ -1143,6 +1142,7 @@ extern "C" int cel_attention(const cel_attn *a, const cel_rows *out, float *lse,
   const char *fn = "cel_attention";
   int rc = check_attn(a, fn);
   if (rc) return rc;
+  if (!a->seq_ptr) return set_error(CEL_E_ARG, "%s: seq_ptr is NULL", fn);
   if (a->tokens == 0) return CEL_OK;
   if ((rc = check_rows(&a->q, a, fn, "q")) || (rc = check_rows(&a->k, a, fn, "k")) ||
       (rc = check_rows(&a->v, a, fn, "v")) || (rc = check_rows(out, a, fn, "out")))
@@ -1163,6 +1163,7 @@ extern "C" int cel_attention_grad(const cel_attn *a, const cel_rows *out, const 
   const char *fn = "cel_attention_grad";
   int rc = check_attn(a, fn);
   if (rc) return rc;
+  if (!a->seq_ptr) return set_error(CEL_E_ARG, "%s: seq_ptr is NULL", fn);
   if (a->tokens == 0) return CEL_OK;
   if ((rc = check_rows(&a->q, a, fn, "q")) || (rc = check_rows(&a->k, a, fn, "k")) ||
       (rc = check_rows(&a->v, a, fn, "v")) || (rc = check_rows(out, a, fn, "out")) ||
