@@ -30,7 +30,8 @@ constexpr int kRankMost = 8192;  // tokens that are ranked against each other, a
 constexpr int kRankB = 256, kRankEach = 16, kRankTokens = kRankB / kRankEach;  // threads, threads a token, tokens
 constexpr int kSlice = 512;      // columns a wave handles
 constexpr int kTogether = 4;     // rows of the lookup that a wave has on their way at once
-constexpr int kRowsAt = 4;       // table rows a wave writes one behind the other
+constexpr int kRowsAt = 4;       // table rows a wave writes one behind the other,
+constexpr int64_t kFewRows = 16384;  // unless there are at most this many pieces of rows, see k_embed_grad
 
 // BYTES at any address of the element type, as one access.
 template <int BYTES>
@@ -365,23 +366,26 @@ __global__ void __launch_bounds__(256) k_embed_parts(const uint32_t *__restrict_
   }
 }
 
-// A wave takes kRowsAt rows of the table and kSlice of their columns.  Bound by memory:
+// A wave takes `rows` rows of the table and kSlice of their columns: one where the
+// pieces are few, so that no wave adds several frequent words while others are done (1,000
+// rows of 64, 8,192 tokens: 24 -> 14 us, 32,768 tokens 50 -> 35; at 16,000 pieces the two are within
+// 7 % of each other), else kRowsAt (131,072 rows of 8,192: 607 us one by one, 480 so).  Bound by memory:
 // 131,072 rows of 8,192 from 32,768 tokens, 16 bits: 480 us, 2.5 GB at 5.2 TB/s; 50,001 rows
 // of 1,024 in 32 bits from 4,096: 32 to 43 us (205 MB written).  Eight rows of dx on their way
 // instead of four take more registers and leave fewer waves: 724 us for the first.
 template <class T, class O, bool NT>
 __global__ void __launch_bounds__(256) k_embed_grad(const uint32_t *start, const uint32_t *__restrict__ order, int64_t vocab,
                                                     const T *dx, int64_t stride, int64_t h, int slices,
-                                                    const float *__restrict__ part, float scale, O *grad) {
+                                                    const float *__restrict__ part, float scale, int rows, O *grad) {
   constexpr int E = Shape<O>::E, S = Shape<O>::S;
   const int lane = threadIdx.x & 63;
   const int64_t task = (int64_t)blockIdx.x * 4 + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-  const int64_t v0 = task / slices * kRowsAt;
+  const int64_t v0 = task / slices * rows;
   if (v0 >= vocab) return;
   const int64_t c0 = (task % slices) * kSlice + lane * E;
-  const uint32_t at = lane <= kRowsAt && v0 + lane <= vocab ? start[v0 + lane] : 0;
+  const uint32_t at = lane <= rows && v0 + lane <= vocab ? start[v0 + lane] : 0;
 #pragma unroll 1
-  for (int r = 0; r < kRowsAt && v0 + r < vocab; r++) {
+  for (int r = 0; r < rows && v0 + r < vocab; r++) {
     const int64_t a = (uint32_t)__builtin_amdgcn_readlane(at, r), b = (uint32_t)__builtin_amdgcn_readlane(at, r + 1);
     float f[S][E] = {};
     if (a < b) {
@@ -512,12 +516,13 @@ int embed_grad(const cel_embed_args *a, const void *dx, void *work, int grad_typ
                                             a->hidden, slices, part);
     CEL_HIP(hipGetLastError());
   }
-  CEL_TRY(blocks_of((a->vocab + kRowsAt - 1) / kRowsAt * slices, "cel_embed_grad", &blocks));
+  const int rows = a->vocab * slices <= kFewRows ? 1 : kRowsAt;
+  CEL_TRY(blocks_of((a->vocab + rows - 1) / rows * slices, "cel_embed_grad", &blocks));
   KTimer kt(s, "k_embed_grad");
   auto go = [&](auto out, auto nt) {
     typedef decltype(out) O;
     k_embed_grad<T, O, decltype(nt)::value><<<blocks, 256, 0, s>>>(start, order, a->vocab, (const T *)dx, a->stride, a->hidden,
-                                                                   slices, part, a->scale, (O *)grad);
+                                                                   slices, part, a->scale, rows, (O *)grad);
   };
   const bool f32 = grad_type == CEL_F32, nt = a->vocab * a->hidden * (f32 ? 4 : (int64_t)sizeof(T)) > kCached;
   if (f32) nt ? go(float{}, std::true_type{}) : go(float{}, std::false_type{});

@@ -242,3 +242,8 @@ def test_views_of_a_buffer_beyond_32_bits():
 @pytest.mark.parametrize("T", [8191, 8192, 8193])
 def test_gradient_where_the_sort_changes(T):
     check_grad(randn(T, 24, seed=T).bfloat16().to(DEV), zipf(T, 9000, T).to(DEV), 9000, 1.0, None)
+
+
+@pytest.mark.parametrize("V,h", [(16384, 8), (16385, 8), (8192, 1024), (8193, 1000)])
+def test_gradient_where_a_waves_rows_change(V, h):
+    check_grad(randn(900, h, seed=V).bfloat16().to(DEV), zipf(900, V, V).to(DEV), V, 1.0, torch.float32)
