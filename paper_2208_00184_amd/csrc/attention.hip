@@ -1118,6 +1118,9 @@ int parts_of(const cel_attn *a) {
   const int64_t per = std::max<int64_t>(1, group * tiles * a->kv_heads / 1536);
   return per >= group ? 1 : (int)((group + per - 1) / per);
 }
+// Where the parts begin in the backward pass's scratch, in floats: behind lse and D of every row, on
+// the 16 bytes of the vectors that they are written and read as.
+int64_t part_at(const cel_attn *a) { return (2 * (int64_t)a->heads * a->tokens + 3) / 4 * 4; }
 Rows rows_of(const cel_rows *x) { return Rows{static_cast<char *>(x->p), x->row, x->head}; }
 AttnArgs args_of(const cel_attn *a) {
   AttnArgs A{};
@@ -1197,8 +1200,7 @@ extern "C" int64_t cel_attention_grad_scratch(const cel_attn *a) {
   const int rc = check_attn(a, "cel_attention_grad_scratch");
   if (rc) return rc;
   const int parts = parts_of(a);
-  const int64_t rows = 2 * (int64_t)a->heads * a->tokens;
-  return 4 * (rows + (parts > 1 ? 2 * (int64_t)parts * a->tokens * a->kv_heads * a->dim : 0));
+  return 4 * (part_at(a) + (parts > 1 ? 2 * (int64_t)parts * a->tokens * a->kv_heads * a->dim : 0));
 }
 
 extern "C" int cel_attention(const cel_attn *a, const cel_rows *out, float *lse, hipStream_t s) {
@@ -1240,7 +1242,7 @@ extern "C" int cel_attention_grad(const cel_attn *a, const cel_rows *out, const 
   A.lse = const_cast<float *>(lse);
   A.rows = scratch;
   A.parts = parts_of(a);
-  A.part = scratch + 2 * (int64_t)a->heads * a->tokens;
+  A.part = scratch + part_at(a);
   if (a->type == CEL_BF16) {
     launch_dq<__bf16>(A, s);
     CEL_HIP(hipGetLastError());

@@ -113,3 +113,9 @@ def test_embed_other_arguments(lib):
     assert lib.cel_embed_grad_scratch(10, 0, 10) == ARG
     assert lib.cel_embed_grad_scratch(10, 10, 0) == ARG
     assert lib.cel_embed_grad_scratch(0, 10, 10) >= 4 * 11
+
+
+def test_attention_scratch_of_an_odd_number_of_rows(lib):
+    """The parts lie behind 2 x 3 x 137 numbers, rounded up to 16 bytes for their vectors of four."""
+    a = attn(tokens=137, heads=3, kv_heads=1, q=rows(row=3 * 64), seq_ptr=None)
+    assert lib.cel_attention_grad_scratch(ctypes.byref(a)) == 4 * (824 + 2 * 3 * 137 * 64)
