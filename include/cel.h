@@ -354,7 +354,8 @@ typedef struct {
  * results, without an access outside the arrays. */
 typedef struct {
   int32_t type;                  /* of all rows: CEL_BF16 or CEL_F16 */
-  int32_t tokens, n_seq;         /* >= 0 */
+  int32_t tokens, n_seq;         /* >= 0; tokens < 2^31 - 4096, tokens * heads below about 2^31,
+                                  * with the gradient 2^30 (2^24 - 1 tiles of 128 tokens of a head, or of 64) */
   int32_t heads, kv_heads, dim;  /* heads a multiple of kv_heads: query head h reads key/value
                                   * head h / (heads / kv_heads); dim 8, 16, ... 128 */
   float scale;                   /* of the scores, > 0 (usually 1 / sqrt(dim)) */

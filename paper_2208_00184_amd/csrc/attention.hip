@@ -1092,6 +1092,12 @@ int check_rows(const cel_rows *x, const cel_attn *a, const char *fn, const char 
     return set_error(CEL_E_ARG, "%s: %s has a stride out of range", fn, what);
   return CEL_OK;
 }
+// A launch has fewer than 2^32 threads: that many workgroups at most, for tiles of `rows` tokens.
+int check_grid(const cel_attn *a, int rows, const char *fn) {
+  if (((int64_t)a->tokens + rows - 1) / rows * a->heads * (kWaves * 64) > UINT32_MAX)
+    return set_error(CEL_E_ARG, "%s: %d tokens of %d heads", fn, a->tokens, a->heads);
+  return CEL_OK;
+}
 int check_attn(const cel_attn *a, const char *fn) {
   if (!a) return set_error(CEL_E_ARG, "%s: NULL descriptor", fn);
   if (a->type != CEL_BF16 && a->type != CEL_F16) return set_error(CEL_E_ARG, "%s: type %d", fn, a->type);
@@ -1103,9 +1109,7 @@ int check_attn(const cel_attn *a, const char *fn) {
     return set_error(CEL_E_ARG, "%s: dim %d is not a multiple of 8 in 8..128", fn, a->dim);
   if (!(a->scale > 0.f) || !std::isfinite(a->scale) || !std::isfinite(8.f / (a->scale * kLog2e)))
     return set_error(CEL_E_ARG, "%s: scale %g is not positive and finite", fn, (double)a->scale);
-  if (((int64_t)a->tokens + kKeyBlock - 1) / kKeyBlock * a->heads > INT32_MAX)
-    return set_error(CEL_E_ARG, "%s: %d tokens of %d heads", fn, a->tokens, a->heads);
-  return CEL_OK;
+  return check_grid(a, kBlock, fn);  // the forward pass's and dq's launch
 }
 // Into how many workgroups a tile of keys deals out the query heads that share
 // them: as many as bring six workgroups to each of the 256 compute units (the
@@ -1197,8 +1201,9 @@ void launch_dkv(const AttnArgs &A, hipStream_t s) {
 using namespace cel;
 
 extern "C" int64_t cel_attention_grad_scratch(const cel_attn *a) {
-  const int rc = check_attn(a, "cel_attention_grad_scratch");
-  if (rc) return rc;
+  const char *fn = "cel_attention_grad_scratch";
+  CEL_TRY(check_attn(a, fn));
+  CEL_TRY(check_grid(a, kKeyBlock, fn));
   const int parts = parts_of(a);
   return 4 * (part_at(a) + (parts > 1 ? 2 * (int64_t)parts * a->tokens * a->kv_heads * a->dim : 0));
 }
@@ -1227,7 +1232,7 @@ extern "C" int cel_attention_grad(const cel_attn *a, const cel_rows *out, const 
                                   hipStream_t s) {
   const char *fn = "cel_attention_grad";
   int rc = check_attn(a, fn);
-  if (rc) return rc;
+  if (rc || (rc = check_grid(a, kKeyBlock, fn))) return rc;
   if (!a->seq_ptr) return set_error(CEL_E_ARG, "%s: seq_ptr is NULL", fn);
   if (a->tokens == 0) return CEL_OK;
   if ((rc = check_rows(&a->q, a, fn, "q")) || (rc = check_rows(&a->k, a, fn, "k")) ||

@@ -33,6 +33,11 @@ constexpr int kTogether = 4;     // rows of the lookup that a wave has on their 
 constexpr int kRowsAt = 4;       // table rows a wave writes one behind the other,
 constexpr int64_t kFewRows = 16384;  // unless there are at most this many pieces of rows, see k_embed_grad
 
+// A launch has fewer than 2^32 threads along x: workgroups beyond kGridX stand in further rows of
+// the grid.  The last row's surplus has nothing to do.
+constexpr int64_t kGridX = 1 << 23;
+__device__ inline int64_t block_number() { return (int64_t)blockIdx.y * gridDim.x + blockIdx.x; }
+
 // BYTES at any address of the element type, as one access.
 template <int BYTES>
 struct __attribute__((packed, aligned(2))) Raw {
@@ -100,7 +105,7 @@ template <class T, class I, bool NT>
 __global__ void __launch_bounds__(256) k_embed(const T *table, int64_t stride, int64_t vocab, const I *ids, int64_t tokens,
                                                int64_t h, int slices, float scale, T *out) {
   constexpr int E = Shape<T>::E, S = Shape<T>::S;
-  const int64_t task = (int64_t)blockIdx.x * 4 + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int64_t task = block_number() * 4 + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int64_t t0 = task / slices * kTogether, c0 = (task % slices) * kSlice + (threadIdx.x & 63) * E;
   if (t0 >= tokens) return;
   Raw<16> r[kTogether][S];
@@ -326,8 +331,9 @@ template <class T>
 __global__ void __launch_bounds__(256) k_embed_parts(const uint32_t *__restrict__ keys, const uint32_t *__restrict__ order,
                                                      int64_t tokens, int64_t vocab, int searches, uint32_t *start, const T *dx,
                                                      int64_t stride, int64_t h, int slices, float *part) {
-  if ((int)blockIdx.x < searches) {
-    const int64_t v = (int64_t)blockIdx.x * 256 + threadIdx.x;
+  const int64_t block = block_number();
+  if (block < searches) {
+    const int64_t v = block * 256 + threadIdx.x;
     if (v > vocab) return;
     int64_t lo = 0, hi = tokens;
     while (lo < hi) {
@@ -339,7 +345,7 @@ __global__ void __launch_bounds__(256) k_embed_parts(const uint32_t *__restrict_
     return;
   }
   constexpr int E = Shape<float>::E, S = Shape<float>::S;
-  const int64_t task = (int64_t)(blockIdx.x - searches) * 4 + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int64_t task = (block - searches) * 4 + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   // The chunk that begins among the kChunk tokens from w on, if there is one,
   // reaches past the last of them, and holds one kChunk / 2 further or nearer too.
   const int64_t chunk = task / slices, w = chunk * kChunk;
@@ -379,7 +385,7 @@ __global__ void __launch_bounds__(256) k_embed_grad(const uint32_t *start, const
                                                     const float *__restrict__ part, float scale, int rows, O *grad) {
   constexpr int E = Shape<O>::E, S = Shape<O>::S;
   const int lane = threadIdx.x & 63;
-  const int64_t task = (int64_t)blockIdx.x * 4 + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int64_t task = block_number() * 4 + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int64_t v0 = task / slices * rows;
   if (v0 >= vocab) return;
   const int64_t c0 = (task % slices) * kSlice + lane * E;
@@ -445,23 +451,23 @@ int check_embed(const cel_embed_args *a, const char *fn) {
 int slices_of(const cel_embed_args *a) {
   return (int)((a->hidden + kSlice - 1) / kSlice);
 }
-int blocks_of(int64_t waves, const char *fn, unsigned *blocks) {
-  const int64_t b = (waves + 3) / 4;
-  if (b > INT32_MAX) return set_error(CEL_E_ARG, "%s: too large a call", fn);
-  *blocks = (unsigned)b;
+int grid_of(int64_t waves, const char *fn, dim3 *grid) {
+  const int64_t b = (waves + 3) / 4, rows = (b + kGridX - 1) / kGridX;
+  if (rows > 65535) return set_error(CEL_E_ARG, "%s: too large a call", fn);
+  *grid = dim3((unsigned)std::min(b, kGridX), (unsigned)rows);
   return CEL_OK;
 }
 
 template <class T>
 int embed(const cel_embed_args *a, const void *table, void *out, hipStream_t s) {
   const int slices = slices_of(a);
-  unsigned blocks;
-  CEL_TRY(blocks_of((a->tokens + kTogether - 1) / kTogether * slices, "cel_embed", &blocks));
+  dim3 grid;
+  CEL_TRY(grid_of((a->tokens + kTogether - 1) / kTogether * slices, "cel_embed", &grid));
   KTimer kt(s, "k_embed");
   auto go = [&](auto id, auto nt) {
     typedef decltype(id) I;
-    k_embed<T, I, decltype(nt)::value><<<blocks, 256, 0, s>>>((const T *)table, a->stride, a->vocab, (const I *)a->ids,
-                                                              a->tokens, a->hidden, slices, a->scale, (T *)out);
+    k_embed<T, I, decltype(nt)::value><<<grid, 256, 0, s>>>((const T *)table, a->stride, a->vocab, (const I *)a->ids,
+                                                            a->tokens, a->hidden, slices, a->scale, (T *)out);
   };
   const bool nt = a->tokens * a->hidden * (int64_t)sizeof(T) > kCached;
   if (a->id_bytes == 4) nt ? go(int32_t{}, std::true_type{}) : go(int32_t{}, std::false_type{});
@@ -500,29 +506,28 @@ int sort_tokens(const cel_embed_args *a, const Plan &p, char *w, int *in, hipStr
 template <class T>
 int embed_grad(const cel_embed_args *a, const void *dx, void *work, int grad_type, void *grad, hipStream_t s) {
   const Plan p = plan_of(a->tokens, a->vocab, a->hidden);
+  const int slices = slices_of(a), searches = (int)((a->vocab + 1 + 255) / 256);
+  const int rows = a->vocab * slices <= kFewRows ? 1 : kRowsAt;
+  dim3 parts, sums;
+  CEL_TRY(grid_of((a->tokens / kChunk) * slices + 4 * (int64_t)searches, "cel_embed_grad", &parts));
+  CEL_TRY(grid_of((a->vocab + rows - 1) / rows * slices, "cel_embed_grad", &sums));
   char *w = static_cast<char *>(work);
   int in = 0;
   CEL_TRY(a->id_bytes == 4 ? sort_tokens<int32_t>(a, p, w, &in, s) : sort_tokens<int64_t>(a, p, w, &in, s));
-  const int slices = slices_of(a);
   const uint32_t *keys = reinterpret_cast<uint32_t *>(w + p.keys[in]), *order = reinterpret_cast<uint32_t *>(w + p.order[in]);
   uint32_t *start = reinterpret_cast<uint32_t *>(w + p.start);
   float *part = reinterpret_cast<float *>(w + p.part);
-  const int searches = (int)((a->vocab + 1 + 255) / 256);
-  unsigned blocks;
-  CEL_TRY(blocks_of((a->tokens / kChunk) * slices + 4 * (int64_t)searches, "cel_embed_grad", &blocks));
   {
     KTimer kt(s, "k_embed_parts");
-    k_embed_parts<T><<<blocks, 256, 0, s>>>(keys, order, a->tokens, a->vocab, searches, start, (const T *)dx, a->stride,
-                                            a->hidden, slices, part);
+    k_embed_parts<T><<<parts, 256, 0, s>>>(keys, order, a->tokens, a->vocab, searches, start, (const T *)dx, a->stride,
+                                           a->hidden, slices, part);
     CEL_HIP(hipGetLastError());
   }
-  const int rows = a->vocab * slices <= kFewRows ? 1 : kRowsAt;
-  CEL_TRY(blocks_of((a->vocab + rows - 1) / rows * slices, "cel_embed_grad", &blocks));
   KTimer kt(s, "k_embed_grad");
   auto go = [&](auto out, auto nt) {
     typedef decltype(out) O;
-    k_embed_grad<T, O, decltype(nt)::value><<<blocks, 256, 0, s>>>(start, order, a->vocab, (const T *)dx, a->stride, a->hidden,
-                                                                   slices, part, a->scale, rows, (O *)grad);
+    k_embed_grad<T, O, decltype(nt)::value><<<sums, 256, 0, s>>>(start, order, a->vocab, (const T *)dx, a->stride, a->hidden,
+                                                                 slices, part, a->scale, rows, (O *)grad);
   };
   const bool f32 = grad_type == CEL_F32, nt = a->vocab * a->hidden * (f32 ? 4 : (int64_t)sizeof(T)) > kCached;
   if (f32) nt ? go(float{}, std::true_type{}) : go(float{}, std::false_type{});

@@ -119,3 +119,15 @@ def test_attention_scratch_of_an_odd_number_of_rows(lib):
     """The parts lie behind 2 x 3 x 137 numbers, rounded up to 16 bytes for their vectors of four."""
     a = attn(tokens=137, heads=3, kv_heads=1, q=rows(row=3 * 64), seq_ptr=None)
     assert lib.cel_attention_grad_scratch(ctypes.byref(a)) == 4 * (824 + 2 * 3 * 137 * 64)
+
+
+def test_attention_launches_stay_below_what_a_grid_takes(lib):
+    """2^24 workgroups of 256 threads are one too many: refused before anything is enqueued."""
+    r, p = ctypes.byref(rows()), ctypes.c_void_p(SOME)
+    for kw, forward in ((dict(tokens=2 ** 26, heads=64, kv_heads=64), True), (dict(tokens=2 ** 24, heads=64, kv_heads=8), False)):
+        a = attn(**kw)
+        assert lib.cel_attention_grad_scratch(ctypes.byref(a)) == ARG
+        assert lib.cel_attention_grad(ctypes.byref(a), r, p, r, p, r, r, r, None) == ARG
+        if forward:
+            assert lib.cel_attention(ctypes.byref(a), r, p, None) == ARG
+    assert lib.cel_attention_grad_scratch(ctypes.byref(attn(tokens=2 ** 24 - 64, heads=64, kv_heads=64))) > 0
