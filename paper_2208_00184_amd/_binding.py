@@ -8,6 +8,7 @@ stream.  There is no CPU fallback: a missing library or a failed call raises.
 from __future__ import annotations
 
 import ctypes as C
+import math
 import os
 from contextlib import nullcontext
 from dataclasses import dataclass
@@ -554,6 +555,50 @@ def _views(*tensors):
     return views, keep
 
 
+def _block(x, T, H, d):
+    """A view's (first element, element behind its last, row stride, head stride, heads)."""
+    at, row, head = (x.p or 0) // 2, x.row, x.head
+    return at, at + (T - 1) * row + (H - 1) * head + d, row, head, H
+
+
+def _folded(x, T, d):
+    """Whether elements of a block share memory."""
+    (lo, n), (hi, m) = sorted([(s, k) for s, k in ((x[3], x[4]), (x[2], T)) if k > 1] + [(1 << 62, 1)] * 2)[:2]
+    if n == 1:
+        return False
+    if lo < d or m == 1:
+        return lo < d
+    for a in range(1, min(m, ((n - 1) * lo + d - 1) // hi + 1)):  # a large steps against the nearest small ones
+        b, off = divmod(a * hi, lo)
+        if (off < d and b < n) or (lo - off < d and b + 1 < n):
+            return True
+    return False
+
+
+def _meet(x, y, T, d):
+    """Whether two blocks share memory.  Of blocks that interleave with different row strides only
+    those with the same first element are known to."""
+    if x[1] <= y[0] or y[1] <= x[0]:
+        return False
+    g = math.gcd(x[2], x[3], y[2], y[3])  # all steps are multiples of it
+    if d <= (x[0] - y[0]) % g <= g - d:
+        return False
+    row = x[2]
+    if y[2] != row:
+        return x[0] == y[0]
+    parts = []
+    for at, _, _, head, heads in (x, y):  # the heads of a row as one piece, where they fit in it
+        width = (heads - 1) * head + d
+        parts.append([(at, width)] if width <= row else [(at + h * head, d) for h in range(heads)])
+    for whole in (True, False):
+        if not any(-w < a - b - s * row < v and -T < s < T
+                   for a, w in parts[0] for b, v in parts[1] for s in ((a - b) // row, (a - b) // row + 1)):
+            return False
+        if whole:
+            parts = [[(at + h * head, d) for h in range(heads)] for at, _, _, head, heads in (x, y)]
+    return True
+
+
 def _attn(fn, q, k, v, seq_ptr, scale):
     """-> (descriptor, tensors to keep alive)"""
     if q.dim() != 3 or k.dim() != 3 or v.dim() != 3 or q.dtype not in (torch.bfloat16, torch.float16) or \
@@ -594,8 +639,8 @@ def attention(q, k, v, seq_ptr, scale=None):
 def attention_grad(dout, q, k, v, out, lse, seq_ptr, scale=None, grads=None):
     """The gradient of attention() at dout [T, heads, dim], with its out and lse.
     -> (dq, dk, dv) as q, k, v are shaped.  grads: three tensors to write them to (for instance views
-    of one fused gradient; values contiguous, addresses and strides multiples of 16 bytes).  The same
-    inputs give the same bits."""
+    of one fused gradient; values contiguous, addresses and strides multiples of 16 bytes; no memory
+    shared with an input, with each other or within one).  The same inputs give the same bits."""
     fn = "attention_grad"
     index = _device_of(fn, q=q, k=k, v=v, seq_ptr=seq_ptr, dout=dout, out=out, lse=lse)
     with _on(index):
@@ -607,7 +652,8 @@ def attention_grad(dout, q, k, v, out, lse, seq_ptr, scale=None, grads=None):
             _refuse(f"{fn}: lse is not float32 [heads, tokens]")
         (gv, ov), keep2 = _views(dout, out)
         lse = lse.contiguous()
-        if grads is None:
+        given = grads is not None
+        if not given:
             grads = tuple(torch.empty(t.shape, dtype=q.dtype, device=q.device) for t in (q, k, v))
         elif len(grads) != 3:
             _refuse(f"{fn}: grads are not three tensors")
@@ -618,12 +664,26 @@ def attention_grad(dout, q, k, v, out, lse, seq_ptr, scale=None, grads=None):
             view = _view(t) if t.shape == x.shape and t.dtype == q.dtype else None
             if view is None and t.numel():
                 _refuse(f"{fn}: {name} cannot be written in place: {tuple(t.shape)} {t.dtype}, strides {t.stride()}")
-            views.append(C.byref(view or _Rows()))
+            views.append(view or _Rows())
+        if given and a.tokens:
+            T, d, heads = a.tokens, a.dim, (a.heads, a.kv_heads, a.kv_heads)
+            blocks = [_block(x, T, n, d) for x, n in zip(views, heads)]
+            others = [(name, _block(x, T, n, d)) for name, x, n in zip(
+                ("q", "k", "v", "out", "dout"), (a.q, a.k, a.v, ov, gv), heads + (heads[0], heads[0]))]
+            first, last = min(x[0] for x in blocks), max(x[1] for x in blocks)
+            others = [y for y in others if y[1][0] < last and first < y[1][1]]
+            for name, x in zip(("dq", "dk", "dv"), blocks):
+                if _folded(x, T, d):
+                    _refuse(f"{fn}: values of {name} share memory")
+                for other, y in others:
+                    if _meet(x, y, T, d):
+                        _refuse(f"{fn}: {name} shares memory with {other}")
+                others.append((name, x))
         size = lib().cel_attention_grad_scratch(C.byref(a))
         if size < 0:
             _check(size)
         scratch = torch.empty(size, dtype=torch.uint8, device=q.device)
-        _check(lib().cel_attention_grad(C.byref(a), C.byref(ov), lse.data_ptr(), C.byref(gv), scratch.data_ptr(), *views,
+        _check(lib().cel_attention_grad(C.byref(a), C.byref(ov), lse.data_ptr(), C.byref(gv), scratch.data_ptr(), *map(C.byref, views),
                                         _raw_stream(index)))
     return tuple(grads)
 
