@@ -500,7 +500,9 @@ def makespan(g: Graph, d: Devices, order, level, level_ptr, n_levels, node_dev, 
 # They enqueue their work on the current stream of the tensors' device and
 # return; outputs and scratch come from torch's allocator on that stream.  An
 # input that another stream fills or frees is the caller's to order, as with
-# any torch operation.
+# any torch operation.  They record nothing for torch's automatic gradients, and
+# refuse tensors that ask for one, unless those are switched off
+# (torch.no_grad(), or inside a torch.autograd.Function).
 
 _TYPES = {torch.bfloat16: 0, torch.float16: 1, torch.float32: 2}
 
@@ -520,14 +522,17 @@ def _raw_stream(index):
 
 
 def _device_of(fn, **tensors):
-    """The index of the ROCm device that all of them are on."""
-    index = -1
+    """The index of the ROCm device that all of them are on.  None may ask for a gradient: results
+    would be cut off from it without a sign."""
+    index, graph = -1, torch.is_grad_enabled()
     for name, t in tensors.items():
         if not isinstance(t, torch.Tensor) or not t.is_cuda:
             _refuse(f"{fn}: {name} is not a tensor on a ROCm device")
         at = t.get_device()
         if index >= 0 and at != index:
             _refuse(f"{fn}: {name} is on device {at}, not on {index}")
+        if graph and t.requires_grad:
+            _refuse(f"{fn}: {name} requires a gradient, which is not recorded: call under torch.no_grad()")
         index = at
     return index
 

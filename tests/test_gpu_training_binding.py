@@ -1,0 +1,73 @@
+"""What the binding of the training-step operations refuses and accepts besides the sizes and types."""
+from __future__ import annotations
+
+import pytest
+
+torch = pytest.importorskip("torch")
+
+pytestmark = pytest.mark.gpu
+
+if not torch.cuda.is_available():  # collected on CPU, skipped there
+    pytest.skip("needs a ROCm GPU", allow_module_level=True)
+
+import paper_2208_00184_amd as cel  # noqa: E402
+
+DEV = "cuda:0"
+
+
+def refused(f, *a, **kw):
+    with pytest.raises(cel.CelError) as e:
+        f(*a, **kw)
+    assert e.value.code == -1
+
+
+def batch(T=40, H=4, K=2, d=64, seed=0):
+    g = torch.Generator().manual_seed(seed)
+    return [torch.randn(T, n, d, generator=g).bfloat16().to(DEV) for n in (H, K, K, H)] + [
+        torch.tensor([0, T], dtype=torch.int32, device=DEV)]
+
+
+def test_tensors_that_ask_for_a_gradient():
+    q, k, v, g, ptr = batch()
+    out, lse = cel.attention(q, k, v, ptr)
+    plain = cel.attention_grad(g, q, k, v, out, lse, ptr)
+    ids, table, dx = torch.arange(5, device=DEV), torch.randn(7, 16, device=DEV), torch.randn(5, 16, device=DEV)
+    rows, dtable = cel.embed(table, ids), cel.embed_grad(dx, ids, 7)
+    for t in (q, k, v, table, dx, g):
+        t.requires_grad_()
+    for x in ((q, k.detach(), v.detach()), (q.detach(), k, v.detach()), (q.detach(), k.detach(), v)):
+        refused(cel.attention, *x, ptr)
+        refused(cel.attention_grad, g.detach(), *x, out, lse, ptr)
+    x = [t.detach() for t in (q, k, v)]
+    refused(cel.attention_grad, g, *x, out, lse, ptr)
+    refused(cel.attention_grad, g.detach(), *x, out, lse, ptr, grads=[torch.zeros_like(t).requires_grad_() for t in x])
+    refused(cel.embed, table, ids)
+    refused(cel.embed_grad, dx, ids, 7)
+    with torch.no_grad():
+        again, _ = cel.attention(q, k, v, ptr)
+        assert torch.equal(again, out)
+        assert all(torch.equal(a, b) for a, b in zip(cel.attention_grad(g, q, k, v, out, lse, ptr), plain))
+        assert torch.equal(cel.embed(table, ids), rows) and torch.equal(cel.embed_grad(dx, ids, 7), dtable)
+
+
+def test_inside_a_function_of_torch():
+    """The two together as a differentiable operation, which a user makes of them."""
+
+    class Attention(torch.autograd.Function):
+        @staticmethod
+        def forward(ctx, q, k, v, ptr):
+            out, lse = cel.attention(q, k, v, ptr)
+            ctx.save_for_backward(q, k, v, ptr, out, lse)
+            return out
+
+        @staticmethod
+        def backward(ctx, dout):
+            q, k, v, ptr, out, lse = ctx.saved_tensors
+            return (*cel.attention_grad(dout, q, k, v, out, lse, ptr), None)
+
+    q, k, v, g, ptr = batch()
+    out, lse = cel.attention(q, k, v, ptr)
+    plain = cel.attention_grad(g, q, k, v, out, lse, ptr)
+    x = [t.clone().requires_grad_() for t in (q, k, v)]
+    Attention.apply(*x, ptr).backward(g)
+    assert all(torch.equal(t.grad, p) for t, p in zip(x, plain))
