@@ -716,7 +716,7 @@ def embed(table, ids, scale=1.0):
     of zeros. -> [tokens, hidden] in the table's type."""
     index = _device_of("embed", table=table, ids=ids)
     with _on(index):
-        a, table, ids = _embed("embed", "table", table, ids, table.shape[0], scale)
+        a, table, ids = _embed("embed", "table", table, ids, table.shape[0] if table.dim() else 0, scale)
         out = torch.empty((a.tokens, a.hidden), dtype=table.dtype, device=table.device)
         _check(lib().cel_embed(C.byref(a), table.data_ptr(), out.data_ptr(), _raw_stream(index)))
     return out

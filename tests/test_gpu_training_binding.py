@@ -71,3 +71,13 @@ def test_inside_a_function_of_torch():
     x = [t.clone().requires_grad_() for t in (q, k, v)]
     Attention.apply(*x, ptr).backward(g)
     assert all(torch.equal(t.grad, p) for t, p in zip(x, plain))
+
+
+def test_tensors_without_dimensions():
+    one, ids = torch.zeros((), device=DEV), torch.zeros(3, dtype=torch.int64, device=DEV)
+    q, k, v, g, ptr = batch()
+    refused(cel.embed, one, ids)
+    refused(cel.embed, torch.zeros(4, 8, device=DEV), ids[0])
+    refused(cel.embed_grad, one, ids, 4)
+    refused(cel.attention, one, one, one, ptr)
+    refused(cel.attention, q, k, v, ptr[0])
