@@ -539,9 +539,14 @@ def _device_of(fn, **tensors):
 
 def _view(t):
     """t [tokens, heads, dim] as the kernels read and write it, or None where its values are not
-    contiguous or its address or strides are off 16 bytes."""
+    contiguous or its address or strides are off 16 bytes.  A single token's and a single head's stride
+    is never taken, whatever it says."""
     row, head, one = t.stride()
     p = t.data_ptr()
+    if t.shape[0] == 1:
+        row = t.shape[2]
+    if t.shape[1] == 1:
+        head = 0
     if one != 1 or row & 7 or head & 7 or p & 15 or not t.shape[2] <= row <= 1 << 23:
         return None
     return _Rows(p, row, head)

@@ -81,3 +81,23 @@ def test_tensors_without_dimensions():
     refused(cel.embed_grad, one, ids, 4)
     refused(cel.attention, one, one, one, ptr)
     refused(cel.attention, q, k, v, ptr[0])
+
+
+@pytest.mark.parametrize("T,H,K", [(1, 4, 2), (40, 1, 1), (1, 1, 1)])
+def test_strides_that_are_never_taken(T, H, K):
+    """One token's or one head's, which torch leaves at anything, also of gradients written in place."""
+    x = batch(T, H, K)
+    q, k, v, g, ptr = x
+
+    def odd(t):
+        row, head, _ = t.stride()
+        row, head = row if T > 1 else 3, head if t.shape[1] > 1 else 5
+        return torch.zeros(2 * T * t.shape[1] * 64, dtype=t.dtype, device=DEV).as_strided(t.shape, (row, head, 1)).copy_(t)
+
+    out, lse = cel.attention(q, k, v, ptr)
+    plain = cel.attention_grad(g, q, k, v, out, lse, ptr)
+    into = [odd(torch.zeros_like(t)) for t in (q, k, v)]
+    again, lse2 = cel.attention(odd(q), odd(k), odd(v), ptr)
+    assert torch.equal(again, out) and torch.equal(lse2, lse)
+    got = cel.attention_grad(odd(g), odd(q), odd(k), odd(v), odd(out), lse, ptr, grads=into)
+    assert all(a is b for a, b in zip(got, into)) and all(torch.equal(a, b) for a, b in zip(got, plain))
