@@ -358,7 +358,7 @@ typedef struct {
                                   * with the gradient 2^30 (2^24 - 1 tiles of 128 tokens of a head, or of 64) */
   int32_t heads, kv_heads, dim;  /* heads a multiple of kv_heads: query head h reads key/value
                                   * head h / (heads / kv_heads); dim 8, 16, ... 128 */
-  float scale;                   /* of the scores, > 0 (usually 1 / sqrt(dim)) */
+  float scale;                   /* of the scores, 10^-37 .. 2 * 10^38 (usually 1 / sqrt(dim)) */
   const int32_t *seq_ptr;
   cel_rows q, k, v;              /* q: heads; k, v: kv_heads; read-only */
 } cel_attn;

@@ -1107,8 +1107,9 @@ int check_attn(const cel_attn *a, const char *fn) {
     return set_error(CEL_E_ARG, "%s: %d heads over %d key/value heads", fn, a->heads, a->kv_heads);
   if (a->dim < 8 || a->dim > 128 || a->dim % 8)
     return set_error(CEL_E_ARG, "%s: dim %d is not a multiple of 8 in 8..128", fn, a->dim);
-  if (!(a->scale > 0.f) || !std::isfinite(a->scale) || !std::isfinite(8.f / (a->scale * kLog2e)))
-    return set_error(CEL_E_ARG, "%s: scale %g is not positive and finite", fn, (double)a->scale);
+  const float c = a->scale * kLog2e;  // of the exponents, to the base of 2
+  if (!(c > 0.f) || !std::isfinite(c) || !std::isfinite(8.f / c))
+    return set_error(CEL_E_ARG, "%s: scale %g is not positive and finite, in units of log 2 too", fn, (double)a->scale);
   return check_grid(a, kBlock, fn);  // the forward pass's and dq's launch
 }
 // Into how many workgroups a tile of keys deals out the query heads that share

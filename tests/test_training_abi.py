@@ -131,3 +131,12 @@ def test_attention_launches_stay_below_what_a_grid_takes(lib):
         if forward:
             assert lib.cel_attention(ctypes.byref(a), r, p, None) == ARG
     assert lib.cel_attention_grad_scratch(ctypes.byref(attn(tokens=2 ** 24 - 64, heads=64, kv_heads=64))) > 0
+
+
+@pytest.mark.parametrize("scale", [3e38, 2.5e38, 1e-38, 1e-45])
+def test_attention_scales_that_exponents_do_not_hold(lib, scale):
+    """log2(e) times the scale, or 8 over it, is not finite in 32 bits."""
+    a, r, p = attn(scale=scale), ctypes.byref(rows()), ctypes.c_void_p(SOME)
+    assert lib.cel_attention_grad_scratch(ctypes.byref(a)) == ARG
+    assert lib.cel_attention(ctypes.byref(a), r, p, None) == ARG
+    assert lib.cel_attention_grad(ctypes.byref(a), r, p, r, p, r, r, r, None) == ARG
