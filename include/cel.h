@@ -434,6 +434,7 @@ int64_t cel_embed_grad_scratch(int64_t tokens, int64_t vocab, int64_t hidden);
  * completes.  cel_kernel_stats writes one line per kernel, "name launches
  * total_ms\n", into buf (NUL-terminated, truncated to buflen), returns the
  * number of kernels listed, and clears the totals when reset != 0.
+ * Launches that are being captured into a graph are not timed.
  * cel_timing returns the previous setting. */
 int cel_timing(int enable);
 int cel_kernel_stats(char *buf, int buflen, int reset);

@@ -59,6 +59,14 @@ void collect_locked() {
 
 KTimer::KTimer(hipStream_t s, const char *name) : s_(s), name_(name) {
   if (!g_timing.load(std::memory_order_relaxed)) return;
+  // An event recorded into a graph has no time, and asking for it is an error
+  // that a later call would report.
+  hipStreamCaptureStatus capture = hipStreamCaptureStatusNone;
+  if (hipStreamIsCapturing(s, &capture) != hipSuccess) {
+    (void)hipGetLastError();
+    return;
+  }
+  if (capture != hipStreamCaptureStatusNone) return;
   std::lock_guard<std::mutex> lk(g_mu);
   a_ = take_event();
   b_ = take_event();

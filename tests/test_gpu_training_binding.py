@@ -101,3 +101,34 @@ def test_strides_that_are_never_taken(T, H, K):
     assert torch.equal(again, out) and torch.equal(lse2, lse)
     got = cel.attention_grad(odd(g), odd(q), odd(k), odd(v), odd(out), lse, ptr, grads=into)
     assert all(a is b for a, b in zip(got, into)) and all(torch.equal(a, b) for a, b in zip(got, plain))
+
+
+def test_timing_and_capture():
+    """Launches that become part of a graph are not timed, and leave no error to a later call."""
+    q, k, v, g, ptr = batch()
+    ids, table = torch.arange(5, device=DEV), torch.randn(7, 16, device=DEV)
+
+    def step():
+        out, lse = cel.attention(q, k, v, ptr)
+        return (out, lse, *cel.attention_grad(g, q, k, v, out, lse, ptr), cel.embed(table, ids))
+
+    plain = step()
+    torch.cuda.synchronize()
+    before = cel.timing(True)
+    try:
+        cel.kernel_stats(reset=True)
+        graph = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(graph):
+            held = step()
+        assert cel.kernel_stats() == {}
+        for _ in range(3):
+            for t in held:
+                t.zero_()
+            graph.replay()
+            torch.cuda.synchronize()
+            assert all(torch.equal(a, b) for a, b in zip(held, plain))
+            assert all(torch.equal(a, b) for a, b in zip(step(), plain))
+        stats = cel.kernel_stats(reset=True)
+        assert stats["k_attention"][0] == 3 and stats["k_embed"][0] == 3
+    finally:
+        cel.timing(before)
