@@ -530,11 +530,12 @@ __device__ __forceinline__ bool attention_tile(const AttnArgs &A, char *s_k0, ch
         for (int r = 0; r < 16; r++) top = fmaxf(top, s[t][r]);
       top = half_max(top);
       // The reference m of the exponents follows the maximum only once that is
-      // 2^8 above it: p stays below 2^8, and the sums are seldom rescaled.
-      if (__any(top > m + far)) {
-        const float to = fmaxf(m, top);
-        const float by = to == -INFINITY ? 1.f : exp2_((m - to) * c);
-        m = to;
+      // 2^8 above it: p stays below 2^8, and the sums are seldom rescaled.  Each row's own
+      // maximum decides, so that a row's bits do not hang on its neighbours'.
+      const bool above = top > m + far;
+      if (__any(above)) {
+        const float by = above ? exp2_((m - top) * c) : 1.f;
+        m = above ? top : m;
         mc = m == -INFINITY ? 0.f : m * c;
         l *= by;
 #pragma unroll

@@ -156,3 +156,33 @@ def test_padding_may_hold_anything(dtype, d, lengths, H, K):
         t[first + sum(lengths):] = float("inf")
     for n, got in run(*x, ptr).items():
         assert torch.equal(got, plain[n]), n
+
+
+@pytest.mark.parametrize("lengths,H,K", BATCHES)
+@pytest.mark.parametrize("d,dtype", [(64, torch.bfloat16), (128, torch.float16)])
+@pytest.mark.parametrize("by", [30.0, -30.0, 0.0])
+def test_a_row_does_not_hang_on_its_neighbours(by, d, dtype, lengths, H, K):
+    """Other tokens' queries and gradients, and later tokens' keys and values, change no bit of a row, also
+    where their scores are large."""
+    T, at = sum(lengths), lengths[0] + 97
+    q, k, v, g = batch(T, H, K, d, dtype, 3 * d + T)
+    ptr = ptr_of(lengths)
+    plain = run(q, k, v, g, ptr)
+    others = (torch.arange(T) % 7 != 3).to(DEV)
+    q2, g2 = q.clone(), g.clone()
+    q2[~others.cpu()] *= by
+    g2[~others.cpu()] *= by
+    got = run(q2, k, v, g2, ptr)
+    for n in ("out", "dq"):
+        assert torch.equal(got[n][others], plain[n][others]), n
+    assert torch.equal(got["lse"][:, others], plain["lse"][:, others])
+    k2, v2 = k.clone(), v.clone()
+    k2[at:at + 3] *= by
+    v2[at:at + 3] *= by
+    got = run(q, k2, v2, g, ptr)
+    before = slice(0, at)
+    assert torch.equal(got["out"][before], plain["out"][before]) and torch.equal(got["dq"][before], plain["dq"][before])
+    assert torch.equal(got["lse"][:, before], plain["lse"][:, before])
+    end = lengths[0] + lengths[1]
+    for n in ("out", "dq", "dk", "dv"):
+        assert torch.equal(got[n][end:], plain[n][end:]), n
