@@ -65,7 +65,8 @@ class Recorder:
             self.made[id(t)] = (t, at)
 
     def workload(self, devices, bandwidth, latency):
-        """The step as the library takes it: times in ns, bytes, devices with a third of all memory each."""
+        """The step as the library takes it: times in ns, bytes, devices that hold two thirds of all
+        memory each (where there are two, all of it, and a single one twice that)."""
         cap = np.full(devices, 2 * sum(self.bytes) // max(1, min(devices, 3)), np.int64)
         return from_edges(len(self.names), self.edges, self.times, self.bytes, devices, cap, bandwidth, latency,
                           name="measured")

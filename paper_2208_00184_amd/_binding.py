@@ -542,12 +542,13 @@ def _view(t):
     contiguous or its address or strides are off 16 bytes.  A single token's and a single head's stride
     is never taken, whatever it says."""
     row, head, one = t.stride()
+    T, H, d = t.shape
     p = t.data_ptr()
-    if t.shape[0] == 1:
-        row = t.shape[2]
-    if t.shape[1] == 1:
+    if T == 1:
+        row = d
+    if H == 1:
         head = 0
-    if one != 1 or row & 7 or head & 7 or p & 15 or not t.shape[2] <= row <= 1 << 23:
+    if one != 1 or row & 7 or head & 7 or p & 15 or not d <= row <= 1 << 23:
         return None
     return _Rows(p, row, head)
 
@@ -573,6 +574,8 @@ def _block(x, T, H, d):
 
 def _folded(x, T, d):
     """Whether elements of a block share memory."""
+    if x[2] >= (x[4] - 1) * x[3] + d and (x[3] >= d or x[4] == 1):
+        return False  # heads side by side, rows one behind the other
     (lo, n), (hi, m) = sorted([(s, k) for s, k in ((x[3], x[4]), (x[2], T)) if k > 1] + [(1 << 62, 1)] * 2)[:2]
     if n == 1:
         return False
@@ -633,8 +636,9 @@ def attention(q, k, v, seq_ptr, scale=None):
     """Causal attention over a packed batch: sequence s is the tokens seq_ptr[s] ..
     seq_ptr[s + 1] - 1 (int32, on the device), a token sees itself and the earlier tokens of its
     sequence.  q [T, heads, dim], k and v [T, kv_heads, dim] in bfloat16 or float16, any strides
-    (views of a fused projection are read in place); heads a multiple of kv_heads, dim a multiple
-    of 8 up to 128; scale: of the scores, 1 / sqrt(dim) by default.
+    (views of a fused projection are read in place; where a head's values are not contiguous, or an
+    address or stride is no multiple of 16 bytes, the call copies the tensor); heads a multiple of
+    kv_heads, dim a multiple of 8 up to 128; scale: of the scores, 1 / sqrt(dim) by default.
     -> (out [T, heads, dim], lse float32 [heads, T]); tokens of no sequence have 0 and -inf."""
     index = _device_of("attention", q=q, k=k, v=v, seq_ptr=seq_ptr)
     with _on(index):
@@ -718,7 +722,8 @@ def _embed(fn, what, rows, ids, vocab, scale):
 def embed(table, ids, scale=1.0):
     """scale * table[ids]: rows of table [vocab, hidden] (bfloat16, float16 or float32, rows any
     stride apart) by token id (int32 or int64 [tokens]); an id outside [0, vocab) is padding, a row
-    of zeros. -> [tokens, hidden] in the table's type."""
+    of zeros. -> [tokens, hidden] in the table's type.  A table whose rows' values are not contiguous
+    (a transposed one) or overlap (an expanded one) is copied whole by every call."""
     index = _device_of("embed", table=table, ids=ids)
     with _on(index):
         a, table, ids = _embed("embed", "table", table, ids, table.shape[0] if table.dim() else 0, scale)
@@ -731,7 +736,7 @@ def embed_grad(dx, ids, vocab, scale=1.0, dtype=None):
     """The gradient of embed()'s table at dx [tokens, hidden], the gradient of its rows: a dense
     [vocab, hidden] in `dtype` (dx's by default, or float32), zeros for words that do not occur.
     The tokens are sorted by id and added in 32 bits in a fixed order: the same inputs give the
-    same bits."""
+    same bits.  A dx whose rows' values are not contiguous or overlap is copied by the call."""
     fn = "embed_grad"
     index = _device_of(fn, dx=dx, ids=ids)
     with _on(index):

@@ -85,7 +85,7 @@ __device__ inline u32x4 operand(const acc16 &x, int j) {
 // of smaller ones is 2^-33 of the largest.  p of dv takes a constant 2^kPUp: at most 1, it
 // leaves room for what lse's own rounding makes it too large where scores are in the millions.
 // The largest entry is looked for in every step, 4 % of the gradient's time (9,973 tokens in 37
-// sequences, 24 heads of 80 over 4, with the forward pass: 383 -> 399 us).  Without all this
+// sequences, 24 heads of 80 over 4: dk and dv 156 -> 164 us, dq 123 -> 126).  Without all this
 // dq of one sequence of 4,096 at a dout of 2^-12 was off by 6.8e-3 where its results' own rounding is 1.2e-3.
 template <class T>
 constexpr bool kScaled = __is_same(T, _Float16);
@@ -457,9 +457,7 @@ __device__ __forceinline__ void rows_products(acc16 &x, const char *lds, int t, 
                  else x = Half<T>::mma(z, f[n / 2], n > 1 ? x : acc16{});
                });
 }
-// x's entries at 32 t .. of a tile outside lo .. hi, replaced.  The empty
-// statement hides where the bounds come from: they are compared with constants, not
-// with 16 numbers of each lane's that would stay in registers across the loop.
+// x's entries at 32 t .. of a tile outside lo .. hi, replaced.
 __device__ __forceinline__ void mask(acc16 &x, int t, int lo, int hi, float by, int lane) {
 #pragma unroll
   for (int r = 0; r < 16; r++) {
@@ -475,9 +473,9 @@ __device__ __forceinline__ void mask(acc16 &x, int t, int lo, int hi, float by, 
 // vector unit, which two waves on a SIMD overlap.  A tile of 128 rows reads each
 // staged key and value four times from LDS, which then gives what the products
 // take; more rows would not fit two waves' registers.  16,384 tokens in one sequence,
-// 16 heads of 128 over 4: 1.04 ms, 1.06 PFLOP/s, where a large library product
+// 16 heads of 128 over 4: 0.98 ms, 1.12 PFLOP/s, where a large library product
 // reaches 1.36 and this kernel without its softmax 1.25; 8,192 tokens, 32 heads
-// over 8: 0.53 ms, 1.04 PFLOP/s, matrix cores 56 % busy, no bank conflicts.
+// over 8: 0.51 ms, 1.08 PFLOP/s, matrix cores 55 % busy, no bank conflicts.
 // 4 sequences of 1,024, 16 heads of 64: 23 us, the 16 steps of a sequence's last
 // tile (0.8 us each at 64 dimensions, 1.1 at 128) behind some 7 us of start and end.
 template <class T, int DP, int DC, int G, bool CAREFUL>
@@ -606,9 +604,11 @@ __device__ __forceinline__ bool attention_tile(const AttnArgs &A, char *s_k0, ch
 }
 
 // A workgroup runs its tile without regard to infinities and NaN, and where
-// the result has any, all of it again with: nothing of the first run is kept in
-// registers for the second, which takes 32 dimensions at a time, so that it
-// needs fewer than the first.
+// the result has any, all of it again with.  The second run takes 32 dimensions at a
+// time, so that its own sums need few registers, but what both make from the lane's number
+// stays in registers across the first: at 128 dimensions dq spills 104 registers, none inside
+// its loop, and waits for each of its rows' first loads before the next; the forward
+// kernel spills 2.
 // G = 2: two groups of waves share the rows and take their keys' tiles in turn,
 // each with buffers of its own, and join their sums at the end.  A tile's chain of
 // steps, each of which waits for the one before, is then half as long, with the
@@ -626,13 +626,13 @@ __device__ __forceinline__ bool attention_tile(const AttnArgs &A, char *s_k0, ch
 CEL_TILE_KERNEL(k_attention, attention_tile, s_k0, s_k1, s_v0, s_v1)
 
 // dq of a tile of 128 tokens of one query head; leaves lse_i and D_i in rows
-// for k_attention_dkv.  D_i is <do_i, o_i> with the rounded o_i, except where a
-// wave's keys all lie in one tile: there, where o_i is large (few values
+// for k_attention_dkv.  D_i is <do_i, o_i> with the rounded o_i, except where the
+// keys of all of a wave's rows lie in one tile: there, where o_i is large (few values
 // averaged) and its rounding would weigh as much as that of ds, it is the sum of
 // p_ij <do_i, v_j> in 32 bits, at the price of that tile's products twice.
 // Tiles and bounds are the forward pass's, with three products a step and 32 keys'
 // scores in registers at a time: 8,192 tokens in one sequence, 32 heads of 128 over
-// 8: 0.75 ms, 1.10 PFLOP/s, matrix cores 61 % busy.  dq has a kernel of its own since
+// 8: 0.72 ms, 1.15 PFLOP/s, matrix cores 60 % busy.  dq has a kernel of its own since
 // its sums run over the other axis than dk's and dv's: joined, one side would be
 // added up in memory, by atomics in no fixed order.  The price is that scores and
 // their gradients are made twice, 7 products where 5 would do.
@@ -825,8 +825,8 @@ __device__ inline void heads_of(const AttnArgs &A, int kvh, int part, int &first
 // and operands take half the registers that 32 keys would, so that two waves
 // share a SIMD and every product is made once; the reads of LDS a product are
 // twice as many, 256 bytes a cycle at the matrix cores' full rate, which is what
-// LDS gives.  8,192 tokens in one sequence, 32 heads of 128 over 8: 1.12 ms for four
-// products, 0.99 PFLOP/s, matrix cores 49 % busy (32 keys a wave and a launch each for
+// LDS gives.  8,192 tokens in one sequence, 32 heads of 128 over 8: 1.07 ms for four
+// products, 1.03 PFLOP/s, matrix cores 49 % busy (32 keys a wave and a launch each for
 // dk and dv, five products: 1.55 ms; pairs of waves that hand p over in LDS: 1.62 ms).
 //   A result tile D[m][n] puts column n = lane % 16 and rows 4 (lane / 16) + r in
 //   register r; two of them are a right operand of 32 rows, in the order
@@ -983,7 +983,9 @@ __device__ __forceinline__ bool dkv_tile(const AttnArgs &A, char *s_q0, char *s_
         }
       if (masked) {
         int from = lo - g4, to = hi - g4;
-        asm volatile("" : "+v"(from), "+v"(to));  // as in mask
+        // hides where the bounds come from: they are compared with constants, not
+        // with 16 numbers of each lane's that would stay in registers across the loop
+        asm volatile("" : "+v"(from), "+v"(to));
 #pragma unroll
         for (int t = 0; t < 4; t++)
 #pragma unroll
@@ -1144,7 +1146,10 @@ AttnArgs args_of(const cel_attn *a) {
 // to be won back.  One head of 64 over a sequence of 2,048 tokens: forward
 // 33.0 -> 26.7 us, dq 41.9 -> 35.2; of 128: forward 45.3 -> 36.1; 8 heads of 64 over 4,096:
 // 57.5 -> 45.2 and 73.1 -> 59.4; but at 512 workgroups (4 sequences of 1,024, 16 heads of
-// 64) 23.9 -> 32.3 and 31.6 -> 43.6, and at 64 tokens 7.4 -> 8.6.
+// 64) 23.9 -> 32.3 and 31.6 -> 43.6, and at 64 tokens 7.4 -> 8.6.  The tokens are the batch's: how
+// long its sequences are only the device knows.  Where all are short the second group
+// has nothing to do and costs up to 1.4 us (8 heads of 64, 16 sequences of 128: forward 10.2 -> 10.6,
+// dq 13.0 -> 14.2; 600 of 1: 10.6 -> 10.7 and 14.4 -> 15.0; 4 of 512: 14.7 -> 13.7 and 18.0 -> 18.1).
 bool split_keys(const AttnArgs &A) { return (int64_t)A.tiles * A.H <= 256 && A.T >= 512; }
 
 // kernel<T, DP, DC, ...> for the call's type and dimension: rows are staged DP

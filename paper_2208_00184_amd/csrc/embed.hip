@@ -377,7 +377,8 @@ __global__ void __launch_bounds__(256) k_embed_parts(const uint32_t *__restrict_
 // rows of 64, 8,192 tokens: 24 -> 14 us, 32,768 tokens 50 -> 35; at 16,000 pieces the two are within
 // 7 % of each other), else kRowsAt (131,072 rows of 8,192: 607 us one by one, 480 so).  Bound by memory:
 // 131,072 rows of 8,192 from 32,768 tokens, 16 bits: 480 us, 2.5 GB at 5.2 TB/s; 50,001 rows
-// of 1,024 in 32 bits from 4,096: 32 to 43 us (205 MB written).  Eight rows of dx on their way
+// of 1,024 in 32 bits from 4,096: 32 us into memory that was written just before, 10 us more
+// into other (205 MB, of which the memory-side cache may hold the one).  Eight rows of dx on their way
 // instead of four take more registers and leave fewer waves: 724 us for the first.
 template <class T, class O, bool NT>
 __global__ void __launch_bounds__(256) k_embed_grad(const uint32_t *start, const uint32_t *__restrict__ order, int64_t vocab,
