@@ -380,8 +380,8 @@ int cel_attention(const cel_attn *a, const cel_rows *out, float *lse, hipStream_
  *   dq_i = scale sum_j ds_ij k_j;  dk_j = scale sum_i ds_ij q_i;  dv_j = sum_i p_ij dout_i
  * p and ds are rounded to the rows' type as matrix operands, in float16 times powers of two
  * of each row's or key's own, so that results are as exact at a small or large dout as at
- * any, as far as float16 holds the results; D = <dout_i, out_i> is taken from the rounded out (but where the keys
- * of 32 neighbouring tokens lie within 64); sums are 32 bit.
+ * any, as far as float16 holds the results; D = <dout_i, out_i> is taken from the rounded out, but for
+ * rows whose keys lie in one of the tiles of 64 that the kernel takes them by, where it is a sum of its own; sums are 32 bit.
  * dk and dv sum over the query heads of their key/value head, in a fixed
  * order: the same inputs give the same bits.  A token of no sequence has
  * gradients of 0.  scratch: cel_attention_grad_scratch(a)

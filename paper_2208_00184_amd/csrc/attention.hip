@@ -473,9 +473,9 @@ __device__ __forceinline__ void mask(acc16 &x, int t, int lo, int hi, float by, 
 // vector unit, which two waves on a SIMD overlap.  A tile of 128 rows reads each
 // staged key and value four times from LDS, which then gives what the products
 // take; more rows would not fit two waves' registers.  16,384 tokens in one sequence,
-// 16 heads of 128 over 4: 0.98 ms, 1.12 PFLOP/s, where a large library product
+// 16 heads of 128 over 4: 1.01 ms, 1.09 PFLOP/s, where a large library product
 // reaches 1.36 and this kernel without its softmax 1.25; 8,192 tokens, 32 heads
-// over 8: 0.51 ms, 1.08 PFLOP/s, matrix cores 55 % busy, no bank conflicts.
+// over 8: 0.51 ms, 1.07 PFLOP/s, matrix cores 55 % busy, no bank conflicts.
 // 4 sequences of 1,024, 16 heads of 64: 23 us, the 16 steps of a sequence's last
 // tile (0.8 us each at 64 dimensions, 1.1 at 128) behind some 7 us of start and end.
 template <class T, int DP, int DC, int G, bool CAREFUL>
@@ -606,9 +606,9 @@ __device__ __forceinline__ bool attention_tile(const AttnArgs &A, char *s_k0, ch
 // A workgroup runs its tile without regard to infinities and NaN, and where
 // the result has any, all of it again with.  The second run takes 32 dimensions at a
 // time, so that its own sums need few registers, but what both make from the lane's number
-// stays in registers across the first: at 128 dimensions dq spills 104 registers, none inside
-// its loop, and waits for each of its rows' first loads before the next; the forward
-// kernel spills 2.
+// stays in registers across the first: at 128 dimensions dq spills 36 registers (20 in float16), most of
+// them outside its loop, and so does not have all of its rows' first loads on their way at once; the
+// forward kernel spills 2.
 // G = 2: two groups of waves share the rows and take their keys' tiles in turn,
 // each with buffers of its own, and join their sums at the end.  A tile's chain of
 // steps, each of which waits for the one before, is then half as long, with the
@@ -626,13 +626,15 @@ __device__ __forceinline__ bool attention_tile(const AttnArgs &A, char *s_k0, ch
 CEL_TILE_KERNEL(k_attention, attention_tile, s_k0, s_k1, s_v0, s_v1)
 
 // dq of a tile of 128 tokens of one query head; leaves lse_i and D_i in rows
-// for k_attention_dkv.  D_i is <do_i, o_i> with the rounded o_i, except where the
-// keys of all of a wave's rows lie in one tile: there, where o_i is large (few values
+// for k_attention_dkv.  D_i is <do_i, o_i> with the rounded o_i, except where a
+// row's keys all lie in one tile: there, where o_i is large (few values
 // averaged) and its rounding would weigh as much as that of ds, it is the sum of
-// p_ij <do_i, v_j> in 32 bits, at the price of that tile's products twice.
+// p_ij <do_i, v_j> in 32 bits, at the price of a wave's products twice on the tiles
+// that hold such a row.  Those reach the wave's own rows, and only there is it looked for: looked for
+// everywhere, 8,192 tokens took 4 % longer.
 // Tiles and bounds are the forward pass's, with three products a step and 32 keys'
 // scores in registers at a time: 8,192 tokens in one sequence, 32 heads of 128 over
-// 8: 0.72 ms, 1.15 PFLOP/s, matrix cores 60 % busy.  dq has a kernel of its own since
+// 8: 0.70 ms, 1.17 PFLOP/s, matrix cores 65 % busy.  dq has a kernel of its own since
 // its sums run over the other axis than dk's and dv's: joined, one side would be
 // added up in memory, by atomics in no fixed order.  The price is that scores and
 // their gradients are made twice, 7 products where 5 would do.
@@ -645,7 +647,7 @@ __device__ __forceinline__ bool dq_tile(const AttnArgs &A, char *s_k0, char *s_k
   const int group = G > 1 ? __builtin_amdgcn_readfirstlane(threadIdx.x / (kWaves * 64)) : 0;
   const Item item = item_of(blockIdx.x, gridDim.x, A.H);
   const int head = item.unit, tile = A.tiles - 1 - item.tile, kvh = head / (A.H / A.K);
-  const int i = tile * kBlock + wave * kRows + (lane & 31);
+  const int first = tile * kBlock + wave * kRows, i = first + (lane & 31);
   const Reach R = reach_of(A, i, true, s_reach + 2 * group, wave);
   u32x4 q[DC / 16], g[DC / 16];
   load_rows(q, A.q, head, i, A.T, A.d, lane);
@@ -684,8 +686,10 @@ __device__ __forceinline__ bool dq_tile(const AttnArgs &A, char *s_k0, char *s_k
       const char *s_k = (buf.at ? s_k1 : s_k0) + group * kTile, *s_v = (buf.at ? s_v1 : s_v0) + group * kTile;
       const bool masked = R.masks(a);
       const int lo = R.lo - a, hi = R.hi - a;
-      if (R.any_lo >= a && R.any_hi < a + kStep) {
-        D = 0.f;
+      // All of a row's keys, of which it is itself the last: not in tiles before the wave's own rows.
+      const bool inside = a + kStep > first && R.real() && lo >= 0 && hi < kStep;
+      if (a + kStep > first && __any(inside)) {
+        float sum = 0.f;
 #pragma unroll
         for (int t = 0; t < 2; t++) {
           acc16 s, dp;
@@ -694,9 +698,10 @@ __device__ __forceinline__ bool dq_tile(const AttnArgs &A, char *s_k0, char *s_k
           for (int r = 0; r < 16; r++) s[r] = exp2_(fmaf(s[r], c, -lse2)) * dp[r];
           mask(s, t, lo, hi, 0.f, lane);
 #pragma unroll
-          for (int r = 0; r < 16; r++) D += s[r];
+          for (int r = 0; r < 16; r++) sum += s[r];
         }
-        D = half_sum(D);
+        sum = half_sum(sum);
+        D = inside ? sum : D;
       }
 #pragma unroll
       for (int t = 0; t < 2; t++) {
@@ -748,8 +753,8 @@ __device__ __forceinline__ bool dq_tile(const AttnArgs &A, char *s_k0, char *s_k
         for (int n = 0; n < NB; n++)
 #pragma unroll
           for (int r = 0; r < 16; r++) dq[n][r] = dq[n][r] * back + theirs[(16 * n + r) * 64];
-        const int t = (R.any_lo - R.from) / kStep;  // the tile with all of the wave's keys, if there is one
-        if (R.any_lo <= R.any_hi && (R.any_hi - R.from) / kStep == t && t & 1) D = *their_D;
+        const int t = (R.lo - R.from) / kStep;  // the tile with all of the row's keys, if there is one
+        if (R.real() && (R.hi - R.from) / kStep == t && t & 1) D = *their_D;
       }
     }
     if (i < A.T && group == 0) {
@@ -826,7 +831,7 @@ __device__ inline void heads_of(const AttnArgs &A, int kvh, int part, int &first
 // share a SIMD and every product is made once; the reads of LDS a product are
 // twice as many, 256 bytes a cycle at the matrix cores' full rate, which is what
 // LDS gives.  8,192 tokens in one sequence, 32 heads of 128 over 8: 1.07 ms for four
-// products, 1.03 PFLOP/s, matrix cores 49 % busy (32 keys a wave and a launch each for
+// products, 1.02 PFLOP/s, matrix cores 49 % busy (32 keys a wave and a launch each for
 // dk and dv, five products: 1.55 ms; pairs of waves that hand p over in LDS: 1.62 ms).
 //   A result tile D[m][n] puts column n = lane % 16 and rows 4 (lane / 16) + r in
 //   register r; two of them are a right operand of 32 rows, in the order

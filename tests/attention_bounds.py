@@ -29,8 +29,9 @@ def _norm(x, dim):
     return x.square().sum(dim).sqrt()
 
 
-def definition(q, k, v, dout, lengths, first=0, scale=None):
-    """-> {name: (value, bound)} for out, lse, dq, dk, dv, on the CPU in 64 bits."""
+def definition(q, k, v, dout, lengths, first=0, scale=None, wide=None):
+    """-> {name: (value, bound)} for out, lse, dq, dk, dv, on the CPU in 64 bits.  wide: the tokens
+    [T] whose D is a sum in 32 bits and carries no rounding of out (none by default)."""
     dtype, u = q.dtype, UNIT[q.dtype]
     half = dtype == torch.float16
     q, k, v, dout = (x.double().cpu() for x in (q, k, v, dout))
@@ -76,10 +77,12 @@ def definition(q, k, v, dout, lengths, first=0, scale=None):
         dp = G @ V.transpose(1, 2)
         dp_sizes = G.abs() @ V.abs().transpose(1, 2)
         D = (G * o).sum(2, keepdim=True)
-        e_D = 6 * u * (_norm(p * dp, 2)[..., None] + _norm(G * o, 2)[..., None])
-        e_D = e_D + w * ((p * dp_sizes).sum(2, keepdim=True)) + (least * G.abs()).sum(2, keepdim=True)
+        e_D = 6 * u * (_norm(p * dp, 2)[..., None] + _norm(G * o, 2)[..., None]) + (least * G.abs()).sum(2, keepdim=True)
         if half:
             e_D = e_D + (2.0 ** -25 * p.amax(2, keepdim=True) * (seen * dp_sizes).sum(2, keepdim=True))
+        if wide is not None:
+            e_D = e_D * ~wide[r, None]
+        e_D = e_D + (w + r32) * ((p * dp_sizes).sum(2, keepdim=True))
         ds = p * (dp - D)
         e_32 = p * ((w + r32) * dp_sizes + w * D.abs())
         tp, tds, t32 = p.transpose(1, 2), ds.transpose(1, 2), e_32.transpose(1, 2)

@@ -186,3 +186,29 @@ def test_a_row_does_not_hang_on_its_neighbours(by, d, dtype, lengths, H, K):
     end = lengths[0] + lengths[1]
     for n in ("out", "dq", "dk", "dv"):
         assert torch.equal(got[n][end:], plain[n][end:]), n
+
+
+@pytest.mark.parametrize("lengths", [[90, 20, 10], [30, 34, 40, 24], [128], [70, 1, 2, 3, 4, 5, 6, 7], [64, 64], [60, 3, 1, 50]])
+@pytest.mark.parametrize("H,K,d", [(2, 1, 64), (3, 3, 128), (4, 2, 80)])
+@pytest.mark.parametrize("more", [0, 600])
+@pytest.mark.parametrize("dtype", TYPES)
+def test_rows_of_few_keys(dtype, more, H, K, d, lengths):
+    """D of a row whose keys lie in one tile of 64 is a sum in 32 bits: where few values are averaged out is
+    as large as they are, and its rounding would weigh as much as all else.  Within one block of 128 tokens
+    the tiles are the tokens 0 to 63 and 64 to 127; `more` others in front make a block of their own."""
+    assert sum(lengths) <= 128
+    ends = np.cumsum(lengths)
+    starts = ends - lengths
+    wide = torch.zeros(more + 128, dtype=torch.bool)
+    for a, b in zip(starts, ends):
+        for t in range(a, b):
+            wide[more + int(t)] = int(a) // 64 == int(t) // 64
+    before = [more] if more else []
+    # the block of 128 tokens has to begin with its sequences
+    first = -more % 128
+    T = first + more + 128
+    q, k, v, g = batch(T, H, K, d, dtype, d + more + len(lengths))
+    expected = definition(q, k, v, g, before + lengths, first, wide=torch.cat([torch.zeros(first, dtype=torch.bool), wide]))
+    got = run(q, k, v, g, ptr_of(before + lengths, first))
+    bad = {n: outside(expected, n, x) for n, x in got.items()}
+    assert not any(n for n, _ in bad.values()), bad
