@@ -354,8 +354,8 @@ typedef struct {
  * results, without an access outside the arrays. */
 typedef struct {
   int32_t type;                  /* of all rows: CEL_BF16 or CEL_F16 */
-  int32_t tokens, n_seq;         /* >= 0; tokens < 2^31 - 4096, tokens * heads below about 2^31,
-                                  * with the gradient 2^30 (2^24 - 1 tiles of 128 tokens of a head, or of 64) */
+  int32_t tokens, n_seq;         /* >= 0; heads times tokens / 128, rounded up, below 2^24; with
+                                  * the gradient tokens / 64 */
   int32_t heads, kv_heads, dim;  /* heads a multiple of kv_heads: query head h reads key/value
                                   * head h / (heads / kv_heads); dim 8, 16, ... 128 */
   float scale;                   /* of the scores, 10^-37 .. 2 * 10^38 (usually 1 / sqrt(dim)) */
@@ -378,10 +378,11 @@ int cel_attention(const cel_attn *a, const cel_rows *out, float *lse, hipStream_
  * that call gave them for the same descriptor.  With p_ij = exp(s_ij - lse_i)
  * and ds_ij = p_ij (<dout_i, v_j> - <dout_i, out_i>):
  *   dq_i = scale sum_j ds_ij k_j;  dk_j = scale sum_i ds_ij q_i;  dv_j = sum_i p_ij dout_i
- * p and ds are rounded to the rows' type as matrix operands, in float16 times powers of two
- * of each row's or key's own, so that results are as exact at a small or large dout as at
- * any, as far as float16 holds the results; D = <dout_i, out_i> is taken from the rounded out, but for
- * rows whose keys lie in one of the tiles of 64 that the kernel takes them by, where it is a sum of its own; sums are 32 bit.
+ * p and ds are rounded to the rows' type as matrix operands, in float16 times
+ * powers of two of each row's or key's own: results are as exact at a small or
+ * a large dout as at any, as far as float16 holds them.  <dout_i, out_i> is
+ * taken from the rounded out, except for rows whose keys lie in one of the
+ * tiles of 64 that the kernel takes them by.  Sums are 32 bit.
  * dk and dv sum over the query heads of their key/value head, in a fixed
  * order: the same inputs give the same bits.  A token of no sequence has
  * gradients of 0.  scratch: cel_attention_grad_scratch(a)
