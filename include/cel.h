@@ -20,6 +20,9 @@
  *
  *   cel_attention, cel_attention_grad  causal attention over a packed batch
  *   cel_embed, cel_embed_grad          embedding lookup, gradient by sorted tokens
+ *   cel_rotary, cel_rotary_grad        rotary positions of one axis or several
+ *   cel_dropout                        dropout without a stored mask
+ *   cel_residual_norm, cel_residual_norm_grad  norms, gate and residual stream between blocks
  *
  * Conventions (all entry points):
  *  - Arrays are DEVICE pointers owned by the caller unless marked (host).  The
@@ -428,6 +431,131 @@ int cel_embed_grad(const cel_embed_args *a, const void *dx, void *scratch, int32
 
 /* Bytes of scratch that cel_embed_grad takes, or CEL_E_ARG. */
 int64_t cel_embed_grad_scratch(int64_t tokens, int64_t vocab, int64_t hidden);
+
+/* Rotary positions.  Pair p of a head's dimensions turns by the angle
+ *   a = positions[axes[p]][t] * freqs[p]
+ * made and reduced to a part of a turn in 64 bits (positions of up to 2^53
+ * either way), its sine and cosine in 32:
+ *   u' = u cos a - v sin a;  v' = v cos a + u sin a
+ * (u, v) are dimensions (p, p + pairs), or (2 p, 2 p + 1) if interleaved.
+ * Dimensions from 2 pairs on are copied, as is a pair whose axis is outside
+ * 0 .. n_axes - 1. */
+typedef struct {
+  int32_t type;                   /* of x and out: CEL_BF16, CEL_F16 or CEL_F32 */
+  int32_t tokens, heads, dim;     /* >= 0, 0 .. 65535, 1 .. 4096 */
+  int32_t pairs, interleaved;     /* 2 pairs <= dim */
+  int32_t n_axes;                 /* >= 1 */
+  int32_t position_bytes;         /* 4 (int32) or 8 (int64) */
+  int32_t freq_bytes;             /* 4 (float) or 8 (double) */
+  const void *positions;          /* [n_axes][tokens], axes axis_stride >= 0 elements apart */
+  int64_t axis_stride;
+  const void *freqs;              /* [pairs], radians a position */
+  const int32_t *axes;            /* [pairs]; NULL: axis 0, with n_axes = 1 */
+} cel_rotary_args;
+
+/* out = x turned: products and sums in 32 bits, rounded once.  x and out are
+ * views as cel_rows describes, but of any address of their type and any strides >= 0.
+ * out may be x itself (the same address and strides); otherwise they share no
+ * memory, and no two values of out do.
+ * Errors: CEL_E_ARG (also for 2^32 and more pieces of 16 dimensions that
+ * cannot be dealt out), CEL_E_HIP. */
+int cel_rotary(const cel_rotary_args *a, const cel_rows *x, const cel_rows *out, hipStream_t stream);
+
+/* The gradient of cel_rotary's x at dout, its result's: dout turned back.
+ * Views and errors as there. */
+int cel_rotary_grad(const cel_rotary_args *a, const cel_rows *dout, const cel_rows *dx, hipStream_t stream);
+
+/* A matrix of device memory: row r begins at p + r * stride (in elements), at
+ * any address of its type. */
+typedef struct {
+  void *p;
+  int64_t stride;
+} cel_matrix;
+
+/* Which values dropout keeps.  Value (r, c) has 16 bits of the counter-based
+ * generator Philox4x32 with ten rounds: those c % 8 from below of the 128 that
+ * counter (c / 8, r, low and high word of the step) gives under the key (low
+ * and high word of the seed).  It stays where they are at least
+ * m = floor(2^16 p + 1/2), and is then multiplied by 1 / (1 - m / 2^16).  What
+ * is dropped becomes 0, infinities and NaN too. */
+typedef struct {
+  double p;                  /* 0 .. 1 */
+  uint64_t seed;
+  int64_t step;
+  const int64_t *step_at;    /* NULL, or on the device: added to step (modulo 2^64) */
+} cel_mask;
+
+typedef struct {
+  int32_t type;              /* CEL_BF16, CEL_F16 or CEL_F32 */
+  int64_t rows, columns;     /* < 2^32, < 2^31 */
+  cel_mask mask;
+} cel_dropout_args;
+
+/* out = x with values dropped, the others' product rounded once.  The
+ * gradient of x is the same call on out's gradient.
+ * Inputs: x; strides >= columns.  Outputs: out, x itself (the same address and
+ * stride) or memory of its own.
+ * Errors: CEL_E_ARG, CEL_E_HIP. */
+int cel_dropout(const cel_dropout_args *a, const cel_matrix *x, const cel_matrix *out, hipStream_t stream);
+
+/* The end of a block and the beginning of the next, over rows of `hidden` values:
+ *   n = norm(f) post + post_bias (f itself without post)
+ *   y = scale x + gate drop(n) (without gate: drop(n))
+ *   z = norm(y) pre + pre_bias
+ *   norm(v) = v / sqrt(mean v^2 + eps); with center of v less its mean
+ * f is the block's output, x the residual stream before it, y behind it and z
+ * the next block's input.  gate is a vector for all rows, or with seq_ptr one
+ * for each sequence; a row of no sequence has y = scale x, and its f is not
+ * looked at.  seq_ptr is as cel_attn describes, of rows. */
+typedef struct {
+  int32_t type;                    /* of f and z: CEL_BF16, CEL_F16 or CEL_F32 */
+  int32_t stream_type;             /* of x and y: the same, or CEL_F32 */
+  int32_t param_type;              /* of the vectors: the same as f, or CEL_F32 */
+  int32_t center;
+  int64_t rows, hidden;            /* 0 .. 2^31 - 1, 1 .. 16384 */
+  int32_t n_seq;                   /* 0 .. 65530 */
+  const int32_t *seq_ptr;          /* NULL, or [n_seq + 1] with a gate */
+  float eps, scale;                /* eps >= 0 */
+  const void *pre, *pre_bias;      /* [hidden] or NULL; a bias only with its norm */
+  const void *post, *post_bias;    /* [hidden] or NULL */
+  const void *gate;                /* [hidden], [n_seq][hidden] or NULL */
+  cel_mask mask;                   /* of rows by hidden values; p = 0: nothing is dropped */
+} cel_norm_args;
+
+/* Everything is in 32 bits up to the one rounding of y and of z, which
+ * is the norm of y before its rounding.
+ * Inputs: f, or NULL: z is the norm of x (no post, gate or dropout, scale 1,
+ * y is not written); x.  Outputs: y; z where there is pre.  They share no
+ * memory with an input nor each other.  Strides >= hidden.
+ * Errors: CEL_E_ARG, CEL_E_HIP. */
+int cel_residual_norm(const cel_norm_args *a, const cel_matrix *f, const cel_matrix *x, const cel_matrix *y,
+                      const cel_matrix *z, hipStream_t stream);
+
+/* Gradients of the vectors that a call has, in 32 bits: [hidden], and gate's as gate is. */
+typedef struct {
+  float *pre, *pre_bias, *post, *post_bias, *gate;
+} cel_norm_grads;
+
+/* The gradient of cel_residual_norm at dy and dz, those of y and z, with f and
+ * y as they stand in memory (y rounded).  Statistics are made anew from them.
+ * With Y = norm(y), N = norm(f) and r their factors:
+ *   g = pre dz;  t = dy + r_y (g - [mean g] - Y mean(g Y));  dx = scale t
+ *   e = gate t where it stays, times the mask's factor;  dgate = sum t drop(n)
+ *   df = r_f (post e - [mean post e] - N mean(post e N)), e without post
+ *   dpre = sum dz Y;  dpre_bias = sum dz;  dpost = sum e N;  dpost_bias = sum e
+ * (means of g and post e with center only).  Sums over rows are in a fixed
+ * order: the same inputs give the same bits.  A row of no sequence has df = 0.
+ * Inputs: dy, or NULL: 0; dz and y where there is pre; f where there is post
+ * or gate; scratch of cel_residual_norm_grad_scratch(a) bytes, aligned to 256.
+ * Outputs: dx; df, or NULL where there was no f; what g names.  They
+ * share no memory with an input nor each other.
+ * Errors: CEL_E_ARG, CEL_E_HIP. */
+int cel_residual_norm_grad(const cel_norm_args *a, const cel_matrix *dy, const cel_matrix *dz, const cel_matrix *f,
+                           const cel_matrix *y, void *scratch, const cel_matrix *dx, const cel_matrix *df,
+                           const cel_norm_grads *g, hipStream_t stream);
+
+/* Bytes of scratch that cel_residual_norm_grad takes, or CEL_E_ARG. */
+int64_t cel_residual_norm_grad_scratch(const cel_norm_args *a);
 
 /* Diagnostics: per-kernel device time.  After cel_timing(1), every call
  * records a pair of HIP events on its stream around each of its main kernel

@@ -26,7 +26,9 @@ EXPORTS = ("cel_topo_levels", "cel_blevel", "cel_cpd_order", "cel_dfs_order", "c
            "cel_makespan_info", "cel_makespan_blocks_info", "cel_makespan_relax", "cel_blevel_info", "cel_policy_iteration",
            "cel_topo_levels_info", "cel_cluster_info",
            "cel_order_place", "cel_comm_sums", "cel_makespan_model", "cel_colocate",
-           "cel_attention", "cel_attention_grad", "cel_attention_grad_scratch", "cel_embed", "cel_embed_grad", "cel_embed_grad_scratch", "cel_step_latency", "cel_timing", "cel_kernel_stats", "cel_last_error", "cel_version")
+           "cel_attention", "cel_attention_grad", "cel_attention_grad_scratch", "cel_embed", "cel_embed_grad", "cel_embed_grad_scratch",
+           "cel_rotary", "cel_rotary_grad", "cel_dropout", "cel_residual_norm", "cel_residual_norm_grad", "cel_residual_norm_grad_scratch",
+           "cel_step_latency", "cel_timing", "cel_kernel_stats", "cel_last_error", "cel_version")
 
 
 class CelError(RuntimeError):
@@ -69,6 +71,37 @@ class _Embed(C.Structure):
                 ("ids", C.c_void_p), ("scale", C.c_float)]
 
 
+class _Rotary(C.Structure):
+    _fields_ = [("type", C.c_int32), ("tokens", C.c_int32), ("heads", C.c_int32), ("dim", C.c_int32),
+                ("pairs", C.c_int32), ("interleaved", C.c_int32), ("n_axes", C.c_int32),
+                ("position_bytes", C.c_int32), ("freq_bytes", C.c_int32), ("positions", C.c_void_p),
+                ("axis_stride", C.c_int64), ("freqs", C.c_void_p), ("axes", C.c_void_p)]
+
+
+class _Matrix(C.Structure):
+    _fields_ = [("p", C.c_void_p), ("stride", C.c_int64)]
+
+
+class _Mask(C.Structure):
+    _fields_ = [("p", C.c_double), ("seed", C.c_uint64), ("step", C.c_int64), ("step_at", C.c_void_p)]
+
+
+class _Dropout(C.Structure):
+    _fields_ = [("type", C.c_int32), ("rows", C.c_int64), ("columns", C.c_int64), ("mask", _Mask)]
+
+
+class _Norm(C.Structure):
+    _fields_ = [("type", C.c_int32), ("stream_type", C.c_int32), ("param_type", C.c_int32), ("center", C.c_int32),
+                ("rows", C.c_int64), ("hidden", C.c_int64), ("n_seq", C.c_int32), ("seq_ptr", C.c_void_p),
+                ("eps", C.c_float), ("scale", C.c_float), ("pre", C.c_void_p), ("pre_bias", C.c_void_p),
+                ("post", C.c_void_p), ("post_bias", C.c_void_p), ("gate", C.c_void_p), ("mask", _Mask)]
+
+
+class _NormGrads(C.Structure):
+    _fields_ = [("pre", C.c_void_p), ("pre_bias", C.c_void_p), ("post", C.c_void_p), ("post_bias", C.c_void_p),
+                ("gate", C.c_void_p)]
+
+
 _lib = None
 
 
@@ -106,11 +139,19 @@ def lib() -> C.CDLL:
         L.cel_embed_grad.argtypes = [Em, vp, vp, i32, vp, vp]
         L.cel_embed_grad_scratch.argtypes = [i64, i64, i64]
         L.cel_embed_grad_scratch.restype = i64
+        Rt, Mx, Nm = C.POINTER(_Rotary), C.POINTER(_Matrix), C.POINTER(_Norm)
+        L.cel_rotary.argtypes = L.cel_rotary_grad.argtypes = [Rt, Ro, Ro, vp]
+        L.cel_dropout.argtypes = [C.POINTER(_Dropout), Mx, Mx, vp]
+        L.cel_residual_norm.argtypes = [Nm, Mx, Mx, Mx, Mx, vp]
+        L.cel_residual_norm_grad.argtypes = [Nm, Mx, Mx, Mx, Mx, vp, Mx, Mx, C.POINTER(_NormGrads), vp]
+        L.cel_residual_norm_grad_scratch.argtypes = [Nm]
+        L.cel_residual_norm_grad_scratch.restype = i64
         for f in ("cel_topo_levels", "cel_blevel", "cel_cluster", "cel_place", "cel_place_ext",
                   "cel_makespan",
                   "cel_makespan_noalloc",
                   "cel_cpd_order", "cel_dfs_order", "cel_order_place", "cel_comm_sums", "cel_makespan_model",
-                  "cel_colocate", "cel_attention", "cel_attention_grad", "cel_embed", "cel_embed_grad", "cel_version"):
+                  "cel_colocate", "cel_attention", "cel_attention_grad", "cel_embed", "cel_embed_grad", "cel_rotary", "cel_rotary_grad",
+                  "cel_dropout", "cel_residual_norm", "cel_residual_norm_grad", "cel_version"):
             getattr(L, f).restype = C.c_int
         L.cel_last_error.argtypes = []
         L.cel_last_error.restype = C.c_char_p
@@ -566,9 +607,9 @@ def _views(*tensors):
     return views, keep
 
 
-def _block(x, T, H, d):
+def _block(x, T, H, d, size=2):
     """A view's (first element, element behind its last, row stride, head stride, heads)."""
-    at, row, head = (x.p or 0) // 2, x.row, x.head
+    at, row, head = (x.p or 0) // size, x.row, x.head
     return at, at + (T - 1) * row + (H - 1) * head + d, row, head, H
 
 
@@ -754,3 +795,291 @@ def embed_grad(dx, ids, vocab, scale=1.0, dtype=None):
         _check(lib().cel_embed_grad(C.byref(a), dx.data_ptr(), work.data_ptr(), _TYPES[dtype], grad.data_ptr(),
                                     _raw_stream(index)))
     return grad
+
+
+def _apart(fn, out, x, T, d, size, *others):
+    """Refuses results (a block) that share memory within themselves, with x (a block, unless they are
+    x itself, in place) or with other tensors."""
+    if _folded(out, T, d):
+        _refuse(f"{fn}: values of out share memory")
+    if out != x and _meet(out, x, T, d):
+        _refuse(f"{fn}: out shares memory with x without being it")
+    for t in others:
+        if t is not None and t.numel():
+            at = t.data_ptr()
+            end = at + t.element_size() * (1 + sum((n - 1) * s for n, s in zip(t.shape, t.stride())))
+            if at < out[1] * size and out[0] * size < end:
+                _refuse(f"{fn}: out shares memory with another input")
+
+
+def _plain_view(t):
+    """t [tokens, heads, dim] with values contiguous, any strides >= 0, or None."""
+    row, head, one = t.stride()
+    T, H, d = t.shape
+    if one != 1 and d > 1:
+        return None
+    return _Rows(t.data_ptr(), row if T > 1 else 0, head if H > 1 else 0)
+
+
+def _rotary(fn, x, positions, freqs, axes, pairs, out):
+    tensors = dict(x=x, positions=positions, freqs=freqs)
+    if axes is not None:
+        tensors["axes"] = axes
+    if out is not None:
+        tensors["out"] = out
+    index = _device_of(fn, **tensors)
+    with _on(index):
+        if x.dim() != 3 or x.dtype not in _TYPES:
+            _refuse(f"{fn}: x is not [tokens, heads, dim] in bfloat16, float16 or float32")
+        T, H, d = x.shape
+        if positions.dim() == 1:
+            positions = positions.unsqueeze(0)
+        if positions.dim() != 2 or positions.dtype not in (torch.int32, torch.int64) or positions.shape[1] != T:
+            _refuse(f"{fn}: positions are not int32 or int64 [tokens] or [axes, tokens]")
+        if freqs.dim() != 1 or freqs.dtype not in (torch.float32, torch.float64):
+            _refuse(f"{fn}: freqs are not float32 or float64 [pairs]")
+        P, A = freqs.numel(), positions.shape[0]
+        if axes is None and A != 1:
+            _refuse(f"{fn}: positions of {A} axes, and no axes of the pairs")
+        if axes is not None and (axes.shape != (P,) or axes.dtype != torch.int32):
+            _refuse(f"{fn}: axes are not int32 [pairs]")
+        if T >= 1 << 31:
+            _refuse(f"{fn}: {T} tokens")
+        if T > 1 and positions.stride(1) != 1:
+            positions = positions.contiguous()
+        freqs = freqs.contiguous()
+        axes = axes if axes is None else axes.contiguous()
+        xv = _plain_view(x)
+        if xv is None:
+            x = x.clone(memory_format=torch.contiguous_format)
+            xv = _Rows(x.data_ptr(), H * d, d)
+        if out is None:
+            out = torch.empty((T, H, d), dtype=x.dtype, device=x.device)
+            ov = _Rows(out.data_ptr(), H * d, d)
+        else:
+            ov = _plain_view(out) if out.shape == x.shape and out.dtype == x.dtype else None
+            if ov is None:
+                _refuse(f"{fn}: out cannot be written in place: {tuple(out.shape)} {out.dtype}, strides {out.stride()}")
+            if x.numel():
+                size = x.element_size()
+                _apart(fn, _block(ov, T, H, d, size), _block(xv, T, H, d, size), T, d, size, positions, freqs, axes)
+        a = _Rotary(_TYPES[x.dtype], T, H, d, P, bool(pairs), A, positions.element_size(), freqs.element_size(), positions.data_ptr(),
+                    positions.stride(0) if A > 1 else 0, freqs.data_ptr(), None if axes is None else axes.data_ptr())
+        call = lib().cel_rotary if fn == "rotary" else lib().cel_rotary_grad
+        _check(call(C.byref(a), C.byref(xv), C.byref(ov), _raw_stream(index)))
+    return out
+
+
+def rotary(x, positions, freqs, axes=None, pairs=False, out=None):
+    """Rotary positions: of each head's dimensions pair p turns by positions[axes[p]][t] * freqs[p]
+    radians, (u, v) -> (u cos - v sin, v cos + u sin).  x [tokens, heads, dim] in bfloat16, float16 or
+    float32, any strides (a copy where a head's values are not contiguous); positions int32 or int64
+    [tokens], or [axes, tokens] (time, height, width); freqs float32 or float64 [pairs]; axes int32
+    [pairs], the axis of each pair, needed with several; a pair whose axis does not exist stays as it is.
+    Pairs are dimensions (p, p + pairs), or with pairs=True the neighbours (2 p, 2 p + 1); dimensions
+    behind them are copied.  Angles are made in 64 bits.  out: where to write, x itself or memory apart
+    from every input. -> out.  Queries and keys side by side in one projection are one call."""
+    return _rotary("rotary", x, positions, freqs, axes, pairs, out)
+
+
+def rotary_grad(dout, positions, freqs, axes=None, pairs=False, out=None):
+    """The gradient of rotary()'s x at dout: the same turns backwards.  Arguments as there."""
+    return _rotary("rotary_grad", dout, positions, freqs, axes, pairs, out)
+
+
+def _mask(fn, p, seed, step):
+    """-> what the kernels take; the step is a number, or a tensor on the device."""
+    if not isinstance(step, torch.Tensor):
+        at = None
+        step &= (1 << 64) - 1
+    elif step.numel() != 1 or step.dtype != torch.int64:
+        _refuse(f"{fn}: step is not a number or one int64")
+    else:
+        at, step = step.data_ptr(), 0
+    return _Mask(p, seed & ((1 << 64) - 1), step if step < 1 << 63 else step - (1 << 64), at)
+
+
+def _matrix(t):
+    """t as (rows, columns, row stride), its last dimension the columns; None where a copy is needed."""
+    shape = t.shape
+    if t.is_contiguous():
+        columns = shape[-1] if shape else 1
+        return (t.numel() // columns if columns else 0), columns, columns
+    columns, rows, stride = shape[-1], 1, 0
+    strides = t.stride()
+    if columns > 1 and strides[-1] != 1:
+        return None
+    for n, s in zip(shape[-2::-1], strides[-2::-1]):
+        if n == 1:
+            continue
+        if rows == 1:
+            stride = s
+        elif s != rows * stride:
+            return None
+        rows *= n
+    if rows == 1:
+        stride = columns
+    return (rows, columns, stride) if stride >= columns else None
+
+
+def dropout(x, p, seed, step=0, out=None):
+    """x with each value dropped (0) with probability p, the others divided by 1 - p; p is rounded to
+    16 bits.  What stays is a function of (seed, step) and of a value's row and column (x's last dimension
+    are the columns, all others together the rows) and is not stored: the gradient of x is the same call
+    on out's gradient.  x in bfloat16, float16 or float32, any strides (a copy where they are no rows of
+    contiguous values); seed and step: integers of 64 bits; step may be an int64 tensor of one value on
+    the device, read when the kernel runs, so that a replayed graph can go on to other masks.  out: where
+    to write, x itself or memory apart. -> out"""
+    fn = "dropout"
+    tensors = dict(x=x)
+    if isinstance(step, torch.Tensor):
+        tensors["step"] = step
+    if out is not None:
+        tensors["out"] = out
+    index = _device_of(fn, **tensors)
+    with _on(index):
+        if x.dtype not in _TYPES:
+            _refuse(f"{fn}: x is not in bfloat16, float16 or float32")
+        mask = _mask(fn, p, seed, step)
+        m = _matrix(x)
+        if m is None:
+            x = x.clone(memory_format=torch.contiguous_format)
+            m = _matrix(x)
+        rows, columns, stride = m
+        if rows >= 1 << 32 or columns >= 1 << 31:
+            _refuse(f"{fn}: {rows} rows of {columns} values")
+        if out is None:
+            out = torch.empty(x.shape, dtype=x.dtype, device=x.device)
+            to = columns
+        else:
+            o = _matrix(out) if out.shape == x.shape and out.dtype == x.dtype else None
+            if o is None:
+                _refuse(f"{fn}: out cannot be written in place: {tuple(out.shape)} {out.dtype}, strides {out.stride()}")
+            to = o[2]
+            if x.numel():
+                size = x.element_size()
+                blocks = [_block(_Rows(t.data_ptr(), s, 0), rows, 1, columns, size) for t, s in ((out, to), (x, stride))]
+                _apart(fn, *blocks, rows, columns, size, tensors.get("step"))
+        a = _Dropout(_TYPES[x.dtype], rows, columns, mask)
+        _check(lib().cel_dropout(C.byref(a), C.byref(_Matrix(x.data_ptr(), stride)), C.byref(_Matrix(out.data_ptr(), to)), _raw_stream(index)))
+    return out
+
+
+_VECTORS = ("pre", "pre_bias", "post", "post_bias", "gate")
+
+
+def _norm(fn, f, stream, of_f, of_stream, vectors, seq_ptr, scale, p, seed, step, eps, center):
+    """-> (device, descriptor, matrices, tensors to keep alive): checks that residual_norm and residual_norm_grad
+    share.  of_f and of_stream: further tensors as f and as the stream, by name; f, those of of_f and the vectors may be None."""
+    given = {n: t for n, t in {**of_f, **of_stream, **dict(zip(_VECTORS, vectors))}.items() if t is not None}
+    if f is not None:
+        given["f"] = f
+    given["the stream"] = stream
+    if seq_ptr is not None:
+        given["seq_ptr"] = seq_ptr
+    if isinstance(step, torch.Tensor):
+        given["step"] = step
+    index = _device_of(fn, **given)
+    if stream.dim() != 2 or stream.dtype not in _TYPES:
+        _refuse(f"{fn}: the stream is not [rows, hidden] in bfloat16, float16 or float32")
+    T, h = shape = stream.shape
+    keep, matrices = [], []
+    like = [t for t in (f, *of_f.values()) if t is not None]
+    kind = like[0].dtype if like else given["pre"].dtype if stream.dtype == torch.float32 and "pre" in given else stream.dtype
+    if kind not in _TYPES or stream.dtype not in (kind, torch.float32):
+        _refuse(f"{fn}: a stream in {stream.dtype} beside blocks in {kind}")
+    for t, dtype in [(f, kind), (stream, stream.dtype)] + [(t, kind) for t in of_f.values()] + [(t, stream.dtype) for t in of_stream.values()]:
+        if t is None:
+            matrices.append(None)
+            continue
+        if t.shape != shape or t.dtype != dtype:
+            _refuse(f"{fn}: {tuple(t.shape)} {t.dtype} beside a stream of {tuple(shape)}, {dtype} wanted")
+        m = _matrix(t)
+        if m is None:
+            t = t.clone(memory_format=torch.contiguous_format)
+            keep.append(t)
+            m = _matrix(t)
+        matrices.append(_Matrix(t.data_ptr(), m[2]))
+    wide, at = None, []
+    S = 0
+    if seq_ptr is not None:
+        if seq_ptr.dim() != 1 or seq_ptr.dtype != torch.int32 or seq_ptr.numel() < 1 or vectors[4] is None:
+            _refuse(f"{fn}: seq_ptr is not int32 [sequences + 1] beside a gate")
+        seq_ptr = seq_ptr.contiguous()
+        keep.append(seq_ptr)
+        S = seq_ptr.numel() - 1
+    for name, t in zip(_VECTORS, vectors):
+        if t is None:
+            at.append(None)
+            continue
+        want = (S, h) if name == "gate" and seq_ptr is not None else (h,)
+        wide = t.dtype if wide is None else wide
+        if t.shape != want or t.dtype != wide or wide not in (kind, torch.float32):
+            _refuse(f"{fn}: {name} is {tuple(t.shape)} {t.dtype}, {want} wanted in one type for all, {kind} or float32")
+        if not h:
+            _refuse(f"{fn}: rows of no values")
+        t = t.contiguous()
+        keep.append(t)
+        at.append(t.data_ptr() or seq_ptr.data_ptr())  # the gates of no sequence have no address, and none is read
+    if T >= 1 << 31:
+        _refuse(f"{fn}: {T} rows")
+    a = _Norm(_TYPES[kind], _TYPES[stream.dtype], _TYPES[wide or kind], bool(center), T, h, S,
+              None if seq_ptr is None else seq_ptr.data_ptr(), eps, scale, *at, _mask(fn, p, seed, step))
+    return index, kind, a, matrices, keep
+
+
+def _at(m):
+    return None if m is None else C.byref(m)
+
+
+def residual_norm(f, x, pre, post=None, gate=None, seq_ptr=None, pre_bias=None, post_bias=None, scale=1.0, p=0.0, seed=0, step=0,
+                  eps=1e-6, center=False):
+    """The end of a block and the beginning of the next, in one pass:
+
+        n = norm(f) * post + post_bias   (f itself without post)
+        y = scale * x + gate * dropout(n, p, seed, step)
+        z = norm(y) * pre + pre_bias
+
+    with norm(v) = v / sqrt(mean(v^2) + eps) over a row, of v less its mean with center=True (a layer norm).
+    f [rows, hidden], the block's output, in bfloat16, float16 or float32; x, the residual stream before it, in
+    the same type or float32; hidden up to 16384; rows any stride apart.  pre, pre_bias, post, post_bias: [hidden]
+    or None; gate: [hidden], or with seq_ptr (int32 [sequences + 1], on the device) [sequences, hidden], a row for
+    the rows seq_ptr[s] .. seq_ptr[s + 1] - 1; a row of no sequence has y = scale * x.  All vectors in one type, f's
+    or float32.  The mask is that of dropout() for [rows, hidden].
+    -> (y as x, z as f): the stream behind the block, and the next block's input (None without pre).  f = None: no
+    block yet, -> (x, norm(x) * pre + pre_bias)."""
+    fn = "residual_norm"
+    index, kind, a, (fm, xm), keep = _norm(fn, f, x, {}, {}, (pre, pre_bias, post, post_bias, gate), seq_ptr, scale, p, seed, step, eps, center)
+    with _on(index):
+        y = x if f is None else torch.empty(x.shape, dtype=x.dtype, device=x.device)
+        z = None if pre is None else torch.empty(x.shape, dtype=kind, device=x.device)
+        h = a.hidden
+        _check(lib().cel_residual_norm(C.byref(a), _at(fm), _at(xm), None if f is None else C.byref(_Matrix(y.data_ptr(), h)),
+                                       None if z is None else C.byref(_Matrix(z.data_ptr(), h)), _raw_stream(index)))
+    return y, z
+
+
+def residual_norm_grad(dy, dz, f, y, pre, post=None, gate=None, seq_ptr=None, pre_bias=None, post_bias=None, scale=1.0, p=0.0,
+                       seed=0, step=0, eps=1e-6, center=False):
+    """The gradient of residual_norm() at dy and dz, those of its results, from its f, its result y (x where f was
+    None) and its other arguments.  dy may be None (0); dz is None where pre was.
+    -> (dx as y, df as f, or None without f, gradients of the vectors by name in float32: those of pre, pre_bias, post,
+    post_bias and gate that there are).  Sums over rows are added in a fixed order: the same inputs give the same bits."""
+    fn = "residual_norm_grad"
+    if (dz is None) != (pre is None):
+        _refuse(f"{fn}: dz and pre come together")
+    vectors = (pre, pre_bias, post, post_bias, gate)
+    index, kind, a, (fm, ym, zm, gm), keep = _norm(fn, f, y, dict(dz=dz), dict(dy=dy), vectors, seq_ptr, scale, p, seed, step, eps, center)
+    with _on(index):
+        dx = torch.empty(y.shape, dtype=y.dtype, device=y.device)
+        df = None if f is None else torch.empty(y.shape, dtype=kind, device=y.device)
+        grads = {n: torch.empty(t.shape, dtype=torch.float32, device=y.device) for n, t in zip(_VECTORS, vectors) if t is not None}
+        size = lib().cel_residual_norm_grad_scratch(C.byref(a))
+        if size < 0:
+            _check(size)
+        scratch = torch.empty(size, dtype=torch.uint8, device=y.device)
+        to = _NormGrads(*(grads[n].data_ptr() or scratch.data_ptr() if n in grads else None for n in _VECTORS))
+        h = a.hidden
+        _check(lib().cel_residual_norm_grad(C.byref(a), _at(gm), _at(zm), _at(fm), _at(ym), scratch.data_ptr(), C.byref(_Matrix(dx.data_ptr(), h)),
+                                            None if df is None else C.byref(_Matrix(df.data_ptr(), h)), C.byref(to), _raw_stream(index)))
+    return dx, df, grads

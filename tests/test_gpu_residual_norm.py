@@ -1,0 +1,310 @@
+"""cel.residual_norm and cel.residual_norm_grad against the definition in 64 bits, element by element,
+within the errors that block_reference derives from the formulas' roundings."""
+from __future__ import annotations
+
+import pytest
+
+torch = pytest.importorskip("torch")
+
+pytestmark = pytest.mark.gpu
+
+if not torch.cuda.is_available():  # collected on CPU, skipped there
+    pytest.skip("needs a ROCm GPU", allow_module_level=True)
+
+import paper_2208_00184_amd as cel  # noqa: E402
+from block_reference import Joint, randn, within  # noqa: E402
+
+DEV = "cuda:0"
+bf16, f16, f32 = torch.bfloat16, torch.float16, torch.float32
+TYPES = [(bf16, bf16, bf16), (bf16, f32, f32), (f16, f16, f32), (f16, f32, f16), (f32, f32, f32)]  # f, stream, vectors
+
+
+def make(T, h, types=(bf16, bf16, f32), post=False, gate=False, bias=False, seqs=None, seed=0):
+    """-> (f, x, dy, dz, vectors by name)"""
+    t, r, w = types
+    f, dz = (randn(T, h, seed=seed + i, by=1.5, at=0.2).to(t).to(DEV) for i in (1, 2))
+    x, dy = (randn(T, h, seed=seed + i, by=2.0, at=-0.3).to(r).to(DEV) for i in (3, 4))
+    v = dict(pre=randn(h, seed=seed + 5, by=0.3, at=1.0))
+    if bias:
+        v["pre_bias"] = randn(h, seed=seed + 6)
+    if post:
+        v["post"] = randn(h, seed=seed + 7, by=0.3, at=1.0)
+        if bias:
+            v["post_bias"] = randn(h, seed=seed + 8)
+    if gate:
+        v["gate"] = randn(h, seed=seed + 9) if seqs is None else randn(len(seqs) - 1, h, seed=seed + 9)
+    v = {n: x.to(w).to(DEV) for n, x in v.items()}
+    if gate and seqs is not None:
+        v["seq_ptr"] = torch.tensor(seqs, dtype=torch.int32, device=DEV)
+    return f, x, dy, dz, v
+
+
+def check(f, x, dy, dz, v, **how):
+    v = {"pre": None, **v}
+    joint = Joint(**v, **how)
+    y, z = cel.residual_norm(f, x, **v, **how)
+    (wy, ey), wz = joint.forward(f, x)
+    if f is None:
+        assert y is x
+    else:
+        assert y.dtype == x.dtype and y.shape == x.shape
+        within(y, wy, ey)
+    if wz is None:
+        assert z is None
+    else:
+        within(z, *wz)
+    dx, df, grads = cel.residual_norm_grad(dy, dz if wz is not None else None, f, y, **v, **how)
+    want = joint.backward(dy, dz, f, y)
+    assert set(grads) == set(want) - {"dx", "df"} and (df is None) == (f is None)
+    for name, got in dict(dx=dx, df=df, **grads).items():
+        if got is not None:
+            assert got.shape == want[name][0].shape, name
+            within(got, *want[name])
+    assert dx.dtype == y.dtype and all(g.dtype == f32 for g in grads.values())
+    return y, z, dx, df, grads
+
+
+@pytest.mark.parametrize("types", TYPES)
+@pytest.mark.parametrize("h", [1, 2, 7, 8, 9, 64, 100, 511, 512, 513, 1000, 1024, 1025, 2049, 3072 + 5, 4096, 8191, 8192])
+def test_widths(h, types):
+    check(*make(19, h, types, post=True, gate=True, bias=True, seed=h), p=0.2, seed=h, scale=0.5)
+    check(*make(19, h, types, seed=h), center=True)
+
+
+@pytest.mark.parametrize("types", TYPES)
+@pytest.mark.parametrize("h", [8193, 12000, 16384])
+def test_rows_of_sixteen_waves(h, types):
+    check(*make(5, h, types, post=True, gate=True, bias=True, seqs=[0, 2, 2, 4], seed=h), p=0.2, seed=h, center=True)
+    check(*make(5, h, types, seed=h))
+
+
+@pytest.mark.parametrize("T", [0, 1, 2, 7, 8, 9, 255, 256, 2047, 2049, 5000])
+def test_lengths(T):
+    """From no row to many rows of each of the workgroups."""
+    check(*make(T, 72, post=True, gate=True, bias=True, seed=T), p=0.1, seed=3, step=T)
+    check(*make(T, 600, seed=T))
+
+
+@pytest.mark.parametrize("center", [False, True])
+@pytest.mark.parametrize("bias", [False, True])
+@pytest.mark.parametrize("gate", [None, "channel", "sequence"])
+@pytest.mark.parametrize("post", [False, True])
+@pytest.mark.parametrize("p", [0.0, 0.4])
+def test_parts(post, gate, bias, center, p):
+    seqs = [0, 5, 5, 6, 30, 41] if gate == "sequence" else None
+    for h in (40, 1500):
+        check(*make(50, h, post=post, gate=gate is not None, bias=bias, seqs=seqs, seed=h), p=p, seed=9, center=center, scale=1.3, eps=1e-5)
+
+
+@pytest.mark.parametrize("how", ["no pre", "no dy", "no pre but post", "no f", "no f, layer"])
+def test_what_may_be_missing(how):
+    for types in TYPES:
+        f, x, dy, dz, v = make(33, 264, types, post="post" in how, bias="layer" in how)
+        if "no pre" in how:
+            v["pre"] = None
+        if how == "no dy":
+            dy = None
+        if "no f" in how:
+            f = None
+            if types[0] != types[1]:  # z is in the vectors' type then
+                dz = dz.to(types[2])
+        check(f, x, dy, dz, v, center="layer" in how, **({} if "no f" in how else dict(p=0.3, seed=1, scale=2.0)))
+
+
+@pytest.mark.parametrize("seqs", [[0, 1, 2, 3, 4, 5, 6, 7, 8, 9], [3, 3, 50, 50, 90], [0, 120], [60], [0, 0, 0], [119, 120], [0, 7, 64, 65, 120],
+                                  list(range(0, 121, 2))])
+@pytest.mark.parametrize("h", [24, 1032, 4100])
+def test_gates_of_sequences(seqs, h):
+    """Sequences of one row and of none, rows before, between and behind them; a row of none has its f not looked at."""
+    f, x, dy, dz, v = make(120, h, post=True, gate=True, seqs=seqs, seed=len(seqs))
+    there = torch.zeros(120, dtype=torch.bool)
+    there[seqs[0]:seqs[-1]] = True
+    got = check(f, x, dy, dz, v, p=0.1, seed=4)
+    bad = f.clone()
+    bad[~there.to(DEV)] = float("nan")
+    y, z = cel.residual_norm(bad, x, **v, p=0.1, seed=4)
+    dx, df, grads = cel.residual_norm_grad(dy, dz, bad, y, **v, p=0.1, seed=4)
+    assert torch.equal(y, got[0]) and torch.equal(z, got[1]) and torch.equal(dx, got[2]) and torch.equal(df, got[3])
+    assert all(torch.equal(grads[n], got[4][n]) for n in grads)
+    assert not bool(df[~there.to(DEV)].any())
+
+
+@pytest.mark.parametrize("T,S", [(6000, 3), (6000, 700), (3000, 2900)])
+def test_gates_of_many_sequences(T, S):
+    g = torch.Generator().manual_seed(S)
+    cuts = torch.randint(0, T + 1, (S + 1,), generator=g).sort().values.tolist()
+    check(*make(T, 40, post=True, gate=True, bias=True, seqs=cuts, seed=S), p=0.1, seed=4)
+
+
+def test_malformed_sequences_stay_in_bounds():
+    f, x, dy, dz, v = make(64, 40, post=True, gate=True, seqs=[0, 20, 64])
+    for ptr in ([0, 70, 64], [50, 10, 64], [-5, 10, 2000], [64, 0, 0], [2 ** 31 - 1, 5, -2 ** 31], [-1, -1, -1]):
+        v["seq_ptr"] = torch.tensor(ptr, dtype=torch.int32, device=DEV)
+        y, z = cel.residual_norm(f, x, **v)
+        cel.residual_norm_grad(dy, dz, f, y, **v)
+    torch.cuda.synchronize()
+
+
+def test_the_masks_are_dropouts():
+    f, x, dy, dz, v = make(40, 136)
+    at = torch.tensor([11], dtype=torch.int64, device=DEV)
+    zero = torch.zeros_like(x)
+    y, _ = cel.residual_norm(f, zero, **v, p=0.3, seed=5, step=at)
+    assert torch.equal(y, cel.dropout(f, 0.3, 5, step=11))
+    _, df, _ = cel.residual_norm_grad(dy, torch.zeros_like(dz), f, y, **v, p=0.3, seed=5, step=at)
+    assert torch.equal(df, cel.dropout(dy, 0.3, 5, step=11))
+
+
+def test_everything_dropped_and_rows_of_zeros():
+    f, x, dy, dz, v = make(20, 100, post=True, gate=True)
+    check(f, x, dy, dz, v, p=1.0)
+    check(torch.zeros_like(f), torch.zeros_like(x), dy, dz, v, eps=1e-3)
+    check(f, x, dy, dz, v, p=2.0 ** -18)  # rounds to nothing dropped
+
+
+def test_no_eps_and_a_ragged_end():
+    """Rows that are not there have no norm without eps: nothing of them reaches a sum."""
+    check(*make(13, 40, post=True, gate=True, bias=True), eps=0.0)
+    check(*make(13, 1030, post=True, gate=True, bias=True, seqs=[1, 4, 12]), eps=0.0, center=True)
+
+
+def test_large_means_are_taken_out_first():
+    """A layer norm of rows far from 0, whose mean square would swallow the variance."""
+    f, x, dy, dz, v = make(30, 700, (f32, f32, f32), post=True)
+    check(f + 3000.0, x + 5000.0, dy, dz, v, center=True)
+
+
+def test_infinities_stay_in_their_row():
+    f, x, dy, dz, v = make(24, 200, (f32, f32, f32), post=True, gate=True)
+    y, z = cel.residual_norm(f, x, **v)
+    x[5, 3], f[9, 7] = float("inf"), float("nan")
+    y2, z2 = cel.residual_norm(f, x, **v)
+    rows = torch.tensor([i for i in range(24) if i not in (5, 9)], device=DEV)
+    assert torch.equal(y[rows], y2[rows]) and torch.equal(z[rows], z2[rows])
+    assert not bool(torch.isfinite(z2[9]).any()) and not bool(torch.isfinite(y2[9]).any()) and not bool(torch.isfinite(y2[5, 3]))
+    dx, df, _ = cel.residual_norm_grad(dy, dz, f, y2, **v)
+    dx1, df1, _ = cel.residual_norm_grad(dy, dz, f.nan_to_num(0.0), y, **v)
+    assert torch.equal(dx[rows], dx1[rows]) and torch.equal(df[rows], df1[rows])
+
+
+def test_strides_and_copies():
+    f, x, dy, dz, v = make(30, 120, post=True, gate=True, bias=True)
+    plain = check(f, x, dy, dz, v, p=0.1)
+
+    def wide(t, first):
+        w = torch.full((30, 131), 7.0, dtype=t.dtype, device=DEV)
+        w[:, first:first + 120] = t
+        return w[:, first:first + 120]
+
+    def turned(t):
+        return t.T.contiguous().T
+
+    for how in (lambda t: wide(t, 1), lambda t: wide(t, 8), turned):
+        w = {n: torch.stack([t, t], -1)[..., 0] for n, t in v.items()}
+        y, z = cel.residual_norm(how(f), how(x), **w, p=0.1)
+        assert torch.equal(y, plain[0]) and torch.equal(z, plain[1])
+        dx, df, grads = cel.residual_norm_grad(how(dy), how(dz), how(f), how(y), **w, p=0.1)
+        assert torch.equal(dx, plain[2]) and torch.equal(df, plain[3]) and all(torch.equal(grads[n], plain[4][n]) for n in grads)
+
+
+def test_the_same_inputs_give_the_same_bits():
+    f, x, dy, dz, v = make(5000, 264, post=True, gate=True, bias=True, seqs=[0, 700, 702, 4000, 5000])
+    a, b = (cel.residual_norm_grad(dy, dz, f, x, **v, p=0.1) for _ in range(2))
+    assert torch.equal(a[0], b[0]) and torch.equal(a[1], b[1]) and all(torch.equal(a[2][n], b[2][n]) for n in a[2])
+
+
+def test_gradients_against_differences():
+    """Directional differences of the forward pass in 32 bits: at a step of 2^-7 the result's change is off by the
+    second-order term, of about step^2 times the third derivative's size, and roundings over the step."""
+    f, x, dy, dz, v = make(6, 48, (f32, f32, f32), post=True, gate=True, bias=True)
+    how = dict(p=0.25, seed=3, scale=0.7, eps=1e-3, center=True)
+    leaves = dict(f=f, x=x, **v)
+
+    def total(d):
+        a = {n: t.double() for n, t in leaves.items()}
+        a = {n: (a[n] + d[n]).float() for n in a}
+        y, z = cel.residual_norm(a.pop("f"), a.pop("x"), **a, **how)
+        return float((y.double() * dy.double()).sum() + (z.double() * dz.double()).sum())
+
+    y, _ = cel.residual_norm(f, x, **v, **how)
+    dx, df, grads = cel.residual_norm_grad(dy, dz, f, y, **v, **how)
+    slopes = dict(f=df, x=dx, **grads)
+    for n in leaves:
+        h = 2.0 ** -7
+        d = {m: torch.zeros_like(t).double() for m, t in leaves.items()}
+        d[n] = randn(*leaves[n].shape, seed=len(n)).double().to(DEV)
+        d[n] /= d[n].norm()
+        one = {m: t * h for m, t in d.items()}
+        two = {m: -t for m, t in one.items()}
+        slope, want = (total(one) - total(two)) / (2 * h), float((slopes[n].double() * d[n]).sum())
+        assert abs(slope - want) <= 2e-3 * float(slopes[n].double().norm()), n
+
+
+def test_inside_a_graph():
+    f, x, dy, dz, v = make(300, 264, post=True, gate=True, seqs=[0, 100, 290])
+    step = torch.zeros(1, dtype=torch.int64, device=DEV)
+
+    def both(step):
+        y, z = cel.residual_norm(f, x, **v, p=0.2, seed=6, step=step)
+        dx, df, grads = cel.residual_norm_grad(dy, dz, f, y, **v, p=0.2, seed=6, step=step)
+        return [y, z, dx, df, *grads.values()]
+
+    want = [both(s) for s in range(4)]
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        out = both(step)
+        step.add_(1)
+    step.zero_()
+    for s in range(3):
+        for t in out:
+            t.zero_()
+        graph.replay()
+        torch.cuda.synchronize()
+        assert all(torch.equal(a, b) for a, b in zip(out, want[s]))
+        assert all(torch.equal(a, b) for a, b in zip(both(step), want[s + 1]))
+
+
+def test_refusals():
+    def refused(f, *a, **kw):
+        with pytest.raises(cel.CelError) as e:
+            f(*a, **kw)
+        assert e.value.code == -1
+
+    f, x, dy, dz, v = make(8, 40, post=True, gate=True, bias=True)
+    pre, gate = v["pre"], v["gate"]
+    ptr = torch.tensor([0, 8], dtype=torch.int32, device=DEV)
+    norm, grad = cel.residual_norm, cel.residual_norm_grad
+    refused(norm, f[0], x, pre)
+    refused(norm, f, x[:7], pre)
+    refused(norm, f, x.half(), pre)
+    refused(norm, f.float(), x, pre)
+    refused(norm, f.double(), x.double(), pre)
+    refused(norm, f, x.cpu(), pre)
+    refused(norm, f, x, pre.cpu())
+    refused(norm, f, x, pre[:39])
+    refused(norm, f, x, pre.half())
+    refused(norm, f, x, pre, post=v["post"].bfloat16())  # vectors of two types
+    refused(norm, f, x, None, pre_bias=v["pre_bias"])
+    refused(norm, f, x, pre, post_bias=v["post_bias"])
+    refused(norm, f, x, pre, seq_ptr=ptr)
+    refused(norm, f, x, pre, gate=gate, seq_ptr=ptr)
+    refused(norm, f, x, pre, gate=gate[None], seq_ptr=ptr.long())
+    refused(norm, f, x, pre, gate=gate[None])
+    refused(norm, f, x, pre, eps=-1.0)
+    refused(norm, f, x, pre, scale=float("inf"))
+    refused(norm, f, x, pre, p=2.0)
+    refused(norm, f, x, pre, p=0.1, step=torch.zeros(2, dtype=torch.int64, device=DEV))
+    refused(norm, None, x, pre, p=0.1)
+    refused(norm, None, x, pre, scale=2.0)
+    refused(norm, None, x, pre, gate=gate)
+    refused(norm, None, x, None)
+    refused(norm, torch.zeros(2, 16385, device=DEV), torch.zeros(2, 16385, device=DEV), None)
+    refused(norm, torch.zeros(2, 0, device=DEV), torch.zeros(2, 0, device=DEV), None)
+    refused(norm, f.clone().requires_grad_(), x, pre)
+    refused(grad, dy, None, f, x, pre)
+    refused(grad, dy, dz, f, x, None)
+    refused(grad, None, None, f, x, None)
+    refused(grad, dy.float(), dz, f, x, pre)
+    refused(grad, dy, dz.float(), f, x, pre)
+    refused(grad, dy, dz[:7], f, x, pre)
