@@ -19,6 +19,7 @@
  * measure the costs that the graph's nodes carry (Section 4.2.1):
  *
  *   cel_attention, cel_attention_grad  causal attention over a packed batch
+ *   cel_cross_attention, cel_cross_attention_grad  attention to an encoder's states
  *   cel_embed, cel_embed_grad          embedding lookup, gradient by sorted tokens
  *   cel_rotary, cel_rotary_grad        rotary positions of one axis or several
  *   cel_dropout                        dropout without a stored mask
@@ -399,6 +400,33 @@ int cel_attention_grad(const cel_attn *a, const cel_rows *out, const float *lse,
 /* Bytes of scratch that cel_attention_grad takes for a (its type, sizes and
  * scale are looked at), or CEL_E_ARG. */
 int64_t cel_attention_grad_scratch(const cel_attn *a);
+
+/* Attention to other states, for instance an encoder's, packed as the tokens
+ * are: sequence s has the tokens seq_ptr[s] .. seq_ptr[s + 1] - 1 and the keys
+ * key_ptr[s] .. key_ptr[s + 1] - 1 (as cel_attn describes seq_ptr, of keys), and
+ * each of its tokens sees all of its keys. */
+typedef struct {
+  int32_t type;                  /* as in cel_attn, up to scale */
+  int32_t tokens, keys, n_seq;   /* heads times tokens / 128, rounded up, below 2^24; with the gradient keys / 64 too */
+  int32_t heads, kv_heads, dim;
+  float scale;
+  const int32_t *seq_ptr, *key_ptr;
+  cel_rows q, k, v;              /* q: tokens, heads; k, v: keys, kv_heads; read-only */
+} cel_cross_attn;
+
+/* As cel_attention, but for who sees whom.  A token whose sequence has no
+ * keys has out = 0 and lse = -infinity, as one of no sequence. */
+int cel_cross_attention(const cel_cross_attn *a, const cel_rows *out, float *lse, hipStream_t stream);
+
+/* Its gradient, as cel_attention_grad.  A key of no sequence, or of one
+ * without tokens, has gradients of 0.  scratch:
+ * cel_cross_attention_grad_scratch(a) bytes, aligned to 256. */
+int cel_cross_attention_grad(const cel_cross_attn *a, const cel_rows *out, const float *lse, const cel_rows *dout,
+                             void *scratch, const cel_rows *dq, const cel_rows *dk, const cel_rows *dv,
+                             hipStream_t stream);
+
+/* Bytes of scratch that cel_cross_attention_grad takes for a, or CEL_E_ARG. */
+int64_t cel_cross_attention_grad_scratch(const cel_cross_attn *a);
 
 /* Rows of an embedding table by token id.  An id outside 0 .. vocab - 1 is
  * padding: its row is zero and it gives no gradient. */

@@ -26,7 +26,8 @@ EXPORTS = ("cel_topo_levels", "cel_blevel", "cel_cpd_order", "cel_dfs_order", "c
            "cel_makespan_info", "cel_makespan_blocks_info", "cel_makespan_relax", "cel_blevel_info", "cel_policy_iteration",
            "cel_topo_levels_info", "cel_cluster_info",
            "cel_order_place", "cel_comm_sums", "cel_makespan_model", "cel_colocate",
-           "cel_attention", "cel_attention_grad", "cel_attention_grad_scratch", "cel_embed", "cel_embed_grad", "cel_embed_grad_scratch",
+           "cel_attention", "cel_attention_grad", "cel_attention_grad_scratch",
+           "cel_cross_attention", "cel_cross_attention_grad", "cel_cross_attention_grad_scratch", "cel_embed", "cel_embed_grad", "cel_embed_grad_scratch",
            "cel_rotary", "cel_rotary_grad", "cel_dropout", "cel_residual_norm", "cel_residual_norm_grad", "cel_residual_norm_grad_scratch",
            "cel_step_latency", "cel_timing", "cel_kernel_stats", "cel_last_error", "cel_version")
 
@@ -62,6 +63,13 @@ class _Attn(C.Structure):
     _fields_ = [("type", C.c_int32), ("tokens", C.c_int32), ("n_seq", C.c_int32),
                 ("heads", C.c_int32), ("kv_heads", C.c_int32), ("dim", C.c_int32),
                 ("scale", C.c_float), ("seq_ptr", C.c_void_p),
+                ("q", _Rows), ("k", _Rows), ("v", _Rows)]
+
+
+class _Cross(C.Structure):
+    _fields_ = [("type", C.c_int32), ("tokens", C.c_int32), ("keys", C.c_int32), ("n_seq", C.c_int32),
+                ("heads", C.c_int32), ("kv_heads", C.c_int32), ("dim", C.c_int32),
+                ("scale", C.c_float), ("seq_ptr", C.c_void_p), ("key_ptr", C.c_void_p),
                 ("q", _Rows), ("k", _Rows), ("v", _Rows)]
 
 
@@ -134,7 +142,11 @@ def lib() -> C.CDLL:
         L.cel_attention_grad_scratch.argtypes = [At]
         L.cel_attention_grad_scratch.restype = i64
         L.cel_attention_grad.argtypes = [At, Ro, vp, Ro, vp, Ro, Ro, Ro, vp]
-        Em = C.POINTER(_Embed)
+        Cr, Em = C.POINTER(_Cross), C.POINTER(_Embed)
+        L.cel_cross_attention.argtypes = [Cr, Ro, vp, vp]
+        L.cel_cross_attention_grad_scratch.argtypes = [Cr]
+        L.cel_cross_attention_grad_scratch.restype = i64
+        L.cel_cross_attention_grad.argtypes = [Cr, Ro, vp, Ro, vp, Ro, Ro, Ro, vp]
         L.cel_embed.argtypes = [Em, vp, vp, vp]
         L.cel_embed_grad.argtypes = [Em, vp, vp, i32, vp, vp]
         L.cel_embed_grad_scratch.argtypes = [i64, i64, i64]
@@ -150,7 +162,7 @@ def lib() -> C.CDLL:
                   "cel_makespan",
                   "cel_makespan_noalloc",
                   "cel_cpd_order", "cel_dfs_order", "cel_order_place", "cel_comm_sums", "cel_makespan_model",
-                  "cel_colocate", "cel_attention", "cel_attention_grad", "cel_embed", "cel_embed_grad", "cel_rotary", "cel_rotary_grad",
+                  "cel_colocate", "cel_attention", "cel_attention_grad", "cel_cross_attention", "cel_cross_attention_grad", "cel_embed", "cel_embed_grad", "cel_rotary", "cel_rotary_grad",
                   "cel_dropout", "cel_residual_norm", "cel_residual_norm_grad", "cel_version"):
             getattr(L, f).restype = C.c_int
         L.cel_last_error.argtypes = []
@@ -653,14 +665,14 @@ def _meet(x, y, T, d):
     return True
 
 
-def _attn(fn, q, k, v, seq_ptr, scale):
-    """-> (descriptor, tensors to keep alive)"""
+def _attn(fn, q, k, v, seq_ptr, scale, key_ptr=None):
+    """-> (descriptor, tensors to keep alive).  key_ptr: of keys apart from the queries' tokens."""
     if q.dim() != 3 or k.dim() != 3 or v.dim() != 3 or q.dtype not in (torch.bfloat16, torch.float16) or \
             k.dtype != q.dtype or v.dtype != q.dtype:
         _refuse(f"{fn}: q, k and v are not [tokens, heads, dim] in bfloat16 or in float16")
     T, H, d = q.shape
     shape = k.shape
-    if v.shape != shape or shape[0] != T or shape[2] != d:
+    if v.shape != shape or (shape[0] != T and key_ptr is None) or shape[2] != d:
         _refuse(f"{fn}: shapes q {tuple(q.shape)}, k {tuple(k.shape)}, v {tuple(v.shape)}")
     if seq_ptr.dim() != 1 or seq_ptr.dtype != torch.int32 or seq_ptr.numel() < 1:
         _refuse(f"{fn}: seq_ptr is not int32 [sequences + 1]")
@@ -669,37 +681,35 @@ def _attn(fn, q, k, v, seq_ptr, scale):
     (qv, kv, vv), keep = _views(q, k, v)
     seq_ptr = seq_ptr.contiguous()
     keep.append(seq_ptr)
-    return _Attn(_TYPES[q.dtype], T, seq_ptr.numel() - 1, H, shape[1], d,
-                 (d or 1) ** -0.5 if scale is None else scale, seq_ptr.data_ptr(), qv, kv, vv), keep
+    scale = (d or 1) ** -0.5 if scale is None else scale
+    if key_ptr is None:
+        return _Attn(_TYPES[q.dtype], T, seq_ptr.numel() - 1, H, shape[1], d, scale, seq_ptr.data_ptr(), qv, kv, vv), keep
+    if key_ptr.shape != seq_ptr.shape or key_ptr.dtype != torch.int32:
+        _refuse(f"{fn}: key_ptr is not int32 [sequences + 1] as seq_ptr")
+    if shape[0] >= 1 << 31:
+        _refuse(f"{fn}: {shape[0]} keys")
+    key_ptr = key_ptr.contiguous()
+    keep.append(key_ptr)
+    return _Cross(_TYPES[q.dtype], T, shape[0], seq_ptr.numel() - 1, H, shape[1], d, scale, seq_ptr.data_ptr(), key_ptr.data_ptr(),
+                  qv, kv, vv), keep
 
 
-def attention(q, k, v, seq_ptr, scale=None):
-    """Causal attention over a packed batch: sequence s is the tokens seq_ptr[s] ..
-    seq_ptr[s + 1] - 1 (int32, on the device), a token sees itself and the earlier tokens of its
-    sequence.  q [T, heads, dim], k and v [T, kv_heads, dim] in bfloat16 or float16, any strides
-    (views of a fused projection are read in place; where a head's values are not contiguous, or an
-    address or stride is no multiple of 16 bytes, the call copies the tensor); heads a multiple of
-    kv_heads, dim a multiple of 8 up to 128; scale: of the scores, 1 / sqrt(dim) by default.
-    -> (out [T, heads, dim], lse float32 [heads, T]); tokens of no sequence have 0 and -inf."""
-    index = _device_of("attention", q=q, k=k, v=v, seq_ptr=seq_ptr)
+def _attention(fn, q, k, v, scale, *ptrs):
+    index = _device_of(fn, q=q, k=k, v=v, **dict(zip(("seq_ptr", "key_ptr"), ptrs)))
     with _on(index):
-        a, keep = _attn("attention", q, k, v, seq_ptr, scale)
+        a, keep = _attn(fn, q, k, v, ptrs[0], scale, *ptrs[1:])
         out = torch.empty(q.shape, dtype=q.dtype, device=q.device)
         lse = torch.empty((a.heads, a.tokens), dtype=torch.float32, device=q.device)
         rows = _Rows(out.data_ptr(), a.heads * a.dim, a.dim)
-        _check(lib().cel_attention(C.byref(a), C.byref(rows), lse.data_ptr(), _raw_stream(index)))
+        call = lib().cel_attention if len(ptrs) == 1 else lib().cel_cross_attention
+        _check(call(C.byref(a), C.byref(rows), lse.data_ptr(), _raw_stream(index)))
     return out, lse
 
 
-def attention_grad(dout, q, k, v, out, lse, seq_ptr, scale=None, grads=None):
-    """The gradient of attention() at dout [T, heads, dim], with its out and lse.
-    -> (dq, dk, dv) as q, k, v are shaped.  grads: three tensors to write them to (for instance views
-    of one fused gradient; values contiguous, addresses and strides multiples of 16 bytes; no memory
-    shared with an input, with each other or within one).  The same inputs give the same bits."""
-    fn = "attention_grad"
-    index = _device_of(fn, q=q, k=k, v=v, seq_ptr=seq_ptr, dout=dout, out=out, lse=lse)
+def _attention_grad(fn, dout, q, k, v, out, lse, scale, grads, *ptrs):
+    index = _device_of(fn, q=q, k=k, v=v, dout=dout, out=out, lse=lse, **dict(zip(("seq_ptr", "key_ptr"), ptrs)))
     with _on(index):
-        a, keep = _attn(fn, q, k, v, seq_ptr, scale)
+        a, keep = _attn(fn, q, k, v, ptrs[0], scale, *ptrs[1:])
         for name, t in (("dout", dout), ("out", out)):
             if t.shape != q.shape or t.dtype != q.dtype:
                 _refuse(f"{fn}: {name} is {tuple(t.shape)} {t.dtype}, not as q")
@@ -720,27 +730,72 @@ def attention_grad(dout, q, k, v, out, lse, seq_ptr, scale=None, grads=None):
             if view is None and t.numel():
                 _refuse(f"{fn}: {name} cannot be written in place: {tuple(t.shape)} {t.dtype}, strides {t.stride()}")
             views.append(view or _Rows())
-        if given and a.tokens:
-            T, d, heads = a.tokens, a.dim, (a.heads, a.kv_heads, a.kv_heads)
-            blocks = [_block(x, T, n, d) for x, n in zip(views, heads)]
-            others = [(name, _block(x, T, n, d)) for name, x, n in zip(
-                ("q", "k", "v", "out", "dout"), (a.q, a.k, a.v, ov, gv), heads + (heads[0], heads[0]))]
-            first, last = min(x[0] for x in blocks), max(x[1] for x in blocks)
-            others = [y for y in others if y[1][0] < last and first < y[1][1]]
-            for name, x in zip(("dq", "dk", "dv"), blocks):
-                if _folded(x, T, d):
-                    _refuse(f"{fn}: values of {name} share memory")
-                for other, y in others:
-                    if _meet(x, y, T, d):
-                        _refuse(f"{fn}: {name} shares memory with {other}")
-                others.append((name, x))
-        size = lib().cel_attention_grad_scratch(C.byref(a))
+        if given:
+            _grads_apart(fn, a, views, (gv, ov), k.shape[0])
+        scratch_of, call = (lib().cel_attention_grad_scratch, lib().cel_attention_grad) if len(ptrs) == 1 else (
+            lib().cel_cross_attention_grad_scratch, lib().cel_cross_attention_grad)
+        size = scratch_of(C.byref(a))
         if size < 0:
             _check(size)
         scratch = torch.empty(size, dtype=torch.uint8, device=q.device)
-        _check(lib().cel_attention_grad(C.byref(a), C.byref(ov), lse.data_ptr(), C.byref(gv), scratch.data_ptr(), *map(C.byref, views),
-                                        _raw_stream(index)))
+        _check(call(C.byref(a), C.byref(ov), lse.data_ptr(), C.byref(gv), scratch.data_ptr() or None, *map(C.byref, views),
+                    _raw_stream(index)))
     return tuple(grads)
+
+
+def _grads_apart(fn, a, views, of_q, U):
+    """Refuses gradients that share memory within themselves, with each other or with an input."""
+    T, d, heads, tokens = a.tokens, a.dim, (a.heads, a.kv_heads, a.kv_heads), (a.tokens, U, U)
+    blocks = [(name, t, _block(x, t, n, d)) for name, x, t, n in zip(("dq", "dk", "dv"), views, tokens, heads) if t]
+    others = [(name, _block(x, t, n, d)) for name, x, t, n in zip(
+        ("q", "k", "v", "dout", "out"), (a.q, a.k, a.v, *of_q), tokens + (T, T), heads + (heads[0], heads[0])) if t]
+    if not blocks:
+        return
+    first, last = min(x[0] for _, _, x in blocks), max(x[1] for _, _, x in blocks)
+    others = [y for y in others if y[1][0] < last and first < y[1][1]]
+    for name, t, x in blocks:
+        if _folded(x, t, d):
+            _refuse(f"{fn}: values of {name} share memory")
+        for other, y in others:
+            if _meet(x, y, max(T, U), d):
+                _refuse(f"{fn}: {name} shares memory with {other}")
+        others.append((name, x))
+
+
+def attention(q, k, v, seq_ptr, scale=None):
+    """Causal attention over a packed batch: sequence s is the tokens seq_ptr[s] ..
+    seq_ptr[s + 1] - 1 (int32, on the device), a token sees itself and the earlier tokens of its
+    sequence.  q [T, heads, dim], k and v [T, kv_heads, dim] in bfloat16 or float16, any strides
+    (views of a fused projection are read in place; where a head's values are not contiguous, or an
+    address or stride is no multiple of 16 bytes, the call copies the tensor); heads a multiple of
+    kv_heads, dim a multiple of 8 up to 128; scale: of the scores, 1 / sqrt(dim) by default.
+    -> (out [T, heads, dim], lse float32 [heads, T]); tokens of no sequence have 0 and -inf."""
+    return _attention("attention", q, k, v, scale, seq_ptr)
+
+
+def attention_grad(dout, q, k, v, out, lse, seq_ptr, scale=None, grads=None):
+    """The gradient of attention() at dout [T, heads, dim], with its out and lse.
+    -> (dq, dk, dv) as q, k, v are shaped.  grads: three tensors to write them to (for instance views
+    of one fused gradient; values contiguous, addresses and strides multiples of 16 bytes; no memory
+    shared with an input, with each other or within one).  The same inputs give the same bits."""
+    return _attention_grad("attention_grad", dout, q, k, v, out, lse, scale, grads, seq_ptr)
+
+
+def cross_attention(q, k, v, seq_ptr, key_ptr, scale=None):
+    """Attention to other states, an encoder's for instance: q [T, heads, dim] of a packed batch as in
+    attention(), k and v [U, kv_heads, dim] of the states, packed alike; sequence s is the tokens seq_ptr[s] ..
+    seq_ptr[s + 1] - 1 and the states key_ptr[s] .. key_ptr[s + 1] - 1 (int32, on the device, of one length),
+    and each of its tokens sees all of its states.  Types, strides, heads, dim and scale as there.
+    -> (out [T, heads, dim], lse float32 [heads, T]); tokens of no sequence, or of one without states, have 0
+    and -inf.  Tokens are taken 128 at a time, over all the states of their sequences: made for as many
+    tokens as training has, not for single ones."""
+    return _attention("cross_attention", q, k, v, scale, seq_ptr, key_ptr)
+
+
+def cross_attention_grad(dout, q, k, v, out, lse, seq_ptr, key_ptr, scale=None, grads=None):
+    """The gradient of cross_attention() at dout [T, heads, dim], with its out and lse.
+    -> (dq, dk, dv) as q, k, v are shaped; grads as in attention_grad().  The same inputs give the same bits."""
+    return _attention_grad("cross_attention_grad", dout, q, k, v, out, lse, scale, grads, seq_ptr, key_ptr)
 
 
 def _embed(fn, what, rows, ids, vocab, scale):

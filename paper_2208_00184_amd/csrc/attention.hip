@@ -1,6 +1,8 @@
-// Causal attention over a packed batch with grouped heads, and its gradient.
+// Attention over a packed batch with grouped heads, and its gradient: causal over
+// the batch itself, or (CROSS) to the states of an encoder, packed alike.
 //
-// Token i of a sequence sees the tokens j <= i of the same sequence:
+// Token i of a sequence sees the tokens j <= i of the same sequence, or all of
+// the states that belong to its sequence:
 //   s_ij = scale <q_i, k_j>,  lse_i = log sum_j exp s_ij,  p_ij = exp(s_ij - lse_i)
 //   o_i = sum_j p_ij v_j
 // and backwards, with D_i = <do_i, o_i>:
@@ -117,12 +119,12 @@ struct Rows {  // a [tokens][heads][dim] view, strides in elements
 };
 struct AttnArgs {
   Rows q, k, v, out, dout, dq, dk, dv;
-  const int32_t *ptr;
-  int32_t S, T, H, K, d, tiles;
+  const int32_t *ptr, *k_ptr;  // of the rows; of the keys where they are others
+  int32_t S, T, U, H, K, d, tiles;  // U: keys
   float *lse;
   float *rows;  // the backward pass's scratch: lse in units of log 2 less kPUp, D, each [heads][tokens]
   float *part;  // and behind it, where a key/value head's query heads are dealt out to `parts` workgroups, dk
-                // and dv of each part, [parts][2][tokens][kv_heads][dim]
+                // and dv of each part, [parts][2][keys][kv_heads][dim]
   int32_t parts;
   float scale;
 };
@@ -263,22 +265,23 @@ __device__ __forceinline__ void careful_product(const char *lds, acc16 (&acc)[NB
     }
 }
 
-// The sequence that holds a token: its tokens [a, b), empty if there is none.
-// Whatever ptr holds, the range lies within the buffer.
-__device__ inline void sequence_of(const AttnArgs &A, int i, int &a, int &b) {
+// The sequence that holds token i of n: its tokens [a, b) of m, as ptr or, of the other
+// side, `other` has them; empty if there is none.  Whatever they hold, the range lies within the buffer.
+__device__ inline void sequence_of(const int32_t *ptr, int S, int n, const int32_t *other, int m, int i, int &a, int &b) {
   a = b = 0;
-  if (i >= A.T) return;
-  int lo = 0, hi = A.S;  // the last s with ptr[s] <= i, if any
+  if (i >= n) return;
+  int lo = 0, hi = S;  // the last s with ptr[s] <= i, if any
   while (lo < hi) {
     const int mid = (lo + hi + 1) >> 1;
-    if (A.ptr[mid] <= i) lo = mid;
+    if (ptr[mid] <= i) lo = mid;
     else hi = mid - 1;
   }
-  if (lo >= A.S) return;
-  const int from = A.ptr[lo], to = A.ptr[lo + 1];
+  if (lo >= S) return;
+  int from = ptr[lo], to = ptr[lo + 1];
   if (from > i || to <= i) return;
+  if (other != ptr) from = other[lo], to = other[lo + 1];
   a = from < 0 ? 0 : from;
-  b = to > A.T ? A.T : to;
+  b = to > m ? m : to;
 }
 
 __device__ inline int wave_min(int x) {
@@ -363,13 +366,16 @@ struct Reach {
   __device__ int steps() const { return to < from ? 0 : (to - from) / kStep + 1; }
 };
 // forward: the keys that token i sees; else the rows that see it.
+template <bool CROSS>
 __device__ inline Reach reach_of(const AttnArgs &A, int i, bool forward, int (*s_reach)[kWaves], int wave) {
   int first, last;
-  sequence_of(A, i, first, last);
+  if constexpr (!CROSS) sequence_of(A.ptr, A.S, A.T, A.ptr, A.T, i, first, last);
+  else if (forward) sequence_of(A.ptr, A.S, A.T, A.k_ptr, A.U, i, first, last);
+  else sequence_of(A.k_ptr, A.S, A.U, A.ptr, A.T, i, first, last);
   Reach R;
   const bool real = last > first;
-  R.lo = !real ? INT32_MAX : forward ? first : i;
-  R.hi = !real ? -1 : forward ? i : last - 1;
+  R.lo = !real ? INT32_MAX : CROSS || forward ? first : i;
+  R.hi = !real ? -1 : !CROSS && forward ? i : last - 1;
   R.any_lo = wave_min(R.lo), R.any_hi = wave_max(R.hi);
   R.all_lo = wave_max(real ? R.lo : -1), R.all_hi = wave_min(real ? R.hi : INT32_MAX);
   s_reach[0][wave] = R.any_lo;
@@ -478,7 +484,7 @@ __device__ __forceinline__ void mask(acc16 &x, int t, int lo, int hi, float by, 
 // over 8: 0.51 ms, 1.07 PFLOP/s, matrix cores 55 % busy, no bank conflicts.
 // 4 sequences of 1,024, 16 heads of 64: 23 us, the 16 steps of a sequence's last
 // tile (0.8 us each at 64 dimensions, 1.1 at 128) behind some 7 us of start and end.
-template <class T, int DP, int DC, int G, bool CAREFUL>
+template <class T, int DP, int DC, int G, bool CROSS, bool CAREFUL>
 __device__ __forceinline__ bool attention_tile(const AttnArgs &A, char *s_k0, char *s_k1, char *s_v0, char *s_v1,
                                                int (*s_reach)[kWaves]) {
   constexpr int kTile = kStep * DP * 2;
@@ -488,7 +494,7 @@ __device__ __forceinline__ bool attention_tile(const AttnArgs &A, char *s_k0, ch
   const Item item = item_of(blockIdx.x, gridDim.x, A.H);
   const int head = item.unit, tile = A.tiles - 1 - item.tile, kvh = head / (A.H / A.K);
   const int i = tile * kBlock + wave * kRows + (lane & 31);  // this lane's row
-  const Reach R = reach_of(A, i, true, s_reach + 2 * group, wave);
+  const Reach R = reach_of<CROSS>(A, i, true, s_reach + 2 * group, wave);
   u32x4 q[DC / 16];
   load_rows(q, A.q, head, i, A.T, A.d, lane);
   const float c = A.scale * kLog2e, far = 8.f / c;
@@ -615,13 +621,13 @@ __device__ __forceinline__ bool attention_tile(const AttnArgs &A, char *s_k0, ch
 // same two waves on every SIMD; it is taken where each workgroup has a compute unit
 // to itself, so that the longest chain is the time (see split_keys).
 #define CEL_TILE_KERNEL(kernel, tile, a0, a1, b0, b1)                                                      \
-  template <class T, int DP, int DC, int G>                                                                \
+  template <class T, int DP, int DC, int G, bool CROSS>                                                    \
   __global__ void __launch_bounds__(G *kWaves * 64, 2) kernel(AttnArgs A) {                                \
     constexpr int kTile = G * kStep * DP * 2;                                                              \
     __shared__ __align__(16) char a0[kTile], a1[kTile], b0[kTile], b1[kTile];                              \
     __shared__ int s_reach[2 * G][kWaves];                                                                 \
-    if (!tile<T, DP, DC, G, false>(A, a0, a1, b0, b1, s_reach))                                            \
-      (void)tile<T, DP, DC, G, true>(A, a0, a1, b0, b1, s_reach);                                          \
+    if (!tile<T, DP, DC, G, CROSS, false>(A, a0, a1, b0, b1, s_reach))                                     \
+      (void)tile<T, DP, DC, G, CROSS, true>(A, a0, a1, b0, b1, s_reach);                                   \
   }
 CEL_TILE_KERNEL(k_attention, attention_tile, s_k0, s_k1, s_v0, s_v1)
 
@@ -638,7 +644,7 @@ CEL_TILE_KERNEL(k_attention, attention_tile, s_k0, s_k1, s_v0, s_v1)
 // its sums run over the other axis than dk's and dv's: joined, one side would be
 // added up in memory, by atomics in no fixed order.  The price is that scores and
 // their gradients are made twice, 7 products where 5 would do.
-template <class T, int DP, int DC, int G, bool CAREFUL>
+template <class T, int DP, int DC, int G, bool CROSS, bool CAREFUL>
 __device__ __forceinline__ bool dq_tile(const AttnArgs &A, char *s_k0, char *s_k1, char *s_v0, char *s_v1,
                                         int (*s_reach)[kWaves]) {
   constexpr int kTile = kStep * DP * 2;
@@ -648,7 +654,7 @@ __device__ __forceinline__ bool dq_tile(const AttnArgs &A, char *s_k0, char *s_k
   const Item item = item_of(blockIdx.x, gridDim.x, A.H);
   const int head = item.unit, tile = A.tiles - 1 - item.tile, kvh = head / (A.H / A.K);
   const int first = tile * kBlock + wave * kRows, i = first + (lane & 31);
-  const Reach R = reach_of(A, i, true, s_reach + 2 * group, wave);
+  const Reach R = reach_of<CROSS>(A, i, true, s_reach + 2 * group, wave);
   u32x4 q[DC / 16], g[DC / 16];
   load_rows(q, A.q, head, i, A.T, A.d, lane);
   load_rows(g, A.dout, head, i, A.T, A.d, lane);
@@ -665,6 +671,7 @@ __device__ __forceinline__ bool dq_tile(const AttnArgs &A, char *s_k0, char *s_k
     }
     D = half_sum(D);
   }
+  const bool few = CROSS && __any(R.real() && R.hi - R.lo < kStep);
   const float lse2 = R.real() ? A.lse[(int64_t)head * A.T + i] * kLog2e : INFINITY;
   const float c = A.scale * kLog2e;
   const Lane<DP> L(lane);
@@ -687,8 +694,10 @@ __device__ __forceinline__ bool dq_tile(const AttnArgs &A, char *s_k0, char *s_k
       const bool masked = R.masks(a);
       const int lo = R.lo - a, hi = R.hi - a;
       // All of a row's keys, of which it is itself the last: not in tiles before the wave's own rows.
-      const bool inside = a + kStep > first && R.real() && lo >= 0 && hi < kStep;
-      if (a + kStep > first && __any(inside)) {
+      // Keys apart from the rows lie anywhere, and are looked for where a row of the wave has few enough.
+      const bool looked = CROSS ? few : a + kStep > first;
+      const bool inside = looked && R.real() && lo >= 0 && hi < kStep;
+      if (looked && __any(inside)) {
         float sum = 0.f;
 #pragma unroll
         for (int t = 0; t < 2; t++) {
@@ -801,7 +810,7 @@ template <class T, int N>
 __device__ __forceinline__ void store_sums(const AttnArgs &A, const Rows &x, int which, int kvh, int part, int j,
                                            const acc4 (&acc)[N], int n0, float by, int lane) {
   char *p = x.p + 2 * ((int64_t)j * x.row + (int64_t)kvh * x.head);
-  float *q = A.part + ((((int64_t)part * 2 + which) * A.T + j) * A.K + kvh) * A.d;
+  float *q = A.part + ((((int64_t)part * 2 + which) * A.U + j) * A.K + kvh) * A.d;
 #pragma unroll
   for (int n = 0; n < N; n++) {
     const int c = 32 * n0 + 16 * n + 4 * (lane >> 4);
@@ -940,7 +949,7 @@ __device__ __forceinline__ void product16(const char *lds, acc4 (&acc)[NB], cons
 // dk and dv of a tile of 64 tokens of one key/value head: each wave 16 of them,
 // over the query heads and the rows up to the end of the last token's sequence,
 // in that order whatever the launch.
-template <class T, int DP, int DC, bool CAREFUL>
+template <class T, int DP, int DC, bool CROSS, bool CAREFUL>
 __device__ __forceinline__ bool dkv_tile(const AttnArgs &A, char *s_q0, char *s_q1, char *s_g0, char *s_g1, float *s_r0,
                                          float *s_r1, int (*s_reach)[kWaves]) {
   constexpr int NB = CAREFUL ? 2 : DC / 16, KK = DC / 32;  // sums a pass holds, see CEL_TILE_KERNEL
@@ -950,10 +959,10 @@ __device__ __forceinline__ bool dkv_tile(const AttnArgs &A, char *s_q0, char *s_
   const int j = item.tile * kKeyBlock + wave * kKeys + (lane & 15);  // this lane's key
   int head0, heads;
   heads_of(A, kvh, part, head0, heads);
-  const Reach R = reach_of(A, j, false, s_reach, wave);
+  const Reach R = reach_of<CROSS>(A, j, false, s_reach, wave);
   u32x4 k[KK], v[KK];
-  load_rows16(k, A.k, kvh, j, A.T, A.d, lane);
-  load_rows16(v, A.v, kvh, j, A.T, A.d, lane);
+  load_rows16(k, A.k, kvh, j, A.U, A.d, lane);
+  load_rows16(v, A.v, kvh, j, A.U, A.d, lane);
   const float c = A.scale * kLog2e;
   const Lane16<DP> L(lane);
   const Stager<DP, Swz16<DP>> qs(A.q, A.d, tid), gs(A.dout, A.d, tid);
@@ -1047,7 +1056,7 @@ __device__ __forceinline__ bool dkv_tile(const AttnArgs &A, char *s_q0, char *s_
 #pragma unroll
       for (int r = 0; r < 4; r++) odd |= !(fabsf(dk[n][r] * by) < INFINITY) || !(fabsf(dv[n][r]) < INFINITY);
     if (!CAREFUL && __syncthreads_or(R.real() && odd)) return false;
-    if (j < A.T) {
+    if (j < A.U) {
       if (!R.real()) clear();
       store_sums<T>(A, A.dk, 0, kvh, part, j, dk, n0, by, lane);
       store_sums<T>(A, A.dv, 1, kvh, part, j, dv, n0, power(-kPUp<T>), lane);
@@ -1059,7 +1068,7 @@ __device__ __forceinline__ bool dkv_tile(const AttnArgs &A, char *s_q0, char *s_
   for (int n0 = 0; n0 < DC / 32; n0++) (void)pass(n0);
   return true;
 }
-template <class T, int DP, int DC>
+template <class T, int DP, int DC, bool CROSS>
 // Beyond 64 dimensions the bound leaves the compiler more registers than two waves
 // have: it takes 237 of their 256 and keeps the reads of LDS ahead of their use,
 // which it gives up under the tighter bound (8,192 tokens, 32 heads of 128 over 8:
@@ -1069,15 +1078,15 @@ __global__ void __launch_bounds__(kWaves * 64, DC > 64 ? 1 : 2) k_attention_dkv(
   __shared__ __align__(16) char s_q0[kTile], s_q1[kTile], s_g0[kTile], s_g1[kTile];
   __shared__ __align__(16) float s_r0[2 * kStep], s_r1[2 * kStep];  // lse and D of the rows
   __shared__ int s_reach[2][kWaves];
-  if (!dkv_tile<T, DP, DC, false>(A, s_q0, s_q1, s_g0, s_g1, s_r0, s_r1, s_reach))
-    (void)dkv_tile<T, DP, DC, true>(A, s_q0, s_q1, s_g0, s_g1, s_r0, s_r1, s_reach);
+  if (!dkv_tile<T, DP, DC, CROSS, false>(A, s_q0, s_q1, s_g0, s_g1, s_r0, s_r1, s_reach))
+    (void)dkv_tile<T, DP, DC, CROSS, true>(A, s_q0, s_q1, s_g0, s_g1, s_r0, s_r1, s_reach);
 }
 
 // dk and dv as the sums of their parts, in the order of the query heads.  Bound by
 // memory: 2 parts of 8,192 tokens of 8 heads of 128, 101 MB, in 26 us (3.9 TB/s).
 template <class T>
 __global__ void __launch_bounds__(256) k_attention_join(AttnArgs A) {
-  const int64_t n = (int64_t)A.T * A.K * A.d, at = ((int64_t)blockIdx.x * 256 + threadIdx.x) * 4;
+  const int64_t n = (int64_t)A.U * A.K * A.d, at = ((int64_t)blockIdx.x * 256 + threadIdx.x) * 4;
   if (at >= n) return;
   const int c = (int)(at % A.d), kvh = (int)(at / A.d % A.K);
   const int64_t t = at / A.d / A.K;
@@ -1101,9 +1110,9 @@ int check_rows(const cel_rows *x, const cel_attn *a, const char *fn, const char 
   return CEL_OK;
 }
 // A launch has fewer than 2^32 threads: that many workgroups at most, for tiles of `rows` tokens.
-int check_grid(const cel_attn *a, int rows, const char *fn) {
-  if (((int64_t)a->tokens + rows - 1) / rows * a->heads * (kWaves * 64) > UINT32_MAX)
-    return set_error(CEL_E_ARG, "%s: %d tokens of %d heads", fn, a->tokens, a->heads);
+int check_grid(const cel_attn *a, int32_t tokens, int rows, const char *fn) {
+  if (((int64_t)tokens + rows - 1) / rows * a->heads * (kWaves * 64) > UINT32_MAX)
+    return set_error(CEL_E_ARG, "%s: %d tokens of %d heads", fn, tokens, a->heads);
   return CEL_OK;
 }
 int check_attn(const cel_attn *a, const char *fn) {
@@ -1118,7 +1127,7 @@ int check_attn(const cel_attn *a, const char *fn) {
   const float c = a->scale * kLog2e;  // of the exponents, to the base of 2
   if (!(c > 0.f) || !std::isfinite(c) || !std::isfinite(8.f / c))
     return set_error(CEL_E_ARG, "%s: scale %g is not positive and finite, in units of log 2 too", fn, (double)a->scale);
-  return check_grid(a, kBlock, fn);  // the forward pass's and dq's launch
+  return check_grid(a, a->tokens, kBlock, fn);  // the forward pass's and dq's launch
 }
 // Into how many workgroups a tile of keys deals out the query heads that share
 // them: as many as bring six workgroups to each of the 256 compute units (the
@@ -1126,8 +1135,8 @@ int check_attn(const cel_attn *a, const char *fn) {
 // same number of heads but the last.  (Against four: 37 ragged sequences, 24 heads of 80
 // over 4: 184 us with the join against 208; 8,192 tokens, 32 heads of 128 over 8: 1.15 ms against
 // 1.20; but 4 sequences of 1,024, 32 heads over 8: 145 against 131 us.)
-int parts_of(const cel_attn *a) {
-  const int64_t group = a->heads / a->kv_heads, tiles = ((int64_t)a->tokens + kKeyBlock - 1) / kKeyBlock;
+int parts_of(const cel_attn *a, int32_t keys) {
+  const int64_t group = a->heads / a->kv_heads, tiles = ((int64_t)keys + kKeyBlock - 1) / kKeyBlock;
   const int64_t per = std::max<int64_t>(1, group * tiles * a->kv_heads / 1536);
   return per >= group ? 1 : (int)((group + per - 1) / per);
 }
@@ -1139,7 +1148,7 @@ AttnArgs args_of(const cel_attn *a) {
   AttnArgs A{};
   A.q = rows_of(&a->q), A.k = rows_of(&a->k), A.v = rows_of(&a->v);
   A.ptr = a->seq_ptr;
-  A.S = a->n_seq, A.T = a->tokens, A.H = a->heads, A.K = a->kv_heads, A.d = a->dim;
+  A.S = a->n_seq, A.T = A.U = a->tokens, A.H = a->heads, A.K = a->kv_heads, A.d = a->dim;
   A.tiles = (a->tokens + kBlock - 1) / kBlock;
   A.scale = a->scale;
   return A;
@@ -1155,7 +1164,7 @@ AttnArgs args_of(const cel_attn *a) {
 // long its sequences are only the device knows.  Where all are short the second group
 // has nothing to do and costs up to 1.4 us (8 heads of 64, 16 sequences of 128: forward 10.2 -> 10.6,
 // dq 13.0 -> 14.2; 600 of 1: 10.6 -> 10.7 and 14.4 -> 15.0; 4 of 512: 14.7 -> 13.7 and 18.0 -> 18.1).
-bool split_keys(const AttnArgs &A) { return (int64_t)A.tiles * A.H <= 256 && A.T >= 512; }
+bool split_keys(const AttnArgs &A) { return (int64_t)A.tiles * A.H <= 256 && A.U >= 512; }
 
 // kernel<T, DP, DC, ...> for the call's type and dimension: rows are staged DP
 // wide (a power of two, for the chunks' order), products run over DC dimensions.
@@ -1170,42 +1179,114 @@ void by_dim(int d, F f) {
   else if (d <= 96) f(c128{}, c96{});
   else f(c128{}, c128{});
 }
-template <class T>
+template <class T, bool CROSS>
 void launch_attention(const AttnArgs &A, hipStream_t s) {
   KTimer kt(s, "k_attention");
   by_dim(A.d, [&](auto dp, auto dc) {
     constexpr int DP = decltype(dp)::value, DC = decltype(dc)::value;
     const int grid = A.tiles * A.H;
-    if (split_keys(A)) k_attention<T, DP, DC, 2><<<grid, 2 * kWaves * 64, 0, s>>>(A);
-    else k_attention<T, DP, DC, 1><<<grid, kWaves * 64, 0, s>>>(A);
+    if (split_keys(A)) k_attention<T, DP, DC, 2, CROSS><<<grid, 2 * kWaves * 64, 0, s>>>(A);
+    else k_attention<T, DP, DC, 1, CROSS><<<grid, kWaves * 64, 0, s>>>(A);
   });
 }
-template <class T>
+template <class T, bool CROSS>
 void launch_dq(const AttnArgs &A, hipStream_t s) {
   KTimer kt(s, "k_attention_dq");
   by_dim(A.d, [&](auto dp, auto dc) {
     constexpr int DP = decltype(dp)::value, DC = decltype(dc)::value;
     const int grid = A.tiles * A.H;
     if constexpr (DC <= 64) {  // beyond, two groups' dq does not fit in the registers (60 -> 126 us at 2,048 tokens)
-      if (split_keys(A)) return k_attention_dq<T, DP, DC, 2><<<grid, 2 * kWaves * 64, 0, s>>>(A);
+      if (split_keys(A)) return k_attention_dq<T, DP, DC, 2, CROSS><<<grid, 2 * kWaves * 64, 0, s>>>(A);
     }
-    k_attention_dq<T, DP, DC, 1><<<grid, kWaves * 64, 0, s>>>(A);
+    k_attention_dq<T, DP, DC, 1, CROSS><<<grid, kWaves * 64, 0, s>>>(A);
   });
 }
-template <class T>
+template <class T, bool CROSS>
 void launch_dkv(const AttnArgs &A, hipStream_t s) {
   {
     KTimer kt(s, "k_attention_dkv");
     by_dim(A.d, [&](auto dp, auto dc) {
-      k_attention_dkv<T, decltype(dp)::value, decltype(dc)::value>
-          <<<(A.T + kKeyBlock - 1) / kKeyBlock * A.K * A.parts, kWaves * 64, 0, s>>>(A);
+      k_attention_dkv<T, decltype(dp)::value, decltype(dc)::value, CROSS>
+          <<<(A.U + kKeyBlock - 1) / kKeyBlock * A.K * A.parts, kWaves * 64, 0, s>>>(A);
     });
   }
   if (A.parts > 1) {
     KTimer kt(s, "k_attention_join");
-    k_attention_join<T><<<(unsigned)(((int64_t)A.T * A.K * A.d / 4 + 255) / 256), 256, 0, s>>>(A);
+    k_attention_join<T><<<(unsigned)(((int64_t)A.U * A.K * A.d / 4 + 255) / 256), 256, 0, s>>>(A);
   }
 }
+
+// What the two kinds of attention share of their checks and launches; k_ptr and
+// keys are the batch's own where it is causal.
+struct Keys {
+  bool cross;
+  const int32_t *ptr;
+  int32_t n;
+};
+int check_keys(const cel_attn *a, const Keys &k, const char *fn) {
+  if (k.n < 0 || k.n > INT32_MAX - 4096) return set_error(CEL_E_ARG, "%s: %d keys", fn, k.n);
+  return CEL_OK;
+}
+int64_t grad_scratch(const cel_attn *a, const Keys &k, const char *fn) {
+  CEL_TRY(check_attn(a, fn));
+  CEL_TRY(check_keys(a, k, fn));
+  CEL_TRY(check_grid(a, k.n, kKeyBlock, fn));
+  const int parts = parts_of(a, k.n);
+  return 4 * (part_at(a) + (parts > 1 ? 2 * (int64_t)parts * k.n * a->kv_heads * a->dim : 0));
+}
+template <class F>
+int by_kind(const cel_attn *a, const Keys &k, F launch) {
+  if (a->type == CEL_BF16) k.cross ? launch(__bf16{}, std::true_type{}) : launch(__bf16{}, std::false_type{});
+  else k.cross ? launch(_Float16{}, std::true_type{}) : launch(_Float16{}, std::false_type{});
+  CEL_HIP(hipGetLastError());
+  return CEL_OK;
+}
+int attention(const cel_attn *a, const Keys &k, const cel_rows *out, float *lse, const char *fn, hipStream_t s) {
+  int rc = check_attn(a, fn);
+  if (rc || (rc = check_keys(a, k, fn))) return rc;
+  if (!a->seq_ptr || !k.ptr) return set_error(CEL_E_ARG, "%s: seq_ptr is NULL", fn);
+  if (a->tokens == 0) return CEL_OK;
+  if ((rc = check_rows(&a->q, a, fn, "q")) || (k.n && ((rc = check_rows(&a->k, a, fn, "k")) || (rc = check_rows(&a->v, a, fn, "v")))) ||
+      (rc = check_rows(out, a, fn, "out")))
+    return rc;
+  if (!lse) return set_error(CEL_E_ARG, "%s: lse is NULL", fn);
+  AttnArgs A = args_of(a);
+  A.k_ptr = k.ptr, A.U = k.n;
+  A.out = rows_of(out);
+  A.lse = lse;
+  return by_kind(a, k, [&](auto t, auto cross) { launch_attention<decltype(t), decltype(cross)::value>(A, s); });
+}
+int attention_grad(const cel_attn *a, const Keys &k, const cel_rows *out, const float *lse, const cel_rows *dout, void *scratch_,
+                   const cel_rows *dq, const cel_rows *dk, const cel_rows *dv, const char *fn, hipStream_t s) {
+  int rc = check_attn(a, fn);
+  if (rc || (rc = check_keys(a, k, fn)) || (rc = check_grid(a, k.n, kKeyBlock, fn))) return rc;
+  if (!a->seq_ptr || !k.ptr) return set_error(CEL_E_ARG, "%s: seq_ptr is NULL", fn);
+  if (a->tokens == 0 && k.n == 0) return CEL_OK;
+  if ((a->tokens && ((rc = check_rows(&a->q, a, fn, "q")) || (rc = check_rows(out, a, fn, "out")) ||
+                     (rc = check_rows(dout, a, fn, "dout")) || (rc = check_rows(dq, a, fn, "dq")))) ||
+      (k.n && ((rc = check_rows(&a->k, a, fn, "k")) || (rc = check_rows(&a->v, a, fn, "v")) ||
+               (rc = check_rows(dk, a, fn, "dk")) || (rc = check_rows(dv, a, fn, "dv")))))
+    return rc;
+  float *scratch = static_cast<float *>(scratch_);
+  if ((a->tokens && !lse) || (!scratch && grad_scratch(a, k, fn))) return set_error(CEL_E_ARG, "%s: lse or scratch is NULL", fn);
+  AttnArgs A = args_of(a);
+  A.k_ptr = k.ptr, A.U = k.n;
+  if (a->tokens) A.out = rows_of(out), A.dout = rows_of(dout), A.dq = rows_of(dq);
+  if (k.n) A.dk = rows_of(dk), A.dv = rows_of(dv);
+  A.lse = const_cast<float *>(lse);
+  A.rows = scratch;
+  A.parts = parts_of(a, k.n);
+  A.part = scratch + part_at(a);
+  return by_kind(a, k, [&](auto t, auto cross) {
+    if (A.T) launch_dq<decltype(t), decltype(cross)::value>(A, s);
+    if (A.U) launch_dkv<decltype(t), decltype(cross)::value>(A, s);
+  });
+}
+// A cross attention's descriptor in the form of the other's.
+cel_attn rows_part(const cel_cross_attn *a) {
+  return cel_attn{a->type, a->tokens, a->n_seq, a->heads, a->kv_heads, a->dim, a->scale, a->seq_ptr, a->q, a->k, a->v};
+}
+Keys own_keys(const cel_attn *a) { return Keys{false, a ? a->seq_ptr : nullptr, a ? a->tokens : 0}; }
 
 }  // namespace
 }  // namespace cel
@@ -1213,62 +1294,34 @@ void launch_dkv(const AttnArgs &A, hipStream_t s) {
 using namespace cel;
 
 extern "C" int64_t cel_attention_grad_scratch(const cel_attn *a) {
-  const char *fn = "cel_attention_grad_scratch";
-  CEL_TRY(check_attn(a, fn));
-  CEL_TRY(check_grid(a, kKeyBlock, fn));
-  const int parts = parts_of(a);
-  return 4 * (part_at(a) + (parts > 1 ? 2 * (int64_t)parts * a->tokens * a->kv_heads * a->dim : 0));
+  return grad_scratch(a, own_keys(a), "cel_attention_grad_scratch");
 }
-
 extern "C" int cel_attention(const cel_attn *a, const cel_rows *out, float *lse, hipStream_t s) {
-  const char *fn = "cel_attention";
-  int rc = check_attn(a, fn);
-  if (rc) return rc;
-  if (!a->seq_ptr) return set_error(CEL_E_ARG, "%s: seq_ptr is NULL", fn);
-  if (a->tokens == 0) return CEL_OK;
-  if ((rc = check_rows(&a->q, a, fn, "q")) || (rc = check_rows(&a->k, a, fn, "k")) ||
-      (rc = check_rows(&a->v, a, fn, "v")) || (rc = check_rows(out, a, fn, "out")))
-    return rc;
-  if (!lse) return set_error(CEL_E_ARG, "%s: lse is NULL", fn);
-  AttnArgs A = args_of(a);
-  A.out = rows_of(out);
-  A.lse = lse;
-  if (a->type == CEL_BF16) launch_attention<__bf16>(A, s);
-  else launch_attention<_Float16>(A, s);
-  CEL_HIP(hipGetLastError());
-  return CEL_OK;
+  return attention(a, own_keys(a), out, lse, "cel_attention", s);
+}
+extern "C" int cel_attention_grad(const cel_attn *a, const cel_rows *out, const float *lse, const cel_rows *dout,
+                                  void *scratch, const cel_rows *dq, const cel_rows *dk, const cel_rows *dv,
+                                  hipStream_t s) {
+  return attention_grad(a, own_keys(a), out, lse, dout, scratch, dq, dk, dv, "cel_attention_grad", s);
 }
 
-extern "C" int cel_attention_grad(const cel_attn *a, const cel_rows *out, const float *lse, const cel_rows *dout,
-                                  void *scratch_, const cel_rows *dq, const cel_rows *dk, const cel_rows *dv,
-                                  hipStream_t s) {
-  const char *fn = "cel_attention_grad";
-  int rc = check_attn(a, fn);
-  if (rc || (rc = check_grid(a, kKeyBlock, fn))) return rc;
-  if (!a->seq_ptr) return set_error(CEL_E_ARG, "%s: seq_ptr is NULL", fn);
-  if (a->tokens == 0) return CEL_OK;
-  if ((rc = check_rows(&a->q, a, fn, "q")) || (rc = check_rows(&a->k, a, fn, "k")) ||
-      (rc = check_rows(&a->v, a, fn, "v")) || (rc = check_rows(out, a, fn, "out")) ||
-      (rc = check_rows(dout, a, fn, "dout")) || (rc = check_rows(dq, a, fn, "dq")) ||
-      (rc = check_rows(dk, a, fn, "dk")) || (rc = check_rows(dv, a, fn, "dv")))
-    return rc;
-  float *scratch = static_cast<float *>(scratch_);
-  if (!lse || !scratch) return set_error(CEL_E_ARG, "%s: lse or scratch is NULL", fn);
-  AttnArgs A = args_of(a);
-  A.out = rows_of(out), A.dout = rows_of(dout), A.dq = rows_of(dq), A.dk = rows_of(dk), A.dv = rows_of(dv);
-  A.lse = const_cast<float *>(lse);
-  A.rows = scratch;
-  A.parts = parts_of(a);
-  A.part = scratch + part_at(a);
-  if (a->type == CEL_BF16) {
-    launch_dq<__bf16>(A, s);
-    CEL_HIP(hipGetLastError());
-    launch_dkv<__bf16>(A, s);
-  } else {
-    launch_dq<_Float16>(A, s);
-    CEL_HIP(hipGetLastError());
-    launch_dkv<_Float16>(A, s);
-  }
-  CEL_HIP(hipGetLastError());
-  return CEL_OK;
+extern "C" int64_t cel_cross_attention_grad_scratch(const cel_cross_attn *a) {
+  const char *fn = "cel_cross_attention_grad_scratch";
+  if (!a) return set_error(CEL_E_ARG, "%s: NULL descriptor", fn);
+  const cel_attn b = rows_part(a);
+  return grad_scratch(&b, Keys{true, a->key_ptr, a->keys}, fn);
+}
+extern "C" int cel_cross_attention(const cel_cross_attn *a, const cel_rows *out, float *lse, hipStream_t s) {
+  const char *fn = "cel_cross_attention";
+  if (!a) return set_error(CEL_E_ARG, "%s: NULL descriptor", fn);
+  const cel_attn b = rows_part(a);
+  return attention(&b, Keys{true, a->key_ptr, a->keys}, out, lse, fn, s);
+}
+extern "C" int cel_cross_attention_grad(const cel_cross_attn *a, const cel_rows *out, const float *lse, const cel_rows *dout,
+                                        void *scratch, const cel_rows *dq, const cel_rows *dk, const cel_rows *dv,
+                                        hipStream_t s) {
+  const char *fn = "cel_cross_attention_grad";
+  if (!a) return set_error(CEL_E_ARG, "%s: NULL descriptor", fn);
+  const cel_attn b = rows_part(a);
+  return attention_grad(&b, Keys{true, a->key_ptr, a->keys}, out, lse, dout, scratch, dq, dk, dv, fn, s);
 }

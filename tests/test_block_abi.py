@@ -151,3 +151,47 @@ def test_the_tests_own_generator_is_the_published_one():
              (0xd16cfe09, 0x94fdcceb, 0x5001e420, 0x24126ea1)),
             ([0] * 4, 0, 7, (0x5f6fb709, 0x0d893f64, 0x4f121f81, 0x4f730a48))):
         assert tuple(int(x) for x in philox([np.uint64(c) for c in counter], key, rounds)) == want
+
+
+def cross(**kw):
+    r = rows()
+    d = dict(type=0, tokens=100, keys=70, n_seq=2, heads=4, kv_heads=2, dim=64, scale=0.125, seq_ptr=SOME, key_ptr=SOME, q=r, k=r, v=r)
+    d.update(kw)
+    return b()._Cross(*d.values())
+
+
+@pytest.mark.parametrize("bad", [dict(type=2), dict(tokens=-1), dict(keys=-1), dict(keys=2 ** 31 - 1), dict(n_seq=-1), dict(heads=0),
+                                 dict(heads=5), dict(dim=12), dict(dim=136), dict(scale=0.0), dict(scale=NAN)])
+def test_cross_descriptors(lib, bad):
+    a, r = ctypes.byref(cross(**bad)), ctypes.byref(rows())
+    assert lib.cel_cross_attention_grad_scratch(a) == ARG
+    assert lib.cel_cross_attention(a, r, SOME, None) == ARG
+    assert lib.cel_cross_attention_grad(a, r, SOME, r, SOME, r, r, r, None) == ARG
+
+
+def test_cross_other_arguments(lib):
+    r = ctypes.byref(rows())
+    assert lib.cel_cross_attention_grad_scratch(None) == ARG
+    assert lib.cel_cross_attention(None, r, SOME, None) == ARG
+    assert lib.cel_cross_attention_grad(None, r, SOME, r, SOME, r, r, r, None) == ARG
+    for bad in (dict(seq_ptr=None), dict(key_ptr=None), dict(q=rows(p=None)), dict(k=rows(p=SOME + 8)), dict(v=rows(row=60))):
+        a = ctypes.byref(cross(**bad))
+        assert lib.cel_cross_attention(a, r, SOME, None) == ARG
+        assert lib.cel_cross_attention_grad(a, r, SOME, r, SOME, r, r, r, None) == ARG
+    a = ctypes.byref(cross())
+    assert lib.cel_cross_attention(a, None, SOME, None) == ARG and lib.cel_cross_attention(a, r, None, None) == ARG
+    for at in range(7):
+        args = [r, SOME, r, SOME, r, r, r]
+        args[at] = None
+        assert lib.cel_cross_attention_grad(a, *args, None) == ARG
+    # 2^24 workgroups of the keys' launch
+    big = ctypes.byref(cross(keys=2 ** 24, heads=64, kv_heads=8))
+    assert lib.cel_cross_attention_grad_scratch(big) == ARG
+    assert lib.cel_cross_attention_grad(big, r, SOME, r, SOME, r, r, r, None) == ARG
+
+
+def test_cross_scratch(lib):
+    size = lambda **kw: lib.cel_cross_attention_grad_scratch(ctypes.byref(cross(**kw)))  # noqa: E731
+    assert size() == 4 * (2 * 4 * 100 + 2 * 2 * 70 * 2 * 64)
+    assert size(kv_heads=4) == 4 * 2 * 4 * 100
+    assert size(tokens=0, kv_heads=4) == 0 and size(tokens=0, keys=0) == 0
