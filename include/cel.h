@@ -485,8 +485,7 @@ typedef struct {
  * views as cel_rows describes, but of any address of their type and any strides >= 0.
  * out may be x itself (the same address and strides); otherwise they share no
  * memory, and no two values of out do.
- * Errors: CEL_E_ARG (also for 2^32 and more pieces of 16 dimensions that
- * cannot be dealt out), CEL_E_HIP. */
+ * Errors: CEL_E_ARG, CEL_E_HIP. */
 int cel_rotary(const cel_rotary_args *a, const cel_rows *x, const cel_rows *out, hipStream_t stream);
 
 /* The gradient of cel_rotary's x at dout, its result's: dout turned back.

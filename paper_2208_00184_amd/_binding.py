@@ -852,6 +852,11 @@ def embed_grad(dx, ids, vocab, scale=1.0, dtype=None):
     return grad
 
 
+def _like(t, dtype):
+    """Room for a result as t, one row behind the other."""
+    return torch.empty_like(t) if dtype == t.dtype and t.is_contiguous() else t.new_empty(t.shape, dtype=dtype)
+
+
 def _apart(fn, out, x, T, d, size, *others):
     """Refuses results (a block) that share memory within themselves, with x (a block, unless they are
     x itself, in place) or with other tensors."""
@@ -909,7 +914,7 @@ def _rotary(fn, x, positions, freqs, axes, pairs, out):
             x = x.clone(memory_format=torch.contiguous_format)
             xv = _Rows(x.data_ptr(), H * d, d)
         if out is None:
-            out = torch.empty((T, H, d), dtype=x.dtype, device=x.device)
+            out = _like(x, x.dtype)
             ov = _Rows(out.data_ptr(), H * d, d)
         else:
             ov = _plain_view(out) if out.shape == x.shape and out.dtype == x.dtype else None
@@ -1004,7 +1009,7 @@ def dropout(x, p, seed, step=0, out=None):
         if rows >= 1 << 32 or columns >= 1 << 31:
             _refuse(f"{fn}: {rows} rows of {columns} values")
         if out is None:
-            out = torch.empty(x.shape, dtype=x.dtype, device=x.device)
+            out = _like(x, x.dtype)
             to = columns
         else:
             o = _matrix(out) if out.shape == x.shape and out.dtype == x.dtype else None
@@ -1023,68 +1028,75 @@ def dropout(x, p, seed, step=0, out=None):
 _VECTORS = ("pre", "pre_bias", "post", "post_bias", "gate")
 
 
-def _norm(fn, f, stream, of_f, of_stream, vectors, seq_ptr, scale, p, seed, step, eps, center):
-    """-> (device, descriptor, matrices, tensors to keep alive): checks that residual_norm and residual_norm_grad
-    share.  of_f and of_stream: further tensors as f and as the stream, by name; f, those of of_f and the vectors may be None."""
-    given = {n: t for n, t in {**of_f, **of_stream, **dict(zip(_VECTORS, vectors))}.items() if t is not None}
-    if f is not None:
-        given["f"] = f
-    given["the stream"] = stream
+def _norm(fn, tensors, vectors, seq_ptr, scale, p, seed, step, eps, center):
+    """-> (device, type of f, descriptor, matrices, tensors to keep alive): checks that residual_norm and
+    residual_norm_grad share.  tensors: (name, tensor or None, whether it is as the stream), the stream's own first."""
+    given = {name: t for name, t, _ in tensors if t is not None}
+    for name, t in zip(_VECTORS, vectors):
+        if t is not None:
+            given[name] = t
     if seq_ptr is not None:
         given["seq_ptr"] = seq_ptr
     if isinstance(step, torch.Tensor):
         given["step"] = step
     index = _device_of(fn, **given)
-    if stream.dim() != 2 or stream.dtype not in _TYPES:
+    stream = tensors[0][1]
+    shape, dtype = stream.shape, stream.dtype
+    if len(shape) != 2 or dtype not in _TYPES:
         _refuse(f"{fn}: the stream is not [rows, hidden] in bfloat16, float16 or float32")
-    T, h = shape = stream.shape
+    T, h = shape
+    kind = None
+    for _, t, as_stream in tensors:
+        if t is not None and not as_stream:
+            kind = t.dtype
+            break
+    if kind is None:
+        kind = vectors[0].dtype if dtype == torch.float32 and vectors[0] is not None else dtype
+    if kind not in _TYPES or (dtype != kind and dtype != torch.float32):
+        _refuse(f"{fn}: a stream in {dtype} beside blocks in {kind}")
     keep, matrices = [], []
-    like = [t for t in (f, *of_f.values()) if t is not None]
-    kind = like[0].dtype if like else given["pre"].dtype if stream.dtype == torch.float32 and "pre" in given else stream.dtype
-    if kind not in _TYPES or stream.dtype not in (kind, torch.float32):
-        _refuse(f"{fn}: a stream in {stream.dtype} beside blocks in {kind}")
-    for t, dtype in [(f, kind), (stream, stream.dtype)] + [(t, kind) for t in of_f.values()] + [(t, stream.dtype) for t in of_stream.values()]:
+    for name, t, as_stream in tensors:
         if t is None:
             matrices.append(None)
             continue
-        if t.shape != shape or t.dtype != dtype:
-            _refuse(f"{fn}: {tuple(t.shape)} {t.dtype} beside a stream of {tuple(shape)}, {dtype} wanted")
-        m = _matrix(t)
-        if m is None:
-            t = t.clone(memory_format=torch.contiguous_format)
-            keep.append(t)
+        want = dtype if as_stream else kind
+        if t.shape != shape or t.dtype != want:
+            _refuse(f"{fn}: {name} is {tuple(t.shape)} {t.dtype} beside a stream of {tuple(shape)}, {want} wanted")
+        if t.is_contiguous():
+            stride = h
+        else:
             m = _matrix(t)
-        matrices.append(_Matrix(t.data_ptr(), m[2]))
-    wide, at = None, []
-    S = 0
+            if m is None:
+                t = t.clone(memory_format=torch.contiguous_format)
+                keep.append(t)
+            stride = h if m is None else m[2]
+        matrices.append(C.byref(_Matrix(t.data_ptr(), stride)))
+    S, ptr = 0, None
     if seq_ptr is not None:
         if seq_ptr.dim() != 1 or seq_ptr.dtype != torch.int32 or seq_ptr.numel() < 1 or vectors[4] is None:
             _refuse(f"{fn}: seq_ptr is not int32 [sequences + 1] beside a gate")
         seq_ptr = seq_ptr.contiguous()
         keep.append(seq_ptr)
-        S = seq_ptr.numel() - 1
+        S, ptr = seq_ptr.numel() - 1, seq_ptr.data_ptr()
+    wide, at = None, []
     for name, t in zip(_VECTORS, vectors):
         if t is None:
             at.append(None)
             continue
-        want = (S, h) if name == "gate" and seq_ptr is not None else (h,)
-        wide = t.dtype if wide is None else wide
-        if t.shape != want or t.dtype != wide or wide not in (kind, torch.float32):
+        want = (S, h) if ptr is not None and name == "gate" else (h,)
+        wide = wide or t.dtype
+        if t.shape != want or t.dtype != wide or (wide != kind and wide != torch.float32):
             _refuse(f"{fn}: {name} is {tuple(t.shape)} {t.dtype}, {want} wanted in one type for all, {kind} or float32")
         if not h:
             _refuse(f"{fn}: rows of no values")
-        t = t.contiguous()
-        keep.append(t)
-        at.append(t.data_ptr() or seq_ptr.data_ptr())  # the gates of no sequence have no address, and none is read
+        if not t.is_contiguous():
+            t = t.contiguous()
+            keep.append(t)
+        at.append(t.data_ptr() or ptr)  # the gates of no sequence have no address, and none is read
     if T >= 1 << 31:
         _refuse(f"{fn}: {T} rows")
-    a = _Norm(_TYPES[kind], _TYPES[stream.dtype], _TYPES[wide or kind], bool(center), T, h, S,
-              None if seq_ptr is None else seq_ptr.data_ptr(), eps, scale, *at, _mask(fn, p, seed, step))
+    a = _Norm(_TYPES[kind], _TYPES[dtype], _TYPES[wide or kind], bool(center), T, h, S, ptr, eps, scale, *at, _mask(fn, p, seed, step))
     return index, kind, a, matrices, keep
-
-
-def _at(m):
-    return None if m is None else C.byref(m)
 
 
 def residual_norm(f, x, pre, post=None, gate=None, seq_ptr=None, pre_bias=None, post_bias=None, scale=1.0, p=0.0, seed=0, step=0,
@@ -1104,12 +1116,12 @@ def residual_norm(f, x, pre, post=None, gate=None, seq_ptr=None, pre_bias=None, 
     -> (y as x, z as f): the stream behind the block, and the next block's input (None without pre).  f = None: no
     block yet, -> (x, norm(x) * pre + pre_bias)."""
     fn = "residual_norm"
-    index, kind, a, (fm, xm), keep = _norm(fn, f, x, {}, {}, (pre, pre_bias, post, post_bias, gate), seq_ptr, scale, p, seed, step, eps, center)
+    index, kind, a, (xm, fm), keep = _norm(fn, (("x", x, True), ("f", f, False)), (pre, pre_bias, post, post_bias, gate), seq_ptr,
+                                           scale, p, seed, step, eps, center)
     with _on(index):
-        y = x if f is None else torch.empty(x.shape, dtype=x.dtype, device=x.device)
-        z = None if pre is None else torch.empty(x.shape, dtype=kind, device=x.device)
         h = a.hidden
-        _check(lib().cel_residual_norm(C.byref(a), _at(fm), _at(xm), None if f is None else C.byref(_Matrix(y.data_ptr(), h)),
+        y, z = x if f is None else _like(x, x.dtype), None if pre is None else _like(x, kind)
+        _check(lib().cel_residual_norm(C.byref(a), fm, xm, None if f is None else C.byref(_Matrix(y.data_ptr(), h)),
                                        None if z is None else C.byref(_Matrix(z.data_ptr(), h)), _raw_stream(index)))
     return y, z
 
@@ -1124,17 +1136,17 @@ def residual_norm_grad(dy, dz, f, y, pre, post=None, gate=None, seq_ptr=None, pr
     if (dz is None) != (pre is None):
         _refuse(f"{fn}: dz and pre come together")
     vectors = (pre, pre_bias, post, post_bias, gate)
-    index, kind, a, (fm, ym, zm, gm), keep = _norm(fn, f, y, dict(dz=dz), dict(dy=dy), vectors, seq_ptr, scale, p, seed, step, eps, center)
+    index, kind, a, (ym, fm, zm, gm), keep = _norm(fn, (("y", y, True), ("f", f, False), ("dz", dz, False), ("dy", dy, True)), vectors,
+                                                   seq_ptr, scale, p, seed, step, eps, center)
     with _on(index):
-        dx = torch.empty(y.shape, dtype=y.dtype, device=y.device)
-        df = None if f is None else torch.empty(y.shape, dtype=kind, device=y.device)
-        grads = {n: torch.empty(t.shape, dtype=torch.float32, device=y.device) for n, t in zip(_VECTORS, vectors) if t is not None}
+        h = a.hidden
+        dx, df = _like(y, y.dtype), None if f is None else _like(y, kind)
+        grads = {n: t.new_empty(t.shape, dtype=torch.float32) for n, t in zip(_VECTORS, vectors) if t is not None}
         size = lib().cel_residual_norm_grad_scratch(C.byref(a))
         if size < 0:
             _check(size)
         scratch = torch.empty(size, dtype=torch.uint8, device=y.device)
         to = _NormGrads(*(grads[n].data_ptr() or scratch.data_ptr() if n in grads else None for n in _VECTORS))
-        h = a.hidden
-        _check(lib().cel_residual_norm_grad(C.byref(a), _at(gm), _at(zm), _at(fm), _at(ym), scratch.data_ptr(), C.byref(_Matrix(dx.data_ptr(), h)),
+        _check(lib().cel_residual_norm_grad(C.byref(a), gm, zm, fm, ym, scratch.data_ptr(), C.byref(_Matrix(dx.data_ptr(), h)),
                                             None if df is None else C.byref(_Matrix(df.data_ptr(), h)), C.byref(to), _raw_stream(index)))
     return dx, df, grads

@@ -24,6 +24,23 @@ __device__ inline Eight<T> load_eight(const T *p, int64_t left) {
   }
   return r;
 }
+// The same of a row of n >= 8 numbers from number `at` on, without a branch that a wave would wait in: where
+// the row ends inside the eight they come from its last eight, and shift_down puts them in their place.
+template <class T>
+__device__ inline Eight<T> load_back(const T *row, int at, int n) {
+  return *reinterpret_cast<const Eight<T> *>(row + min(at, n - 8));
+}
+// f[e] = f[e + by], 0 behind the last.
+__device__ inline void shift_down(float (&f)[8], int by) {
+#pragma unroll
+  for (int step = 4; step; step /= 2) {
+    const bool on = by & step;
+#pragma unroll
+    for (int e = 0; e < 8; e++) f[e] = on ? (e + step < 8 ? f[e + step] : 0.f) : f[e];
+  }
+#pragma unroll
+  for (int e = 0; e < 8; e++) f[e] = by >= 8 ? 0.f : f[e];
+}
 template <class T>
 __device__ inline void values(float (&f)[8], const Eight<T> &r) {
   T x[8];
@@ -37,8 +54,14 @@ __device__ inline void store_eight(T *p, const float (&f)[8], int64_t left) {
 #pragma unroll
   for (int e = 0; e < 8; e++) x[e] = (T)f[e];
   if (left >= 8) {
+    // As words that the compiler does not know from the single stores below: it would make one
+    // of both branches' first store, and the wide store three narrow ones.
+    uint32_t w[2 * sizeof(T)];
+    __builtin_memcpy(w, x, sizeof w);
+#pragma unroll
+    for (uint32_t &y : w) asm("" : "+v"(y));
     Eight<T> r;
-    __builtin_memcpy(&r, x, sizeof r);
+    __builtin_memcpy(&r, w, sizeof r);
     *reinterpret_cast<Eight<T> *>(p) = r;
   } else {
 #pragma unroll
@@ -78,11 +101,21 @@ struct Mask {
     const uint64_t s = ((uint64_t)s1 << 32 | s0) + (uint64_t)*step;
     s0 = (uint32_t)s, s1 = (uint32_t)(s >> 32);
   }
-  // Values of row r, block c / 8: what is dropped becomes 0 whatever it was.
-  __device__ void apply(float (&f)[8], uint32_t block, uint32_t row) const {
+  // Which values of row r, block c / 8 stay: a condition of each, which takes no vector registers.
+  __device__ void kept(bool (&k)[8], uint32_t block, uint32_t row) const {
     const Words x = philox(block, row, s0, s1, k0, k1);
 #pragma unroll
-    for (int e = 0; e < 8; e++) f[e] = (e & 1 ? x.w[e / 2] >> 16 : x.w[e / 2] & 0xffffu) >= least ? f[e] * by : 0.f;
+    for (int e = 0; e < 8; e++) k[e] = (e & 1 ? x.w[e / 2] >> 16 : x.w[e / 2] & 0xffffu) >= least;
+  }
+  // What is dropped becomes 0 whatever it was.
+  __device__ void apply(float (&f)[8], const bool (&k)[8]) const {
+#pragma unroll
+    for (int e = 0; e < 8; e++) f[e] = k[e] ? f[e] * by : 0.f;
+  }
+  __device__ void apply(float (&f)[8], uint32_t block, uint32_t row) const {
+    bool k[8];
+    kept(k, block, row);
+    apply(f, k);
   }
 };
 inline int check_mask(const cel_mask *m, const char *fn) {
@@ -95,26 +128,57 @@ inline Mask mask_of(const cel_mask *m) {
               least >= 65536u ? 0.f : (float)(65536.0 / (65536.0 - least)), m->step_at};
 }
 
-// Sums over the 64 lanes, in all of them, in a fixed order.
 template <int CTRL>
 __device__ inline float dpp_add(float x) {
   return x + __int_as_float(__builtin_amdgcn_update_dpp(0, __float_as_int(x), CTRL, 0xf, 0xf, true));
 }
-__device__ inline float wave_sum(float x) {
-  typedef __attribute__((ext_vector_type(2))) uint32_t u32x2;
-  x = dpp_add<0x128>(x);  // rotations inside 16 lanes by 8, 4, 2 and 1
+// The sum over 16 lanes beside each other, in all of them, by rotations.
+__device__ inline float sixteen_sum(float x) {
+  x = dpp_add<0x128>(x);
   x = dpp_add<0x124>(x);
   x = dpp_add<0x122>(x);
-  x = dpp_add<0x121>(x);
-  u32x2 r = __builtin_amdgcn_permlane16_swap(__float_as_uint(x), __float_as_uint(x), false, false);
-  x = __uint_as_float(r[0]) + __uint_as_float(r[1]);
-  r = __builtin_amdgcn_permlane32_swap(__float_as_uint(x), __float_as_uint(x), false, false);
-  return __uint_as_float(r[0]) + __uint_as_float(r[1]);
+  return dpp_add<0x121>(x);
 }
+// Sums of N numbers a lane over 64 lanes, in a fixed order.  A swap of halves (or of 16 lanes) puts two
+// numbers' sums into one register, so that N of them take little more than one: value v's sum is
+// in register v / 4, in the 16 lanes from at(v) on.
+template <int N>
+struct LaneSums {
+  static constexpr int kRegisters = (N + 3) / 4;
+  float r[kRegisters];
+  static constexpr int at(int v) {
+    constexpr int rows[4] = {0, 2, 1, 3};
+    const bool alone = v / 4 * 4 + 2 >= N;  // a register with two numbers
+    return 16 * (alone ? v % 4 * 2 : rows[v % 4]);
+  }
+  __device__ explicit LaneSums(const float (&x)[N]) {
+    typedef __attribute__((ext_vector_type(2))) uint32_t u32x2;
+#pragma unroll
+    for (int j = 0; j < kRegisters; j++) {
+      float a[2];
+#pragma unroll
+      for (int k = 0; k < 2; k++) {
+        const int v = 4 * j + 2 * k;
+        if (v >= N) continue;
+        const u32x2 y = __builtin_amdgcn_permlane32_swap(__float_as_uint(x[v]), v + 1 < N ? __float_as_uint(x[v + 1 < N ? v + 1 : v]) : 0u,
+                                                         false, false);
+        a[k] = __uint_as_float(y[0]) + __uint_as_float(y[1]);
+      }
+      const float b = 4 * j + 2 < N ? a[1] : a[0];
+      const u32x2 y = __builtin_amdgcn_permlane16_swap(__float_as_uint(a[0]), __float_as_uint(b), false, false);
+      r[j] = sixteen_sum(__uint_as_float(y[0]) + __uint_as_float(y[1]));
+    }
+  }
+  __device__ void get(float (&x)[N]) const {
+#pragma unroll
+    for (int v = 0; v < N; v++) x[v] = __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(r[v / 4]), at(v)));
+  }
+};
 
 // n / d for a divisor that the host knows.
 struct Divisor {
   uint32_t d, m;  // m = 2^32 / d rounded down, at most 2^32 - 1
+  Divisor() = default;
   explicit Divisor(uint32_t d_) : d(d_), m(d_ > 1 ? (uint32_t)((uint64_t(1) << 32) / d_) : ~0u) {}
   // -> the quotient; n becomes the remainder.  n m / 2^32 is less than 1 below n / d.
   __device__ uint32_t split(uint32_t &n) const {
@@ -123,6 +187,7 @@ struct Divisor {
     if (n >= d) q++, n -= d;
     return q;
   }
+  __device__ uint32_t quotient(uint32_t n) const { return split(n); }
 };
 
 }  // namespace cel

@@ -17,6 +17,7 @@
 // segments of one sequence, and leaves a sum for each.
 #include <algorithm>
 #include <cmath>
+#include <cstring>
 #include <type_traits>
 
 #include "elements.h"
@@ -25,12 +26,14 @@ namespace cel {
 namespace {
 
 constexpr int kMost = 2;        // eights of a row a lane holds
-constexpr int kWaves = 8;       // waves of a workgroup, unless a row takes more
-constexpr int kWidest = 16;     // waves of a row
-constexpr int kGroups = 256;    // workgroups that leave sums, at most
+constexpr int kWidest = 16;     // waves of a row, and of a workgroup
+constexpr int kForward = 4, kBackward = 16;  // waves of a workgroup, unless a row takes more
+constexpr int kGroups = 256;    // workgroups that leave sums, at most; four times that forward
 
 // Which vectors there are, as far as registers are held for them.
 constexpr int kBias = 1, kBranch = 2;  // biases; a norm of f or a gate
+
+__host__ __device__ constexpr int vectors_of(int kind) { return kind & kBranch ? kind & kBias ? 4 : 3 : 1; }
 
 struct NormArgs {
   const char *f, *x, *dy, *dz;  // x: the stream read (x, or y backwards)
@@ -39,31 +42,47 @@ struct NormArgs {
   const void *pre, *pre_bias, *post, *post_bias, *gate;
   bool wide;                    // parameters of 32 bits
   bool center;
+  bool has_dy;
   const int32_t *ptr;           // NULL: one gate for all rows
   int32_t S;
   int64_t T, per;               // rows; rows of a workgroup
   int32_t h, W, teams;
+  Divisor waves;                // of a row
   float eps, scale;
   Mask mask;
   float *part;                  // sums that workgroups leave: [vector][slot][h]
   int64_t slots;
 };
 
-struct Column {  // where a lane stands in its row
-  int at, left;
-};
-
-// Eight values of a vector of parameters; `none` where there is no such vector.
-template <class T>
-__device__ inline void parameters(float (&f)[8], const void *p, bool wide, Column c, float none) {
-  if (!p || c.left <= 0) {
+// The kernel's arguments as they lie in memory, read anew: a loop that holds all of them has no scalar
+// registers left, and spills some into vector registers' lanes.
+__device__ inline NormArgs again() {
+  typedef const __attribute__((address_space(4))) uint32_t *args_ptr;
+  static_assert(sizeof(NormArgs) % 4 == 0, "whole words");
+  args_ptr p = (args_ptr)__builtin_amdgcn_kernarg_segment_ptr();
+  asm volatile("" : "+s"(p));
+  uint32_t w[sizeof(NormArgs) / 4];
 #pragma unroll
-    for (int e = 0; e < 8; e++) f[e] = none;
-  } else if (wide) {
-    values<float>(f, load_eight(static_cast<const float *>(p) + c.at, c.left));
-  } else {
-    values<T>(f, load_eight(static_cast<const T *>(p) + c.at, c.left));
-  }
+  for (int i = 0; i < (int)(sizeof(NormArgs) / 4); i++) w[i] = p[i];
+  NormArgs A;
+  __builtin_memcpy(&A, w, sizeof A);
+  return A;
+}
+
+// Where a lane stands in its row: its first column and how many of the eight lack at the row's end (8 and more: all).
+struct Column {
+  int at, lack;
+  bool tail;  // of any lane of the wave
+};
+template <class T, bool NARROW>  // rows of less than eight columns
+__device__ inline Eight<T> load_piece(const T *row, Column c, int h) {
+  if constexpr (NARROW) return load_eight(row, h - c.at);
+  else return load_back(row, c.at, h);
+}
+template <class T, bool NARROW>
+__device__ inline void piece_values(float (&f)[8], const Eight<T> &r, Column c, int h) {
+  values<T>(f, r);
+  if (!NARROW && c.tail) shift_down(f, c.lack);
 }
 
 // The sequence that holds row t and the first row behind t that need not be in it; -1: none.
@@ -91,52 +110,83 @@ __device__ inline int sequence_at(const NormArgs &A, int64_t t, int hint, int64_
 
 // Sums over a row's columns, in all of its lanes: over the lanes, and through
 // LDS over the team's waves.  Two buffers in turn make one barrier enough.
+constexpr int kSums = 8;
 struct RowSum {
-  float (*red)[kWidest][4];
-  int wave, W, turn;
+  float (*red)[kSums][kWidest];
+  int wave, team, W, turn;
   template <int N>
   __device__ void operator()(float (&x)[N]) {
+    LaneSums<N> s(x);
+    if (W > 1) {
+      float (*to)[kWidest] = red[turn];
+      turn ^= 1;
+      const int lane = threadIdx.x & 63, row = lane >> 4, i = lane & 15;
+      if (i == 0) {
 #pragma unroll
-    for (int n = 0; n < N; n++) x[n] = wave_sum(x[n]);
-    if (W == 1) return;
-    float (*r)[4] = red[turn];
-    turn ^= 1;
-    if ((threadIdx.x & 63) == 0) {
+        for (int j = 0; j < LaneSums<N>::kRegisters; j++) to[4 * j + row][wave] = s.r[j];
+      }
+      lds_barrier();
 #pragma unroll
-      for (int n = 0; n < N; n++) r[wave][n] = x[n];
+      for (int j = 0; j < LaneSums<N>::kRegisters; j++) {
+        const float y = to[4 * j + row][team * W + min(i, W - 1)];
+        s.r[j] = sixteen_sum(i < W ? y : 0.f);
+      }
     }
-    lds_barrier();
-    const int first = wave / W * W;
-#pragma unroll
-    for (int n = 0; n < N; n++) x[n] = 0.f;
-    for (int w = 0; w < W; w++)
-#pragma unroll
-      for (int n = 0; n < N; n++) x[n] += r[first + w][n];
+    s.get(x);
   }
 };
 
+// A row as it comes from memory, and as numbers.
+template <class T, int C, bool NARROW>
+struct Raw {
+  Eight<T> e[C];
+  __device__ void load(const char *p, int64_t at, const Column (&c)[C], int h) {
+#pragma unroll
+    for (int u = 0; u < C; u++) e[u] = load_piece<T, NARROW>(reinterpret_cast<const T *>(p) + at, c[u], h);
+  }
+};
 template <int C>
 struct Row {
   float v[C][8];
-  template <class T>
-  __device__ void load(const char *p, int64_t at, const Column (&c)[C], bool real) {
+  template <class T, bool NARROW>
+  __device__ void from(const Raw<T, C, NARROW> &r, const Column (&c)[C], int h) {
 #pragma unroll
-    for (int u = 0; u < C; u++) {
-      if (real && c[u].left > 0) {
-        values<T>(v[u], load_eight(reinterpret_cast<const T *>(p) + at + c[u].at, c[u].left));
-      } else {
+    for (int u = 0; u < C; u++) piece_values<T, NARROW>(v[u], r.e[u], c[u], h);
+  }
+  __device__ void fill(float x) {
 #pragma unroll
-        for (int e = 0; e < 8; e++) v[u][e] = 0.f;
+    for (int u = 0; u < C; u++)
+#pragma unroll
+      for (int e = 0; e < 8; e++) v[u][e] = x;
+  }
+  __device__ void cut(const Column (&c)[C]) {  // 0 past the row's end
+#pragma unroll
+    for (int u = 0; u < C; u++)
+      if (c[u].tail) {
+#pragma unroll
+        for (int e = 0; e < 8; e++) v[u][e] = e < 8 - c[u].lack ? v[u][e] : 0.f;
       }
-    }
   }
   template <class T>
   __device__ void store(char *p, int64_t at, const Column (&c)[C]) const {
 #pragma unroll
     for (int u = 0; u < C; u++)
-      if (c[u].left > 0) store_eight(reinterpret_cast<T *>(p) + at + c[u].at, v[u], c[u].left);
+      if (c[u].lack < 8) store_eight(reinterpret_cast<T *>(p) + at + c[u].at, v[u], 8 - c[u].lack);
   }
 };
+// N vectors of parameters, all loads before the first use; `none` where there is no such vector.
+template <class T, bool NARROW, int C, int N>
+__device__ inline void parameters(Row<C> *const (&to)[N], const void *const (&from)[N], const float (&none)[N], const Column (&c)[C], int h) {
+  Raw<T, C, NARROW> r[N];
+#pragma unroll
+  for (int n = 0; n < N; n++)
+    if (from[n]) r[n].load(static_cast<const char *>(from[n]), 0, c, h);
+#pragma unroll
+  for (int n = 0; n < N; n++) {
+    if (from[n]) to[n]->from(r[n], c, h);
+    else to[n]->fill(none[n]);
+  }
+}
 #define EACH(u, e) \
   _Pragma("unroll") for (int u = 0; u < C; u++) _Pragma("unroll") for (int e = 0; e < 8; e++)
 
@@ -148,72 +198,92 @@ __device__ inline float normalise(Row<C> &v, const NormArgs &A, const Column (&c
     EACH(u, e) m[0] += v.v[u][e];
     sum(m);
     m[0] /= A.h;
-    EACH(u, e) v.v[u][e] = e < c[u].left ? v.v[u][e] - m[0] : 0.f;
+    EACH(u, e) v.v[u][e] -= m[0];
+    v.cut(c);
   }
   float q[1] = {0.f};
   EACH(u, e) q[0] = fmaf(v.v[u][e], v.v[u][e], q[0]);
   sum(q);
-  return 1.f / sqrtf(q[0] / A.h + A.eps);
+  return rsqrtf(q[0] / A.h + A.eps);
 }
 
 template <int C>
-__device__ inline void columns_of(Column (&c)[C], const NormArgs &A) {
-  const int lane = threadIdx.x % (64 * A.W);
-#pragma unroll
-  for (int u = 0; u < C; u++) c[u].at = 8 * (u * 64 * A.W + lane), c[u].left = A.h - c[u].at;
-}
-
-// T: of f and z; R: of the stream x and y.
-template <class T, class R, int C, int KIND, int THREADS>
-__global__ void __launch_bounds__(THREADS) k_residual_norm(NormArgs A) {
-  __shared__ float s_red[2][kWidest][4];
-  constexpr bool bias = (KIND & kBias) != 0, branch = (KIND & kBranch) != 0;
-  A.mask.begin();
-  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), team = wave / A.W;
-  RowSum sum{s_red, wave, A.W, 0};
-  Column c[C];
-  columns_of(c, A);
-  Row<C> pre, pre_bias, post, post_bias, gate;
+__device__ inline void columns_of(Column (&c)[C], const NormArgs &A, int team) {
+  const int lane = threadIdx.x - team * 64 * A.W;
 #pragma unroll
   for (int u = 0; u < C; u++) {
-    parameters<T>(pre.v[u], A.pre, A.wide, c[u], 0.f);
-    if (bias) parameters<T>(pre_bias.v[u], A.pre_bias, A.wide, c[u], 0.f);
-    if (branch) {
-      parameters<T>(post.v[u], A.post, A.wide, c[u], 0.f);
-      if (bias) parameters<T>(post_bias.v[u], A.post_bias, A.wide, c[u], 0.f);
-      parameters<T>(gate.v[u], A.ptr ? nullptr : A.gate, A.wide, c[u], 1.f);
-    }
+    c[u].at = 8 * (u * 64 * A.W + lane);
+    c[u].lack = max(0, c[u].at + 8 - A.h);
+    c[u].tail = __any(c[u].lack);
   }
+}
+// The gates of sequence s.
+template <class T, bool NARROW, int C>
+__device__ inline void gates_of(Row<C> &gate, const NormArgs &A, int s, const Column (&c)[C]) {
+  Row<C> *const to[1] = {&gate};
+  const float none[1] = {1.f};
+  const void *const from[1] = {static_cast<const char *>(A.gate) + (int64_t)s * A.h * (A.wide ? 4 : sizeof(T))};
+  if (A.wide) parameters<float, NARROW>(to, from, none, c, A.h);
+  else parameters<T, NARROW>(to, from, none, c, A.h);
+}
+
+// T: of f and z; R: of the stream x and y.  The next row is on its way while one is dealt with.
+template <class T, class R, int C, int KIND, bool NARROW>
+__global__ void __launch_bounds__(64 * kWidest) k_residual_norm(NormArgs A) {
+  __shared__ float s_red[2][kSums][kWidest];
+  constexpr bool bias = (KIND & kBias) != 0, branch = (KIND & kBranch) != 0;
+  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), team = A.waves.quotient(wave);
+  RowSum sum{s_red, wave, team, A.W, 0};
+  Column c[C];
+  columns_of(c, A, team);
   const int64_t first = blockIdx.x * A.per, last = min(A.T, first + A.per);
+  const int teams = A.teams;
+  Raw<T, C, NARROW> f_next;
+  Raw<R, C, NARROW> x_next;
+  auto load = [&](const NormArgs &A, int64_t t) {  // rows that are not there: the last in their place
+    t = min(t, last - 1);
+    if (A.f) f_next.load(A.f, t * A.f_row, c, A.h);
+    x_next.load(A.x, t * A.x_row, c, A.h);
+  };
+  load(A, first + team);
+  Mask mask = A.mask;
+  mask.begin();
+  Row<C> pre, pre_bias, post, post_bias, gate;
+  {
+    Row<C> *const to[5] = {&pre, &gate, &post, &pre_bias, &post_bias};
+    const void *const from[5] = {A.pre, branch && !A.ptr ? A.gate : nullptr, branch ? A.post : nullptr, bias ? A.pre_bias : nullptr,
+                                 bias && branch ? A.post_bias : nullptr};
+    const float none[5] = {0.f, 1.f, 0.f, 0.f, 0.f};
+    if (A.wide) parameters<float, NARROW>(to, from, none, c, A.h);
+    else parameters<T, NARROW>(to, from, none, c, A.h);
+  }
   int s = -1;
   int64_t s_end = branch && A.ptr ? first : A.T;
-  for (int64_t base = first; base < last; base += A.teams) {
+  for (int64_t base = first; base < last; base += teams) {
+    const NormArgs A = again();
+    mask.k0 = A.mask.k0, mask.k1 = A.mask.k1, mask.least = A.mask.least, mask.by = A.mask.by;
     const int64_t t = base + team;
     const bool real = t < last;
     Row<C> f, x;
-    if (A.f) f.template load<T>(A.f, t * A.f_row, c, real);
-    x.template load<R>(A.x, t * A.x_row, c, real);
+    if (A.f) f.from(f_next, c, A.h);
+    x.from(x_next, c, A.h);
+    load(A, t + teams);
     if (branch && A.ptr && real && t >= s_end) {
       s = sequence_at(A, t, s + 1, s_end);
-#pragma unroll
-      for (int u = 0; u < C; u++)
-        if (s >= 0)
-          parameters<T>(gate.v[u], static_cast<const char *>(A.gate) + (int64_t)s * A.h * (A.wide ? 4 : sizeof(T)), A.wide, c[u], 0.f);
+      if (s >= 0) gates_of<T, NARROW>(gate, A, s, c);
     }
     if (A.f) {
       if (branch && A.post) {
         const float r = normalise(f, A, c, sum);
         EACH(u, e) f.v[u][e] = f.v[u][e] * r * post.v[u][e] + (bias ? post_bias.v[u][e] : 0.f);
       }
-      if (A.mask.least) {
+      if (mask.least) {
 #pragma unroll
-        for (int u = 0; u < C; u++) A.mask.apply(f.v[u], c[u].at >> 3, (uint32_t)t);
+        for (int u = 0; u < C; u++) mask.apply(f.v[u], c[u].at >> 3, (uint32_t)t);
       }
-      const bool open = !(branch && A.ptr) || s >= 0;
-      EACH(u, e) {
-        const float n = branch ? f.v[u][e] * gate.v[u][e] : f.v[u][e];
-        x.v[u][e] = fmaf(x.v[u][e], A.scale, open ? n : 0.f);
-      }
+      if (branch) EACH(u, e) f.v[u][e] *= gate.v[u][e];
+      if (branch && A.ptr && s < 0) f.fill(0.f);
+      EACH(u, e) x.v[u][e] = fmaf(x.v[u][e], A.scale, f.v[u][e]);
       if (real) x.template store<R>(A.y, t * A.y_row, c);
     }
     if (A.pre) {
@@ -224,69 +294,105 @@ __global__ void __launch_bounds__(THREADS) k_residual_norm(NormArgs A) {
   }
 }
 
-// The gradient of v = (a norm's value) at g, both as they stand in the row: v less
-// its mean if centered, r its factor.  -> g; v becomes the norm's value.
-template <int C>
-__device__ inline void norm_gradient(Row<C> &g, Row<C> &v, float r, const NormArgs &A, const Column (&c)[C], RowSum &sum) {
-  float m[2] = {0.f, 0.f};
-  EACH(u, e) {
-    v.v[u][e] *= r;
-    m[0] = fmaf(g.v[u][e], v.v[u][e], m[0]);
-    m[1] += g.v[u][e];
+// The vectors that the gradient's rows need, where rows have need of the registers: in 32 bits in
+// LDS, each padded with zeros to whole eights; or of rows beyond 8,192 columns, whose vectors LDS does not hold, read anew.
+enum { kPre, kPost, kGate, kPostBias };
+template <class T>
+struct Vectors {
+  float *lds;
+  const void *at[4];
+  bool wide;
+  int h, padded;
+  __device__ void stage(int which) const {
+    const void *p = at[which];
+    for (int k = threadIdx.x; k < padded; k += blockDim.x)
+      lds[which * padded + k] = k >= h ? 0.f : !p ? 1.f : wide ? static_cast<const float *>(p)[k] : (float)static_cast<const T *>(p)[k];
   }
-  sum(m);
-  const float a = m[0] / A.h, b = A.center ? m[1] / A.h : 0.f;
-  EACH(u, e) g.v[u][e] = (g.v[u][e] - b - v.v[u][e] * a) * r;
-}
+  template <int C>
+  __device__ void get(Row<C> &to, int which, const Column (&c)[C]) const {
+    if constexpr (C == 1) {
+      typedef __attribute__((ext_vector_type(4))) float f32x4;
+      const f32x4 *p = reinterpret_cast<const f32x4 *>(lds + which * padded + min(c[0].at, padded - 8));
+      const f32x4 a = p[0], b = p[1];
+#pragma unroll
+      for (int e = 0; e < 4; e++) to.v[0][e] = a[e], to.v[0][4 + e] = b[e];
+    } else {
+      Row<C> *const rows[1] = {&to};
+      const void *const from[1] = {at[which]};
+      const float none[1] = {1.f};
+      if (wide) parameters<float, false>(rows, from, none, c, h);
+      else parameters<T, false>(rows, from, none, c, h);
+    }
+  }
+};
 
-// A team's sums of a vector's gradient to the workgroup's slot.
+// The teams' sums of up to two vectors' gradients (`to` NULL: none) to the workgroup's slots.
 template <int C>
-__device__ inline void leave_sums(Row<C> &acc, const NormArgs &A, float *to, const Column (&c)[C], int team, float *s_join) {
+__device__ inline void leave_sums(Row<C> &one, float *to_one, Row<C> &two, float *to_two, const NormArgs &A, const Column (&c)[C], int team,
+                                  float *s_join) {
   if (A.teams > 1) {
+    float *s_two = s_join + A.teams * A.h;
     __syncthreads();
-#pragma unroll
-    for (int u = 0; u < C; u++)
-      if (c[u].left > 0) {
-#pragma unroll
-        for (int e = 0; e < 8; e++)
-          if (e < c[u].left) s_join[team * A.h + c[u].at + e] = acc.v[u][e];
-      }
+    if (to_one) one.template store<float>(reinterpret_cast<char *>(s_join), (int64_t)team * A.h, c);
+    if (to_two) two.template store<float>(reinterpret_cast<char *>(s_two), (int64_t)team * A.h, c);
     __syncthreads();
     for (int k = threadIdx.x; k < A.h; k += blockDim.x) {
-      float x = 0.f;
-      for (int w = 0; w < A.teams; w++) x += s_join[w * A.h + k];
-      to[k] = x;
+      float x = 0.f, y = 0.f;
+      for (int w = 0; w < A.teams; w++) {
+        if (to_one) x += s_join[w * A.h + k];
+        if (to_two) y += s_two[w * A.h + k];
+      }
+      if (to_one) to_one[k] = x;
+      if (to_two) to_two[k] = y;
     }
   } else {
-    acc.template store<float>(reinterpret_cast<char *>(to), 0, c);
+    if (to_one) one.template store<float>(reinterpret_cast<char *>(to_one), 0, c);
+    if (to_two) two.template store<float>(reinterpret_cast<char *>(to_two), 0, c);
   }
-  EACH(u, e) acc.v[u][e] = 0.f;
 }
 
 // The vectors' order in the sums that workgroups leave: pre, pre_bias, post, post_bias, gate.
-template <class T, class R, int C, int KIND, int THREADS>
-__global__ void __launch_bounds__(THREADS) k_residual_norm_grad(NormArgs A) {
-  extern __shared__ float s_join[];
-  __shared__ float s_red[2][kWidest][4];
+// A row's sums are taken together: means, where they come out first; squares and products with
+// g; and those with post e, which need t.  The factors are taken out of the products.
+template <class T, class R, int C, int KIND, bool NARROW>
+__global__ void __launch_bounds__(64 * kWidest) k_residual_norm_grad(NormArgs A) {
+  extern __shared__ __align__(16) float s_dynamic[];
+  __shared__ float s_red[2][kSums][kWidest];
   constexpr bool bias = (KIND & kBias) != 0, branch = (KIND & kBranch) != 0;
-  A.mask.begin();
-  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), team = wave / A.W;
-  RowSum sum{s_red, wave, A.W, 0};
+  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), team = A.waves.quotient(wave);
+  RowSum sum{s_red, wave, team, A.W, 0};
   Column c[C];
-  columns_of(c, A);
-  Row<C> pre, post, post_bias, gate;
-  Row<C> d_pre = {}, d_pre_bias = {}, d_post = {}, d_post_bias = {}, d_gate = {};
-#pragma unroll
-  for (int u = 0; u < C; u++) {
-    parameters<T>(pre.v[u], A.pre, A.wide, c[u], 0.f);
-    if (branch) {
-      parameters<T>(post.v[u], A.post, A.wide, c[u], 0.f);
-      if (bias) parameters<T>(post_bias.v[u], A.post_bias, A.wide, c[u], 0.f);
-      parameters<T>(gate.v[u], A.ptr ? nullptr : A.gate, A.wide, c[u], 1.f);
-    }
-  }
-  const bool reads_f = branch && (A.post || A.gate);
+  columns_of(c, A, team);
+  const int padded = (A.h + 7) & ~7;
+  Vectors<T> vectors{s_dynamic, {A.pre, A.post, A.ptr ? nullptr : A.gate, A.post_bias}, A.wide, A.h, padded};
+  float *const s_join = s_dynamic + (C == 1 ? vectors_of(KIND) * padded : 0);
   const int64_t first = blockIdx.x * A.per, last = min(A.T, first + A.per);
+  Raw<T, C, NARROW> f_next, dz_next;
+  Raw<R, C, NARROW> y_next, dy_next;
+  const int teams = A.teams;
+  // Every load of a row, whether the call has need of it or not (then it is another's place): a branch
+  // between them would make a wave wait for the ones before it.  Rows that are not there: the last in their place.
+  auto load = [&](int64_t t) {
+    t = min(t, last - 1);
+    dz_next.load(A.dz, t * A.dz_row, c, A.h);
+    y_next.load(A.x, t * A.x_row, c, A.h);
+    dy_next.load(A.dy, t * A.dy_row, c, A.h);
+    if (branch) f_next.load(A.f, t * A.f_row, c, A.h);
+  };
+  load(first + team);
+  Mask mask = A.mask;
+  mask.begin();
+  Row<C> d_pre = {}, d_pre_bias = {}, d_post = {}, d_post_bias = {}, d_gate = {};
+  if (C == 1) {
+    if (A.pre) vectors.stage(kPre);
+    if (branch) {
+      if (A.post) vectors.stage(kPost);
+      if (!A.ptr) vectors.stage(kGate);
+      if (bias && A.post_bias) vectors.stage(kPostBias);
+    }
+    lds_barrier();
+  }
+  const float over = 1.f / A.h;
   int s = -1;
   for (int64_t from = first; from < last;) {
     int64_t to = last;
@@ -294,80 +400,146 @@ __global__ void __launch_bounds__(THREADS) k_residual_norm_grad(NormArgs A) {
       int64_t end;
       s = sequence_at(A, from, s + 1, end);
       to = min(last, end);
-#pragma unroll
-      for (int u = 0; u < C; u++)
-        if (s >= 0)
-          parameters<T>(gate.v[u], static_cast<const char *>(A.gate) + (int64_t)s * A.h * (A.wide ? 4 : sizeof(T)), A.wide, c[u], 0.f);
+      if (s >= 0) {
+        vectors.at[kGate] = static_cast<const char *>(A.gate) + (int64_t)s * A.h * (A.wide ? 4 : sizeof(T));
+        if (C == 1) {
+          lds_barrier();  // the segment before has read its gates
+          vectors.stage(kGate);
+          lds_barrier();
+        }
+      }
+      if (from > first) load(from + team);
     }
     const bool open = !(branch && A.ptr) || s >= 0;
-    for (int64_t base = from; base < to; base += A.teams) {
+    for (int64_t base = from; base < to; base += teams) {
       const int64_t t = base + team;
-      const bool real = t < to, live = real && open;
-      Row<C> dy, dz, y, f;
-      dy.template load<R>(A.dy, t * A.dy_row, c, real && A.dy);
+      const bool real = t < to;
+      Row<C> dy, y, f, g, dz;
+      dz.from(dz_next, c, A.h);
+      y.from(y_next, c, A.h);
+      dy.from(dy_next, c, A.h);
+      if (branch) f.from(f_next, c, A.h);
+      const int64_t tn = min(t + teams, last - 1);
+      if (branch) f_next.load(A.f, tn * A.f_row, c, A.h);
+      if (!A.has_dy) dy.fill(0.f);
+      float m[3] = {0.f, 0.f, 0.f}, q[3] = {0.f, 0.f, 0.f};
       if (A.pre) {
-        dz.template load<T>(A.dz, t * A.dz_row, c, real);
-        y.template load<R>(A.x, t * A.x_row, c, real);
+        vectors.get(g, kPre, c);
+        EACH(u, e) g.v[u][e] *= dz.v[u][e];
       }
-      if (reads_f) f.template load<T>(A.f, t * A.f_row, c, real);
+      if (A.center) {
+        if (A.pre) EACH(u, e) m[0] += y.v[u][e], m[1] += g.v[u][e];
+        if (branch && A.post) EACH(u, e) m[2] += f.v[u][e];
+        sum(m);
+        m[0] *= over, m[1] *= over, m[2] *= over;
+        if (A.pre) {
+          EACH(u, e) y.v[u][e] -= m[0];
+          y.cut(c);
+        }
+        if (branch && A.post) {
+          EACH(u, e) f.v[u][e] -= m[2];
+          f.cut(c);
+        }
+      }
+      if (A.pre) EACH(u, e) q[0] = fmaf(y.v[u][e], y.v[u][e], q[0]), q[1] = fmaf(g.v[u][e], y.v[u][e], q[1]);
+      if (branch && A.post) EACH(u, e) q[2] = fmaf(f.v[u][e], f.v[u][e], q[2]);
+      if (A.pre || (branch && A.post)) sum(q);
       if (A.pre) {
-        const float r = normalise(y, A, c, sum);
-        Row<C> g;
-        EACH(u, e) g.v[u][e] = dz.v[u][e] * pre.v[u][e];
-        norm_gradient(g, y, r, A, c, sum);
+        const float r = rsqrtf(q[0] * over + A.eps), k = q[1] * over * r * r * r, b = m[1] * r;
         if (real) {  // a row that is not there may have no norm
           EACH(u, e) {
-            d_pre.v[u][e] = fmaf(dz.v[u][e], y.v[u][e], d_pre.v[u][e]);
+            d_pre.v[u][e] = fmaf(dz.v[u][e], y.v[u][e] * r, d_pre.v[u][e]);
             if (bias) d_pre_bias.v[u][e] += dz.v[u][e];
           }
         }
-        EACH(u, e) dy.v[u][e] += g.v[u][e];
+        EACH(u, e) dy.v[u][e] = fmaf(g.v[u][e], r, fmaf(y.v[u][e], -k, dy.v[u][e]));
+        if (A.center) {
+          EACH(u, e) dy.v[u][e] -= b;
+          dy.cut(c);
+        }
       }
-      Row<C> dx;
-      EACH(u, e) dx.v[u][e] = dy.v[u][e] * A.scale;
-      if (real) dx.template store<R>(A.y, t * A.y_row, c);
+      if (A.scale == 1.f) {
+        if (real) dy.template store<R>(A.y, t * A.y_row, c);
+      } else {
+        EACH(u, e) g.v[u][e] = dy.v[u][e] * A.scale;
+        if (real) g.template store<R>(A.y, t * A.y_row, c);
+      }
+      dz_next.load(A.dz, tn * A.dz_row, c, A.h);
+      y_next.load(A.x, tn * A.x_row, c, A.h);
+      dy_next.load(A.dy, tn * A.dy_row, c, A.h);
       if (!A.z) continue;  // no branch at all
-      float r = 0.f;
-      if (branch && A.post) r = normalise(f, A, c, sum);
-      if (branch && A.gate) {
-        Row<C> n;
-        EACH(u, e) n.v[u][e] = A.post ? f.v[u][e] * r * post.v[u][e] + (bias ? post_bias.v[u][e] : 0.f) : f.v[u][e];
-        if (A.mask.least) {
-#pragma unroll
-          for (int u = 0; u < C; u++) A.mask.apply(n.v[u], c[u].at >> 3, (uint32_t)t);
-        }
-        if (live) {
-          EACH(u, e) d_gate.v[u][e] = fmaf(dy.v[u][e], n.v[u][e], d_gate.v[u][e]);
-        }
-        EACH(u, e) dy.v[u][e] = open ? dy.v[u][e] * gate.v[u][e] : 0.f;
+      if (!open) {  // a row of no sequence
+        dy.fill(0.f);
+        if (real) dy.template store<T>(A.z, t * A.z_row, c);
+        continue;
       }
-      if (A.mask.least) {
+      // From here on dy is t where the mask keeps it, times the mask's factor and r: r is in every product that follows but
+      // one, so that f need not be multiplied by it.
+      const float r = branch && A.post ? rsqrtf(q[2] * over + A.eps) : 1.f;
+      if (mask.least) {
+        const float by = mask.by * r;
 #pragma unroll
-        for (int u = 0; u < C; u++) A.mask.apply(dy.v[u], c[u].at >> 3, (uint32_t)t);
+        for (int u = 0; u < C; u++) {
+          bool k[8];
+          mask.kept(k, c[u].at >> 3, (uint32_t)t);
+#pragma unroll
+          for (int e = 0; e < 8; e++) dy.v[u][e] = k[e] ? dy.v[u][e] * by : 0.f;
+        }
+      } else if (branch && A.post) {
+        EACH(u, e) dy.v[u][e] *= r;
+      }
+      if (branch && A.gate) {
+        if (A.post) {
+          vectors.get(g, kPost, c);
+          EACH(u, e) g.v[u][e] *= f.v[u][e];
+          if (bias && A.post_bias) {
+            Row<C> b;
+            vectors.get(b, kPostBias, c);
+            EACH(u, e) g.v[u][e] = fmaf(b.v[u][e], 1.f / r, g.v[u][e]);
+          }
+          if (real) EACH(u, e) d_gate.v[u][e] = fmaf(dy.v[u][e], g.v[u][e], d_gate.v[u][e]);
+        } else if (real) {
+          EACH(u, e) d_gate.v[u][e] = fmaf(dy.v[u][e], f.v[u][e], d_gate.v[u][e]);
+        }
+        vectors.get(g, kGate, c);
+        EACH(u, e) dy.v[u][e] *= g.v[u][e];
       }
       if (branch && A.post) {
-        Row<C> g;
-        EACH(u, e) g.v[u][e] = dy.v[u][e] * post.v[u][e];
-        norm_gradient(g, f, r, A, c, sum);
-        if (live) {
-          EACH(u, e) {
-            d_post.v[u][e] = fmaf(dy.v[u][e], f.v[u][e], d_post.v[u][e]);
-            if (bias) d_post_bias.v[u][e] += dy.v[u][e];
-          }
+        if (real) {
+          EACH(u, e) d_post.v[u][e] = fmaf(dy.v[u][e], f.v[u][e], d_post.v[u][e]);
+          if (bias && A.post_bias) EACH(u, e) d_post_bias.v[u][e] = fmaf(dy.v[u][e], 1.f / r, d_post_bias.v[u][e]);
         }
-        EACH(u, e) dy.v[u][e] = open ? g.v[u][e] : 0.f;
+        vectors.get(g, kPost, c);
+        float p[1] = {0.f};
+        EACH(u, e) {
+          dy.v[u][e] *= g.v[u][e];
+          p[0] = fmaf(dy.v[u][e], f.v[u][e], p[0]);
+        }
+        if (A.center) {
+          float both[2] = {p[0], 0.f};
+          EACH(u, e) both[1] += dy.v[u][e];
+          sum(both);
+          p[0] = both[0], both[1] *= over;
+          EACH(u, e) dy.v[u][e] -= both[1];
+        } else {
+          sum(p);
+        }
+        p[0] *= over * r * r;
+        EACH(u, e) dy.v[u][e] = fmaf(f.v[u][e], -p[0], dy.v[u][e]);
       }
       if (real) dy.template store<T>(A.z, t * A.z_row, c);
     }
-    if (branch && A.gate && s + 1 + (A.ptr == nullptr) > 0)
-      leave_sums(d_gate, A, A.part + (4 * A.slots + blockIdx.x + (A.ptr ? s : 0)) * A.h, c, team, s_join);
+    if (branch && A.gate && open) {
+      leave_sums(d_gate, A.part + (4 * A.slots + blockIdx.x + (A.ptr ? s : 0)) * A.h, d_gate, nullptr, A, c, team, s_join);
+      d_gate.fill(0.f);
+    }
     from = to;
   }
   float *part = A.part + (int64_t)blockIdx.x * A.h;
-  if (A.pre) leave_sums(d_pre, A, part, c, team, s_join);
-  if (bias && A.pre_bias) leave_sums(d_pre_bias, A, part + A.slots * A.h, c, team, s_join);
-  if (branch && A.post) leave_sums(d_post, A, part + 2 * A.slots * A.h, c, team, s_join);
-  if (branch && bias && A.post_bias) leave_sums(d_post_bias, A, part + 3 * A.slots * A.h, c, team, s_join);
+  const int64_t apart = A.slots * A.h;
+  if (A.pre) leave_sums(d_pre, part, d_pre_bias, bias && A.pre_bias ? part + apart : nullptr, A, c, team, s_join);
+  if (branch && A.post)
+    leave_sums(d_post, part + 2 * apart, d_post_bias, bias && A.post_bias ? part + 3 * apart : nullptr, A, c, team, s_join);
 }
 
 struct SumArgs {
@@ -397,7 +569,16 @@ __global__ void __launch_bounds__(64 * kSumWaves) k_norm_sums(SumArgs A) {
   const int64_t each = (b - a + kSumWaves - 1) / kSumWaves;
   if (column < A.h) {
     const float *p = A.part + which * A.slots * A.h + column;
-    for (int64_t k = a + wave * each; k < min(b, a + (wave + 1) * each); k++) x += p[k * A.h];
+    int64_t k = a + wave * each;
+    const int64_t end = min(b, k + each);
+    for (; k + 8 <= end; k += 8) {  // eight on their way at once
+      float y[8];
+#pragma unroll
+      for (int i = 0; i < 8; i++) y[i] = p[(k + i) * A.h];
+#pragma unroll
+      for (int i = 0; i < 8; i++) x += y[i];
+    }
+    for (; k < end; k++) x += p[k * A.h];
   }
   s_sum[wave][lane] = x;
   __syncthreads();
@@ -412,12 +593,12 @@ struct Shape {
   int C, W, teams;
   int64_t per, groups;
 };
-Shape shape_of(const cel_norm_args *a, int64_t most) {
+Shape shape_of(const cel_norm_args *a, int waves, int64_t most) {
   Shape s;
   const int eights = (int)((a->hidden + 7) / 8);
-  s.C = eights > 64 ? kMost : 1;
+  s.C = eights > 64 * kWidest ? kMost : 1;
   s.W = (eights + 64 * s.C - 1) / (64 * s.C);
-  s.teams = std::max(1, kWaves / s.W);
+  s.teams = std::max(1, waves / s.W);
   const int64_t groups = std::max<int64_t>(1, std::min(most, (a->rows + s.teams - 1) / s.teams));
   s.per = std::max<int64_t>(1, (a->rows + groups - 1) / groups);
   s.groups = (a->rows + s.per - 1) / s.per;
@@ -446,7 +627,9 @@ int check_matrix(const cel_matrix *x, const cel_norm_args *a, int type, const ch
   return CEL_OK;
 }
 NormArgs args_of(const cel_norm_args *a, const Shape &s) {
-  NormArgs A{};
+  NormArgs A;
+  memset(static_cast<void *>(&A), 0, sizeof A);
+  A.waves = Divisor(s.W);
   A.pre = a->pre, A.pre_bias = a->pre_bias, A.post = a->post, A.post_bias = a->post_bias, A.gate = a->gate;
   A.wide = a->param_type == CEL_F32;
   A.center = a->center != 0;
@@ -458,22 +641,21 @@ NormArgs args_of(const cel_norm_args *a, const Shape &s) {
 }
 int64_t slots_of(const cel_norm_args *a) { return kGroups + (a->seq_ptr ? a->n_seq : 0); }
 
-// go(type, stream type, eights of a lane, kind, threads at most)
+// go(type, stream type, eights of a lane, kind, whether rows are narrower than eight)
 template <class F>
 void by_type(const cel_norm_args *a, const Shape &s, F go) {
   const int kind = (a->pre_bias || a->post_bias ? kBias : 0) | (a->post || a->gate ? kBranch : 0);
   auto with = [&](auto t, auto r) {
-    auto more = [&](auto c, auto threads) {
-      if (kind == 0) go(t, r, c, std::integral_constant<int, 0>{}, threads);
-      else if (kind == 1) go(t, r, c, std::integral_constant<int, 1>{}, threads);
-      else if (kind == 2) go(t, r, c, std::integral_constant<int, 2>{}, threads);
-      else go(t, r, c, std::integral_constant<int, 3>{}, threads);
+    auto more = [&](auto c, auto narrow) {
+      if (kind == 0) go(t, r, c, std::integral_constant<int, 0>{}, narrow);
+      else if (kind == 1) go(t, r, c, std::integral_constant<int, 1>{}, narrow);
+      else if (kind == 2) go(t, r, c, std::integral_constant<int, 2>{}, narrow);
+      else go(t, r, c, std::integral_constant<int, 3>{}, narrow);
     };
-    constexpr std::integral_constant<int, kMost> most{};
-    constexpr std::integral_constant<int, 64 * kWaves> usual{};
-    if (s.C == 1) more(std::integral_constant<int, 1>{}, usual);
-    else if (s.W <= kWaves) more(most, usual);
-    else more(most, std::integral_constant<int, 64 * kWidest>{});
+    constexpr std::integral_constant<int, 1> one{};
+    if (a->hidden < 8) more(one, std::true_type{});
+    else if (s.C == 1) more(one, std::false_type{});
+    else more(std::integral_constant<int, kMost>{}, std::false_type{});
   };
   const bool wide = a->stream_type == CEL_F32;
   if (a->type == CEL_F32) with(float{}, float{});
@@ -497,14 +679,14 @@ extern "C" int cel_residual_norm(const cel_norm_args *a, const cel_matrix *f, co
   CEL_TRY(check_matrix(x, a, a->stream_type, fn, "x"));
   if (f) CEL_TRY(check_matrix(y, a, a->stream_type, fn, "y"));
   if (a->pre) CEL_TRY(check_matrix(z, a, a->type, fn, "z"));
-  const Shape s = shape_of(a, 4 * kGroups);
+  const Shape s = shape_of(a, kForward, 4 * kGroups);
   NormArgs A = args_of(a, s);
   if (f) A.f = (const char *)f->p, A.f_row = f->stride, A.y = (char *)y->p, A.y_row = y->stride;
   A.x = (const char *)x->p, A.x_row = x->stride;
   if (a->pre) A.z = (char *)z->p, A.z_row = z->stride;
   KTimer kt(st, "k_residual_norm");
-  by_type(a, s, [&](auto t, auto r, auto c, auto kind, auto threads) {
-    k_residual_norm<decltype(t), decltype(r), decltype(c)::value, decltype(kind)::value, decltype(threads)::value>
+  by_type(a, s, [&](auto t, auto r, auto c, auto kind, auto narrow) {
+    k_residual_norm<decltype(t), decltype(r), decltype(c)::value, decltype(kind)::value, decltype(narrow)::value>
         <<<(unsigned)s.groups, 64 * s.W * s.teams, 0, st>>>(A);
   });
   CEL_HIP(hipGetLastError());
@@ -528,7 +710,7 @@ extern "C" int cel_residual_norm_grad(const cel_norm_args *a, const cel_matrix *
     return set_error(CEL_E_ARG, "%s: a parameter without a place for its gradient", fn);
   if (!scratch) return set_error(CEL_E_ARG, "%s: scratch is NULL", fn);
   if (!dy && !a->pre) return set_error(CEL_E_ARG, "%s: neither dy nor a norm before the next block", fn);
-  const Shape s = shape_of(a, kGroups);
+  const Shape s = shape_of(a, kBackward, kGroups);
   NormArgs A = args_of(a, s);
   A.part = static_cast<float *>(scratch);
   A.slots = slots_of(a);
@@ -541,17 +723,28 @@ extern "C" int cel_residual_norm_grad(const cel_norm_args *a, const cel_matrix *
     if (a->post || a->gate) CEL_TRY(check_matrix(f, a, a->type, fn, "f"));
     CEL_TRY(check_matrix(dx, a, a->stream_type, fn, "dx"));
     if (df) CEL_TRY(check_matrix(df, a, a->type, fn, "df"));
-    if (dy) A.dy = (const char *)dy->p, A.dy_row = dy->stride;
+    // what a call lacks is read where another array lies, and not looked at
+    A.has_dy = dy != nullptr;
+    const cel_matrix *some = dy ? dy : y;
+    A.dy = (const char *)some->p, A.dy_row = some->stride;
+    A.x = A.dz = A.dy, A.x_row = A.dy_row, A.dz_row = A.dy_row * (a->stream_type == a->type ? 1 : 2);
     if (a->pre) A.dz = (const char *)dz->p, A.dz_row = dz->stride, A.x = (const char *)y->p, A.x_row = y->stride;
     if (a->post || a->gate) A.f = (const char *)f->p, A.f_row = f->stride;
     A.y = (char *)dx->p, A.y_row = dx->stride;
     if (df) A.z = (char *)df->p, A.z_row = df->stride;
     KTimer kt(st, "k_residual_norm_grad");
-    by_type(a, s, [&](auto t, auto r, auto c, auto kind, auto threads) {
-      k_residual_norm_grad<decltype(t), decltype(r), decltype(c)::value, decltype(kind)::value, decltype(threads)::value>
-          <<<(unsigned)s.groups, 64 * s.W * s.teams, s.teams > 1 ? 4 * s.teams * A.h : 0, st>>>(A);
+    int rc = CEL_OK;
+    by_type(a, s, [&](auto t, auto r, auto c, auto kind, auto narrow) {
+      const auto kernel = k_residual_norm_grad<decltype(t), decltype(r), decltype(c)::value, decltype(kind)::value, decltype(narrow)::value>;
+      const int lds = 4 * ((s.C == 1 ? vectors_of(kind) * ((A.h + 7) & ~7) : 0) + (s.teams > 1 ? (kind & kBias ? 2 : 1) * s.teams * A.h : 0));
+      rc = [&]() -> int {
+        if (lds > 65536) CEL_HIP(hipFuncSetAttribute(reinterpret_cast<const void *>(kernel), hipFuncAttributeMaxDynamicSharedMemorySize, lds));
+        kernel<<<(unsigned)s.groups, 64 * s.W * s.teams, lds, st>>>(A);
+        CEL_HIP(hipGetLastError());
+        return CEL_OK;
+      }();
     });
-    CEL_HIP(hipGetLastError());
+    CEL_TRY(rc);
   }
   if (!a->pre && !a->post && !a->gate) return CEL_OK;
   SumArgs S{A.part,
