@@ -415,8 +415,12 @@ typedef struct {
 } cel_cross_attn;
 
 /* As cel_attention, but for who sees whom.  A token whose sequence has no
- * keys has out = 0 and lse = -infinity, as one of no sequence. */
-int cel_cross_attention(const cel_cross_attn *a, const cel_rows *out, float *lse, hipStream_t stream);
+ * keys has out = 0 and lse = -infinity, as one of no sequence.  scratch:
+ * cel_cross_attention_scratch(a) bytes, aligned to 256 (NULL where that is 0). */
+int cel_cross_attention(const cel_cross_attn *a, const cel_rows *out, float *lse, void *scratch, hipStream_t stream);
+
+/* Bytes of scratch that cel_cross_attention takes for a, or CEL_E_ARG. */
+int64_t cel_cross_attention_scratch(const cel_cross_attn *a);
 
 /* Its gradient, as cel_attention_grad.  A key of no sequence, or of one
  * without tokens, has gradients of 0.  scratch:

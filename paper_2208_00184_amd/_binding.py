@@ -27,7 +27,7 @@ EXPORTS = ("cel_topo_levels", "cel_blevel", "cel_cpd_order", "cel_dfs_order", "c
            "cel_topo_levels_info", "cel_cluster_info",
            "cel_order_place", "cel_comm_sums", "cel_makespan_model", "cel_colocate",
            "cel_attention", "cel_attention_grad", "cel_attention_grad_scratch",
-           "cel_cross_attention", "cel_cross_attention_grad", "cel_cross_attention_grad_scratch", "cel_embed", "cel_embed_grad", "cel_embed_grad_scratch",
+           "cel_cross_attention", "cel_cross_attention_scratch", "cel_cross_attention_grad", "cel_cross_attention_grad_scratch", "cel_embed", "cel_embed_grad", "cel_embed_grad_scratch",
            "cel_rotary", "cel_rotary_grad", "cel_dropout", "cel_residual_norm", "cel_residual_norm_grad", "cel_residual_norm_grad_scratch",
            "cel_step_latency", "cel_timing", "cel_kernel_stats", "cel_last_error", "cel_version")
 
@@ -143,7 +143,9 @@ def lib() -> C.CDLL:
         L.cel_attention_grad_scratch.restype = i64
         L.cel_attention_grad.argtypes = [At, Ro, vp, Ro, vp, Ro, Ro, Ro, vp]
         Cr, Em = C.POINTER(_Cross), C.POINTER(_Embed)
-        L.cel_cross_attention.argtypes = [Cr, Ro, vp, vp]
+        L.cel_cross_attention.argtypes = [Cr, Ro, vp, vp, vp]
+        L.cel_cross_attention_scratch.argtypes = [Cr]
+        L.cel_cross_attention_scratch.restype = i64
         L.cel_cross_attention_grad_scratch.argtypes = [Cr]
         L.cel_cross_attention_grad_scratch.restype = i64
         L.cel_cross_attention_grad.argtypes = [Cr, Ro, vp, Ro, vp, Ro, Ro, Ro, vp]
@@ -701,8 +703,16 @@ def _attention(fn, q, k, v, scale, *ptrs):
         out = torch.empty(q.shape, dtype=q.dtype, device=q.device)
         lse = torch.empty((a.heads, a.tokens), dtype=torch.float32, device=q.device)
         rows = _Rows(out.data_ptr(), a.heads * a.dim, a.dim)
-        call = lib().cel_attention if len(ptrs) == 1 else lib().cel_cross_attention
-        _check(call(C.byref(a), C.byref(rows), lse.data_ptr(), _raw_stream(index)))
+        if len(ptrs) == 1:
+            _check(lib().cel_attention(C.byref(a), C.byref(rows), lse.data_ptr(), _raw_stream(index)))
+            return out, lse
+        size, scratch = lib().cel_cross_attention_scratch(C.byref(a)), None
+        if size < 0:
+            _check(size)
+        if size:
+            scratch = torch.empty(size, dtype=torch.uint8, device=q.device)
+        _check(lib().cel_cross_attention(C.byref(a), C.byref(rows), lse.data_ptr(), None if scratch is None else scratch.data_ptr(),
+                                         _raw_stream(index)))
     return out, lse
 
 

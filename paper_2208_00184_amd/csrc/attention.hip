@@ -126,6 +126,7 @@ struct AttnArgs {
   float *part;  // and behind it, where a key/value head's query heads are dealt out to `parts` workgroups, dk
                 // and dv of each part, [parts][2][keys][kv_heads][dim]
   int32_t parts;
+  int32_t *order, *k_order;  // CROSS: the tiles of rows and of keys with the longest first, or NULL: as they come
   float scale;
 };
 
@@ -492,7 +493,8 @@ __device__ __forceinline__ bool attention_tile(const AttnArgs &A, char *s_k0, ch
   const int tid = threadIdx.x % (kWaves * 64), lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int group = G > 1 ? __builtin_amdgcn_readfirstlane(threadIdx.x / (kWaves * 64)) : 0;
   const Item item = item_of(blockIdx.x, gridDim.x, A.H);
-  const int head = item.unit, tile = A.tiles - 1 - item.tile, kvh = head / (A.H / A.K);
+  const int head = item.unit, kvh = head / (A.H / A.K);
+  const int tile = CROSS ? A.order ? A.order[item.tile] : item.tile : A.tiles - 1 - item.tile;
   const int i = tile * kBlock + wave * kRows + (lane & 31);  // this lane's row
   const Reach R = reach_of<CROSS>(A, i, true, s_reach + 2 * group, wave);
   u32x4 q[DC / 16];
@@ -652,7 +654,8 @@ __device__ __forceinline__ bool dq_tile(const AttnArgs &A, char *s_k0, char *s_k
   const int tid = threadIdx.x % (kWaves * 64), lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int group = G > 1 ? __builtin_amdgcn_readfirstlane(threadIdx.x / (kWaves * 64)) : 0;
   const Item item = item_of(blockIdx.x, gridDim.x, A.H);
-  const int head = item.unit, tile = A.tiles - 1 - item.tile, kvh = head / (A.H / A.K);
+  const int head = item.unit, kvh = head / (A.H / A.K);
+  const int tile = CROSS ? A.order ? A.order[item.tile] : item.tile : A.tiles - 1 - item.tile;
   const int first = tile * kBlock + wave * kRows, i = first + (lane & 31);
   const Reach R = reach_of<CROSS>(A, i, true, s_reach + 2 * group, wave);
   u32x4 q[DC / 16], g[DC / 16];
@@ -956,7 +959,8 @@ __device__ __forceinline__ bool dkv_tile(const AttnArgs &A, char *s_q0, char *s_
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), g4 = 4 * (lane >> 4);
   const Item item = item_of(blockIdx.x, gridDim.x, A.K * A.parts);
   const int kvh = item.unit / A.parts, part = item.unit % A.parts;
-  const int j = item.tile * kKeyBlock + wave * kKeys + (lane & 15);  // this lane's key
+  const int tile = CROSS && A.k_order ? A.k_order[item.tile] : item.tile;
+  const int j = tile * kKeyBlock + wave * kKeys + (lane & 15);  // this lane's key
   int head0, heads;
   heads_of(A, kvh, part, head0, heads);
   const Reach R = reach_of<CROSS>(A, j, false, s_reach, wave);
@@ -1099,6 +1103,63 @@ __global__ void __launch_bounds__(256) k_attention_join(AttnArgs A) {
   }
 }
 
+// The tiles of rows (blockIdx.x = 0) and of keys (1) in the order of how many steps
+// they walk, the longest first: with lengths apart from each other on the two sides, how long a tile
+// takes does not follow from where it is, and a long one that starts at a launch's end is
+// waited for alone.  37 sequences of 16 to 1,957 tokens and 0 to 1,288 states, 24 heads of 80 over 4:
+// forward 107 -> 94 us, dq 137 -> 123, dk and dv 206 -> 160, for 5 us here.
+constexpr int kOrderB = 1024, kOrderMost = 4096;  // threads; tiles that are ordered, at most
+__global__ void __launch_bounds__(kOrderB) k_attention_order(AttnArgs A) {
+  __shared__ int s_at[kOrderB], s_sum[kOrderB / 64];
+  const bool keys = blockIdx.x != 0;
+  const int32_t *own = keys ? A.k_ptr : A.ptr, *other = keys ? A.ptr : A.k_ptr;
+  int32_t *order = keys ? A.k_order : A.order;
+  const int n = keys ? A.U : A.T, m = keys ? A.T : A.U, size = keys ? kKeyBlock : kBlock, tiles = (n + size - 1) / size;
+  const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
+  if (!order) return;
+  s_at[tid] = 0;
+  __syncthreads();
+  int bin[kOrderMost / kOrderB];
+#pragma unroll
+  for (int k = 0; k < kOrderMost / kOrderB; k++) {
+    const int tile = k * kOrderB + tid;
+    bin[k] = 0;
+    if (tile >= tiles) continue;
+    const int first = tile * size, last = min(n, first + size) - 1;
+    int lo[2] = {0, 0}, hi[2] = {A.S, A.S};  // the last sequences that begin at or before the two
+    while (lo[0] < hi[0] || lo[1] < hi[1]) {
+#pragma unroll
+      for (int x = 0; x < 2; x++) {
+        if (lo[x] >= hi[x]) continue;
+        const int mid = (lo[x] + hi[x] + 1) >> 1;
+        if (own[mid] <= (x ? last : first)) lo[x] = mid;
+        else hi[x] = mid - 1;
+      }
+    }
+    const int64_t from = max(other[lo[0]], 0), to = min(other[min(lo[1] + 1, A.S)], m);
+    bin[k] = kOrderB - 1 - (int)min(max((to - from + kStep - 1) / kStep, (int64_t)0), (int64_t)kOrderB - 1);
+    atomicAdd(&s_at[bin[k]], 1);
+  }
+  __syncthreads();
+  const int count = s_at[tid];
+  int up = count;
+  for (int o = 1; o < 64; o <<= 1) {
+    const int y = __shfl_up(up, o);
+    if (lane >= o) up += y;
+  }
+  if (lane == 63) s_sum[wave] = up;
+  __syncthreads();
+  for (int w = 0; w < wave; w++) up += s_sum[w];
+  s_at[tid] = up - count;
+  __syncthreads();
+  // tiles of as many steps stand in any order, which no result depends on
+#pragma unroll
+  for (int k = 0; k < kOrderMost / kOrderB; k++) {
+    const int tile = k * kOrderB + tid;
+    if (tile < tiles) order[atomicAdd(&s_at[bin[k]], 1)] = tile;
+  }
+}
+
 // ------------------------------------------------------------- entry points
 // A view's address and strides: 16-byte loads and stores of whole chunks.
 int check_rows(const cel_rows *x, const cel_attn *a, const char *fn, const char *what) {
@@ -1227,12 +1288,37 @@ int check_keys(const cel_attn *a, const Keys &k, const char *fn) {
   if (k.n < 0 || k.n > INT32_MAX - 4096) return set_error(CEL_E_ARG, "%s: %d keys", fn, k.n);
   return CEL_OK;
 }
+// Whether `tiles` tiles of `units` heads are put in order: where more workgroups than the GPU holds at once leave
+// an order to choose, and more sequences than one a reason to.
+bool ordered(const cel_attn *a, const Keys &k, int64_t tiles, int64_t units) {
+  return k.cross && a->n_seq > 1 && tiles * units > 512 && tiles <= kOrderMost;
+}
+int64_t row_tiles(const cel_attn *a) { return ((int64_t)a->tokens + kBlock - 1) / kBlock; }
+int64_t key_tiles(const Keys &k) { return ((int64_t)k.n + kKeyBlock - 1) / kKeyBlock; }
+// Where the orders begin in the backward pass's scratch, in 32-bit words.
+int64_t order_at(const cel_attn *a, const Keys &k) {
+  const int parts = parts_of(a, k.n);
+  return part_at(a) + (parts > 1 ? 2 * (int64_t)parts * k.n * a->kv_heads * a->dim : 0);
+}
+bool rows_ordered(const cel_attn *a, const Keys &k) { return ordered(a, k, row_tiles(a), a->heads); }
+bool keys_ordered(const cel_attn *a, const Keys &k) { return ordered(a, k, key_tiles(k), (int64_t)a->kv_heads * parts_of(a, k.n)); }
+int64_t scratch_of(const cel_attn *a, const Keys &k, const char *fn) {
+  CEL_TRY(check_attn(a, fn));
+  CEL_TRY(check_keys(a, k, fn));
+  return rows_ordered(a, k) ? 4 * row_tiles(a) : 0;
+}
 int64_t grad_scratch(const cel_attn *a, const Keys &k, const char *fn) {
   CEL_TRY(check_attn(a, fn));
   CEL_TRY(check_keys(a, k, fn));
   CEL_TRY(check_grid(a, k.n, kKeyBlock, fn));
-  const int parts = parts_of(a, k.n);
-  return 4 * (part_at(a) + (parts > 1 ? 2 * (int64_t)parts * k.n * a->kv_heads * a->dim : 0));
+  return 4 * (order_at(a, k) + (rows_ordered(a, k) ? row_tiles(a) : 0) + (keys_ordered(a, k) ? key_tiles(k) : 0));
+}
+int put_in_order(const AttnArgs &A, hipStream_t s) {
+  if (!A.order && !A.k_order) return CEL_OK;
+  KTimer kt(s, "k_attention_order");
+  k_attention_order<<<A.k_order ? 2 : 1, kOrderB, 0, s>>>(A);
+  CEL_HIP(hipGetLastError());
+  return CEL_OK;
 }
 template <class F>
 int by_kind(const cel_attn *a, const Keys &k, F launch) {
@@ -1241,7 +1327,7 @@ int by_kind(const cel_attn *a, const Keys &k, F launch) {
   CEL_HIP(hipGetLastError());
   return CEL_OK;
 }
-int attention(const cel_attn *a, const Keys &k, const cel_rows *out, float *lse, const char *fn, hipStream_t s) {
+int attention(const cel_attn *a, const Keys &k, const cel_rows *out, float *lse, void *scratch, const char *fn, hipStream_t s) {
   int rc = check_attn(a, fn);
   if (rc || (rc = check_keys(a, k, fn))) return rc;
   if (!a->seq_ptr || !k.ptr) return set_error(CEL_E_ARG, "%s: seq_ptr is NULL", fn);
@@ -1254,6 +1340,11 @@ int attention(const cel_attn *a, const Keys &k, const cel_rows *out, float *lse,
   A.k_ptr = k.ptr, A.U = k.n;
   A.out = rows_of(out);
   A.lse = lse;
+  if (rows_ordered(a, k)) {
+    if (!scratch) return set_error(CEL_E_ARG, "%s: scratch is NULL", fn);
+    A.order = static_cast<int32_t *>(scratch);
+    CEL_TRY(put_in_order(A, s));
+  }
   return by_kind(a, k, [&](auto t, auto cross) { launch_attention<decltype(t), decltype(cross)::value>(A, s); });
 }
 int attention_grad(const cel_attn *a, const Keys &k, const cel_rows *out, const float *lse, const cel_rows *dout, void *scratch_,
@@ -1277,6 +1368,10 @@ int attention_grad(const cel_attn *a, const Keys &k, const cel_rows *out, const 
   A.rows = scratch;
   A.parts = parts_of(a, k.n);
   A.part = scratch + part_at(a);
+  int32_t *orders = reinterpret_cast<int32_t *>(scratch) + order_at(a, k);
+  if (rows_ordered(a, k)) A.order = orders, orders += row_tiles(a);
+  if (keys_ordered(a, k)) A.k_order = orders;
+  CEL_TRY(put_in_order(A, s));
   return by_kind(a, k, [&](auto t, auto cross) {
     if (A.T) launch_dq<decltype(t), decltype(cross)::value>(A, s);
     if (A.U) launch_dkv<decltype(t), decltype(cross)::value>(A, s);
@@ -1297,7 +1392,7 @@ extern "C" int64_t cel_attention_grad_scratch(const cel_attn *a) {
   return grad_scratch(a, own_keys(a), "cel_attention_grad_scratch");
 }
 extern "C" int cel_attention(const cel_attn *a, const cel_rows *out, float *lse, hipStream_t s) {
-  return attention(a, own_keys(a), out, lse, "cel_attention", s);
+  return attention(a, own_keys(a), out, lse, nullptr, "cel_attention", s);
 }
 extern "C" int cel_attention_grad(const cel_attn *a, const cel_rows *out, const float *lse, const cel_rows *dout,
                                   void *scratch, const cel_rows *dq, const cel_rows *dk, const cel_rows *dv,
@@ -1311,11 +1406,17 @@ extern "C" int64_t cel_cross_attention_grad_scratch(const cel_cross_attn *a) {
   const cel_attn b = rows_part(a);
   return grad_scratch(&b, Keys{true, a->key_ptr, a->keys}, fn);
 }
-extern "C" int cel_cross_attention(const cel_cross_attn *a, const cel_rows *out, float *lse, hipStream_t s) {
+extern "C" int64_t cel_cross_attention_scratch(const cel_cross_attn *a) {
+  const char *fn = "cel_cross_attention_scratch";
+  if (!a) return set_error(CEL_E_ARG, "%s: NULL descriptor", fn);
+  const cel_attn b = rows_part(a);
+  return scratch_of(&b, Keys{true, a->key_ptr, a->keys}, fn);
+}
+extern "C" int cel_cross_attention(const cel_cross_attn *a, const cel_rows *out, float *lse, void *scratch, hipStream_t s) {
   const char *fn = "cel_cross_attention";
   if (!a) return set_error(CEL_E_ARG, "%s: NULL descriptor", fn);
   const cel_attn b = rows_part(a);
-  return attention(&b, Keys{true, a->key_ptr, a->keys}, out, lse, fn, s);
+  return attention(&b, Keys{true, a->key_ptr, a->keys}, out, lse, scratch, fn, s);
 }
 extern "C" int cel_cross_attention_grad(const cel_cross_attn *a, const cel_rows *out, const float *lse, const cel_rows *dout,
                                         void *scratch, const cel_rows *dq, const cel_rows *dk, const cel_rows *dv,

@@ -165,21 +165,21 @@ def cross(**kw):
 def test_cross_descriptors(lib, bad):
     a, r = ctypes.byref(cross(**bad)), ctypes.byref(rows())
     assert lib.cel_cross_attention_grad_scratch(a) == ARG
-    assert lib.cel_cross_attention(a, r, SOME, None) == ARG
+    assert lib.cel_cross_attention(a, r, SOME, SOME, None) == ARG
     assert lib.cel_cross_attention_grad(a, r, SOME, r, SOME, r, r, r, None) == ARG
 
 
 def test_cross_other_arguments(lib):
     r = ctypes.byref(rows())
     assert lib.cel_cross_attention_grad_scratch(None) == ARG
-    assert lib.cel_cross_attention(None, r, SOME, None) == ARG
+    assert lib.cel_cross_attention(None, r, SOME, SOME, None) == ARG
     assert lib.cel_cross_attention_grad(None, r, SOME, r, SOME, r, r, r, None) == ARG
     for bad in (dict(seq_ptr=None), dict(key_ptr=None), dict(q=rows(p=None)), dict(k=rows(p=SOME + 8)), dict(v=rows(row=60))):
         a = ctypes.byref(cross(**bad))
-        assert lib.cel_cross_attention(a, r, SOME, None) == ARG
+        assert lib.cel_cross_attention(a, r, SOME, SOME, None) == ARG
         assert lib.cel_cross_attention_grad(a, r, SOME, r, SOME, r, r, r, None) == ARG
     a = ctypes.byref(cross())
-    assert lib.cel_cross_attention(a, None, SOME, None) == ARG and lib.cel_cross_attention(a, r, None, None) == ARG
+    assert lib.cel_cross_attention(a, None, SOME, SOME, None) == ARG and lib.cel_cross_attention(a, r, None, SOME, None) == ARG
     for at in range(7):
         args = [r, SOME, r, SOME, r, r, r]
         args[at] = None
@@ -195,3 +195,11 @@ def test_cross_scratch(lib):
     assert size() == 4 * (2 * 4 * 100 + 2 * 2 * 70 * 2 * 64)
     assert size(kv_heads=4) == 4 * 2 * 4 * 100
     assert size(tokens=0, kv_heads=4) == 0 and size(tokens=0, keys=0) == 0
+    few = lambda **kw: lib.cel_cross_attention_scratch(ctypes.byref(cross(**kw)))  # noqa: E731
+    assert few() == 0 and lib.cel_cross_attention_scratch(None) == ARG and few(tokens=-1) == ARG
+    # more workgroups than fit at once: the tiles' order, of rows, and in the gradient of keys too
+    big = dict(tokens=10000, keys=20000, heads=64, kv_heads=64)
+    assert few(**big) == 4 * 79 and few(n_seq=1, **big) == 0 and few(**{**big, "tokens": 4097 * 128}) == 0
+    assert size(**big) == 4 * (2 * 64 * 10000 + 79 + 313)
+    a, r = ctypes.byref(cross(**big, q=rows(row=64 * 64), k=rows(row=64 * 64), v=rows(row=64 * 64))), ctypes.byref(rows(row=64 * 64))
+    assert lib.cel_cross_attention(a, r, SOME, None, None) == ARG

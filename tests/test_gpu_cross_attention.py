@@ -93,6 +93,13 @@ def test_large_launches(T, U, n, H, K, d, dtype):
     check(*batch(T, U, H, K, d, dtype, T), lengths, sources, 4, 3)
 
 
+@pytest.mark.parametrize("T,U,n", [(5000, 3000, 300), (3000, 9000, 2), (20000, 70, 60), (70, 20000, 60)])
+def test_tiles_in_order_of_their_length(T, U, n):
+    """Launches whose tiles are put in order, on one side or both: each is dealt with once."""
+    lengths, sources = mixed(n, T, 0, T + n), mixed(n, U, 0, U + n)
+    check(*batch(T, U, 64, 16, 32, torch.bfloat16, T), lengths, sources)
+
+
 def test_as_many_keys_as_fit_one_tile_in_odd_places():
     """D is a sum in 32 bits for rows whose keys lie in one tile, wherever that tile is among a workgroup's."""
     lengths, sources = [1, 90, 2, 30, 128, 7], [100, 3, 64, 60, 1, 130]
