@@ -797,8 +797,7 @@ def cross_attention(q, k, v, seq_ptr, key_ptr, scale=None):
     seq_ptr[s + 1] - 1 and the states key_ptr[s] .. key_ptr[s + 1] - 1 (int32, on the device, of one length),
     and each of its tokens sees all of its states.  Types, strides, heads, dim and scale as there.
     -> (out [T, heads, dim], lse float32 [heads, T]); tokens of no sequence, or of one without states, have 0
-    and -inf.  Tokens are taken 128 at a time, over all the states of their sequences: made for as many
-    tokens as training has, not for single ones."""
+    and -inf.  Where tokens are few (one of each sequence, say), several workgroups share their states."""
     return _attention("cross_attention", q, k, v, scale, seq_ptr, key_ptr)
 
 

@@ -127,6 +127,9 @@ struct AttnArgs {
                 // and dv of each part, [parts][2][keys][kv_heads][dim]
   int32_t parts;
   int32_t *order, *k_order;  // CROSS: the tiles of rows and of keys with the longest first, or NULL: as they come
+  int32_t splits;            // CROSS: workgroups that share a tile's keys, one behind the other
+  float *split;              // where these leave their sums, [splits][heads][tokens][dim], and behind them each
+                             // row's maximum and sum of the forward pass, [splits][heads][tokens][2]
   float scale;
 };
 
@@ -473,6 +476,31 @@ __device__ __forceinline__ void mask(acc16 &x, int t, int lo, int hi, float by, 
   }
 }
 
+// CROSS: this workgroup's share of a tile's keys, from R.from on; how many steps it is.
+__device__ inline int share_of_keys(const AttnArgs &A, Reach &R) {
+  const int all = R.steps();
+  if (A.splits == 1) return all;
+  const int first = (int)((int64_t)all * blockIdx.y / A.splits), end = (int)((int64_t)all * (blockIdx.y + 1) / A.splits);
+  R.from += first * kStep;
+  return end - first;
+}
+// Row i's place among the rows of all heads and shares.
+__device__ inline int64_t split_row(const AttnArgs &A, int head, int i) { return ((int64_t)blockIdx.y * A.H + head) * A.T + i; }
+// acc[n][r] times `by` to this workgroup's share of a row, laid out as in store_rows.
+template <int N>
+__device__ inline void store_split(const AttnArgs &A, int head, int i, const acc16 (&acc)[N], int n0, float by, int lane) {
+  float *p = A.split + split_row(A, head, i) * A.d;
+#pragma unroll
+  for (int n = 0; n < N; n++)
+#pragma unroll
+    for (int g = 0; g < 4; g++) {
+      const int c = 32 * (n0 + n) + 8 * g + 4 * (lane >> 5);
+      if (c < A.d)
+        *reinterpret_cast<acc4 *>(p + c) =
+            acc4{acc[n][4 * g] * by, acc[n][4 * g + 1] * by, acc[n][4 * g + 2] * by, acc[n][4 * g + 3] * by};
+    }
+}
+
 // One tile of 128 tokens of one query head: each wave 32 of them, over the
 // keys from the first row's sequence on.  A softmax in one pass: the sums o and
 // l stand relative to 2^mc and are rescaled when the maximum m has moved.
@@ -496,7 +524,8 @@ __device__ __forceinline__ bool attention_tile(const AttnArgs &A, char *s_k0, ch
   const int head = item.unit, kvh = head / (A.H / A.K);
   const int tile = CROSS ? A.order ? A.order[item.tile] : item.tile : A.tiles - 1 - item.tile;
   const int i = tile * kBlock + wave * kRows + (lane & 31);  // this lane's row
-  const Reach R = reach_of<CROSS>(A, i, true, s_reach + 2 * group, wave);
+  Reach R = reach_of<CROSS>(A, i, true, s_reach + 2 * group, wave);
+  const int steps = CROSS ? share_of_keys(A, R) : R.steps();
   u32x4 q[DC / 16];
   load_rows(q, A.q, head, i, A.T, A.d, lane);
   const float c = A.scale * kLog2e, far = 8.f / c;
@@ -568,7 +597,7 @@ __device__ __forceinline__ bool attention_tile(const AttnArgs &A, char *s_k0, ch
       m = -INFINITY, mc = 0.f, l = 0.f;
     };
     clear();
-    through_tiles<CAREFUL>((R.steps() + G - 1) / G, load, step);
+    through_tiles<CAREFUL>((steps + G - 1) / G, load, step);
     // An infinity or NaN may come from a value that the row does not see.
     if (!CAREFUL && __syncthreads_or(R.real() && not_finite(o, 1.f))) return false;
     l = half_sum(l);
@@ -595,7 +624,13 @@ __device__ __forceinline__ bool attention_tile(const AttnArgs &A, char *s_k0, ch
           for (int r = 0; r < 16; r++) o[n][r] = o[n][r] * a0 + theirs[(16 * n + r) * 64] * a1;
       }
     }
-    if (i < A.T && group == 0) {
+    if (CROSS && G == 1 && A.splits > 1) {
+      if (i < A.T) {
+        store_split(A, head, i, o, n0, 1.f, lane);
+        float *stats = A.split + (int64_t)A.splits * A.H * A.T * A.d + 2 * split_row(A, head, i);
+        if (lane < 32) *reinterpret_cast<f32x2 *>(stats) = R.real() ? f32x2{m, l} : f32x2{-INFINITY, -1.f};
+      }
+    } else if (i < A.T && group == 0) {
       if (!R.real()) {
 #pragma unroll
         for (int n = 0; n < NB; n++) o[n] = acc16{};
@@ -657,7 +692,8 @@ __device__ __forceinline__ bool dq_tile(const AttnArgs &A, char *s_k0, char *s_k
   const int head = item.unit, kvh = head / (A.H / A.K);
   const int tile = CROSS ? A.order ? A.order[item.tile] : item.tile : A.tiles - 1 - item.tile;
   const int first = tile * kBlock + wave * kRows, i = first + (lane & 31);
-  const Reach R = reach_of<CROSS>(A, i, true, s_reach + 2 * group, wave);
+  Reach R = reach_of<CROSS>(A, i, true, s_reach + 2 * group, wave);
+  const int from = R.from, steps = CROSS ? share_of_keys(A, R) : R.steps();
   u32x4 q[DC / 16], g[DC / 16];
   load_rows(q, A.q, head, i, A.T, A.d, lane);
   load_rows(g, A.dout, head, i, A.T, A.d, lane);
@@ -745,7 +781,7 @@ __device__ __forceinline__ bool dq_tile(const AttnArgs &A, char *s_k0, char *s_k
       for (int n = 0; n < NB; n++) dq[n] = acc16{};
     };
     clear();
-    through_tiles<CAREFUL>((R.steps() + G - 1) / G, load, step);
+    through_tiles<CAREFUL>((steps + G - 1) / G, load, step);
     const float back = power(-up), by = A.scale * back;
     if (!CAREFUL && __syncthreads_or(R.real() && not_finite(dq, by))) return false;
     if constexpr (G > 1) {
@@ -765,14 +801,21 @@ __device__ __forceinline__ bool dq_tile(const AttnArgs &A, char *s_k0, char *s_k
         for (int n = 0; n < NB; n++)
 #pragma unroll
           for (int r = 0; r < 16; r++) dq[n][r] = dq[n][r] * back + theirs[(16 * n + r) * 64];
-        const int t = (R.lo - R.from) / kStep;  // the tile with all of the row's keys, if there is one
-        if (R.real() && (R.hi - R.from) / kStep == t && t & 1) D = *their_D;
+        const int t = (R.lo - from) / kStep;  // the tile with all of the row's keys, if there is one
+        if (R.real() && (R.hi - from) / kStep == t && t & 1) D = *their_D;
       }
     }
     if (i < A.T && group == 0) {
       if (!R.real()) clear();
-      store_rows<T>(A.dq, head, i, dq, n0, G > 1 ? A.scale : by, A.d, lane);
-      if (lane < 32) {
+      bool states = true;  // whether this workgroup's D is the row's: of a row with its keys in one tile, that one's
+      if (CROSS && G == 1 && A.splits > 1) {
+        store_split(A, head, i, dq, n0, by, lane);
+        const int t = (R.lo - from) / kStep, here = (R.from - from) / kStep;
+        states = R.real() && (R.hi - from) / kStep == t ? t >= here && t < here + steps : blockIdx.y == 0;
+      } else {
+        store_rows<T>(A.dq, head, i, dq, n0, G > 1 ? A.scale : by, A.d, lane);
+      }
+      if (lane < 32 && states) {
         A.rows[(int64_t)head * A.T + i] = lse2 - kPUp<T>;
         A.rows[((int64_t)A.H + head) * A.T + i] = D;
       }
@@ -831,6 +874,14 @@ struct Walk {
     if (a > R.to) a = R.from, head++;
   }
 };
+// CROSS: a part's share of all of a key/value head's query heads and their rows: equal shares of the walk,
+// wherever they begin.
+__device__ inline Walk share_of_rows(const AttnArgs &A, const Reach &R, int kvh, int part, int &count) {
+  const int group = A.H / A.K, steps = R.steps();
+  const int64_t all = (int64_t)steps * group, first = all * part / A.parts;
+  count = (int)(all * (part + 1) / A.parts - first);
+  return Walk{kvh * group + (steps ? (int)(first / steps) : 0), R.from + (steps ? (int)(first % steps) * kStep : 0)};
+}
 // The query heads of a workgroup: part `part` of those that share head kvh.
 __device__ inline void heads_of(const AttnArgs &A, int kvh, int part, int &first, int &count) {
   const int group = A.H / A.K, per = (group + A.parts - 1) / A.parts;
@@ -970,7 +1021,9 @@ __device__ __forceinline__ bool dkv_tile(const AttnArgs &A, char *s_q0, char *s_
   const float c = A.scale * kLog2e;
   const Lane16<DP> L(lane);
   const Stager<DP, Swz16<DP>> qs(A.q, A.d, tid), gs(A.dout, A.d, tid);
-  const int all = R.steps() * heads;
+  int all = R.steps() * heads;
+  Walk start{head0, R.from};
+  if constexpr (CROSS) start = share_of_rows(A, R, kvh, part, all);
   Walk copies, steps;
   auto load = [&](int, auto buf) {
     qs.load(buf.at ? s_q1 : s_q0, 2 * copies.head * A.q.head, copies.a, R.to + 1, wave);
@@ -1051,7 +1104,7 @@ __device__ __forceinline__ bool dkv_tile(const AttnArgs &A, char *s_q0, char *s_
       for (int n = 0; n < NB; n++) dk[n] = dv[n] = acc4{};
     };
     clear();
-    copies = steps = Walk{head0, R.from};
+    copies = steps = start;
     through_tiles<CAREFUL>(all, load, step);
     const float by = A.scale * power(-up - kPUp<T>);
     bool odd = false;
@@ -1160,6 +1213,46 @@ __global__ void __launch_bounds__(kOrderB) k_attention_order(AttnArgs A) {
   }
 }
 
+// Rows of the forward pass (DQ: of dq) as the sums of the shares of their keys, in the keys' order,
+// the forward pass's over the largest of their maxima.
+template <class T, bool DQ>
+__global__ void __launch_bounds__(256) k_attention_unite(AttnArgs A) {
+  const int64_t rows = (int64_t)A.H * A.T, at = ((int64_t)blockIdx.x * 256 + threadIdx.x) * 4;
+  if (at >= rows * A.d) return;
+  const int c = (int)(at % A.d);
+  const int64_t row = at / A.d;
+  const int head = (int)(row / A.T), i = (int)(row % A.T);
+  acc4 sum = {0, 0, 0, 0};
+  float by = 1.f;
+  if constexpr (DQ) {
+    for (int p = 0; p < A.splits; p++) sum += *reinterpret_cast<const acc4 *>(A.split + (p * rows + row) * A.d + c);
+  } else {
+    const f32x2 *stats = reinterpret_cast<const f32x2 *>(A.split + A.splits * rows * A.d) + row;
+    const float scale = A.scale * kLog2e;
+    float m = -INFINITY, l = 0.f;
+    for (int p = 0; p < A.splits; p++) m = fmaxf(m, stats[p * rows][0]);
+    for (int p = 0; p < A.splits; p++) {
+      const f32x2 x = stats[p * rows];
+      if (x[0] == -INFINITY) continue;  // a share without a key that the row sees
+      const float w = exp2_((x[0] - m) * scale);
+      l += x[1] * w;
+      sum += *reinterpret_cast<const acc4 *>(A.split + (p * rows + row) * A.d + c) * w;
+    }
+    by = stats[0][1] < 0.f ? 0.f : 1.f / l;
+    if (by == 0.f) sum = acc4{0, 0, 0, 0};
+    if (c == 0) A.lse[row] = m == -INFINITY ? -INFINITY : (m * scale + __builtin_amdgcn_logf(l)) * kLn2;
+  }
+  const Rows &x = DQ ? A.dq : A.out;
+  *reinterpret_cast<u32x2 *>(x.p + 2 * ((int64_t)i * x.row + (int64_t)head * x.head + c)) =
+      u32x2{pack2<T>(sum[0] * by, sum[1] * by), pack2<T>(sum[2] * by, sum[3] * by)};
+}
+template <class T, bool DQ>
+void unite(const AttnArgs &A, hipStream_t s) {
+  if (A.splits == 1) return;
+  KTimer kt(s, "k_attention_unite");
+  k_attention_unite<T, DQ><<<(unsigned)(((int64_t)A.H * A.T * A.d / 4 + 255) / 256), 256, 0, s>>>(A);
+}
+
 // ------------------------------------------------------------- entry points
 // A view's address and strides: 16-byte loads and stores of whole chunks.
 int check_rows(const cel_rows *x, const cel_attn *a, const char *fn, const char *what) {
@@ -1212,6 +1305,7 @@ AttnArgs args_of(const cel_attn *a) {
   A.S = a->n_seq, A.T = A.U = a->tokens, A.H = a->heads, A.K = a->kv_heads, A.d = a->dim;
   A.tiles = (a->tokens + kBlock - 1) / kBlock;
   A.scale = a->scale;
+  A.splits = 1;
   return A;
 }
 
@@ -1225,7 +1319,7 @@ AttnArgs args_of(const cel_attn *a) {
 // long its sequences are only the device knows.  Where all are short the second group
 // has nothing to do and costs up to 1.4 us (8 heads of 64, 16 sequences of 128: forward 10.2 -> 10.6,
 // dq 13.0 -> 14.2; 600 of 1: 10.6 -> 10.7 and 14.4 -> 15.0; 4 of 512: 14.7 -> 13.7 and 18.0 -> 18.1).
-bool split_keys(const AttnArgs &A) { return (int64_t)A.tiles * A.H <= 256 && A.U >= 512; }
+bool split_keys(const AttnArgs &A) { return A.splits == 1 && (int64_t)A.tiles * A.H <= 256 && A.U >= 512; }
 
 // kernel<T, DP, DC, ...> for the call's type and dimension: rows are staged DP
 // wide (a power of two, for the chunks' order), products run over DC dimensions.
@@ -1245,22 +1339,24 @@ void launch_attention(const AttnArgs &A, hipStream_t s) {
   KTimer kt(s, "k_attention");
   by_dim(A.d, [&](auto dp, auto dc) {
     constexpr int DP = decltype(dp)::value, DC = decltype(dc)::value;
-    const int grid = A.tiles * A.H;
+    const dim3 grid(A.tiles * A.H, A.splits);
     if (split_keys(A)) k_attention<T, DP, DC, 2, CROSS><<<grid, 2 * kWaves * 64, 0, s>>>(A);
     else k_attention<T, DP, DC, 1, CROSS><<<grid, kWaves * 64, 0, s>>>(A);
   });
+  if constexpr (CROSS) unite<T, false>(A, s);
 }
 template <class T, bool CROSS>
 void launch_dq(const AttnArgs &A, hipStream_t s) {
   KTimer kt(s, "k_attention_dq");
   by_dim(A.d, [&](auto dp, auto dc) {
     constexpr int DP = decltype(dp)::value, DC = decltype(dc)::value;
-    const int grid = A.tiles * A.H;
+    const dim3 grid(A.tiles * A.H, A.splits);
     if constexpr (DC <= 64) {  // beyond, two groups' dq does not fit in the registers (60 -> 126 us at 2,048 tokens)
       if (split_keys(A)) return k_attention_dq<T, DP, DC, 2, CROSS><<<grid, 2 * kWaves * 64, 0, s>>>(A);
     }
     k_attention_dq<T, DP, DC, 1, CROSS><<<grid, kWaves * 64, 0, s>>>(A);
   });
+  if constexpr (CROSS) unite<T, true>(A, s);
 }
 template <class T, bool CROSS>
 void launch_dkv(const AttnArgs &A, hipStream_t s) {
@@ -1288,29 +1384,62 @@ int check_keys(const cel_attn *a, const Keys &k, const char *fn) {
   if (k.n < 0 || k.n > INT32_MAX - 4096) return set_error(CEL_E_ARG, "%s: %d keys", fn, k.n);
   return CEL_OK;
 }
+int64_t row_tiles(const cel_attn *a) { return ((int64_t)a->tokens + kBlock - 1) / kBlock; }
+int64_t key_tiles(const Keys &k) { return ((int64_t)k.n + kKeyBlock - 1) / kKeyBlock; }
+// The steps that a tile of `tile` of n tokens walks on the other side of m, if all sequences are as long.
+int64_t steps_of(const cel_attn *a, int tile, int64_t n, int64_t m) {
+  const double share = std::min(1.0, (double)tile / n + 1.0 / std::max(a->n_seq, 1));
+  return (int64_t)(share * m / kStep);
+}
+// Into how many workgroups the keys of a tile of rows are dealt out where there are few rows: as many as give
+// every compute unit two, of eight steps at least, which win back the 4 us of uniting their sums.
+// One token of 16 heads of 128 over 4, 16,384 states: 205 -> 42 us; 16 sequences of one token and
+// 1,500 states each: 389 -> 43; with the gradient 300 tokens of 4 heads of 128 over 2, 8,000 states: 317 -> 94,
+// and 8,000 tokens of 2 heads of 64 over 1, 300 states (whose rows are dealt out): 122 -> 52.
+int splits_of(const cel_attn *a, const Keys &k) {
+  const int64_t units = row_tiles(a) * a->heads;
+  if (!k.cross || units == 0) return 1;
+  return (int)std::max<int64_t>(1, std::min(512 / units, steps_of(a, kBlock, a->tokens, k.n) / 8));
+}
+// The same of the rows of a tile of keys, beyond the query heads.
+int parts_of(const cel_attn *a, const Keys &k) {
+  const int parts = parts_of(a, k.n);
+  const int64_t units = key_tiles(k) * a->kv_heads;
+  if (!k.cross || units == 0) return parts;
+  return (int)std::max<int64_t>(parts, std::min(512 / units, steps_of(a, kKeyBlock, k.n, a->tokens) * (a->heads / a->kv_heads) / 8));
+}
 // Whether `tiles` tiles of `units` heads are put in order: where more workgroups than the GPU holds at once leave
 // an order to choose, and more sequences than one a reason to.
 bool ordered(const cel_attn *a, const Keys &k, int64_t tiles, int64_t units) {
   return k.cross && a->n_seq > 1 && tiles * units > 512 && tiles <= kOrderMost;
 }
-int64_t row_tiles(const cel_attn *a) { return ((int64_t)a->tokens + kBlock - 1) / kBlock; }
-int64_t key_tiles(const Keys &k) { return ((int64_t)k.n + kKeyBlock - 1) / kKeyBlock; }
 // Where the orders begin in the backward pass's scratch, in 32-bit words.
 int64_t order_at(const cel_attn *a, const Keys &k) {
-  const int parts = parts_of(a, k.n);
+  const int parts = parts_of(a, k);
   return part_at(a) + (parts > 1 ? 2 * (int64_t)parts * k.n * a->kv_heads * a->dim : 0);
 }
 bool rows_ordered(const cel_attn *a, const Keys &k) { return ordered(a, k, row_tiles(a), a->heads); }
-bool keys_ordered(const cel_attn *a, const Keys &k) { return ordered(a, k, key_tiles(k), (int64_t)a->kv_heads * parts_of(a, k.n)); }
+bool keys_ordered(const cel_attn *a, const Keys &k) { return ordered(a, k, key_tiles(k), (int64_t)a->kv_heads * parts_of(a, k)); }
+// Bytes of the shares' sums, with each row's maximum and sum (forward) or without.
+int64_t split_bytes(const cel_attn *a, const Keys &k, int more) {
+  const int64_t splits = splits_of(a, k);
+  return splits > 1 ? 4 * splits * a->heads * a->tokens * (a->dim + more) : 0;
+}
+// Where they begin in the backward pass's scratch, in 32-bit words, on 16 bytes.
+int64_t split_at(const cel_attn *a, const Keys &k) {
+  return (order_at(a, k) + (rows_ordered(a, k) ? row_tiles(a) : 0) + (keys_ordered(a, k) ? key_tiles(k) : 0) + 3) / 4 * 4;
+}
 int64_t scratch_of(const cel_attn *a, const Keys &k, const char *fn) {
   CEL_TRY(check_attn(a, fn));
   CEL_TRY(check_keys(a, k, fn));
-  return rows_ordered(a, k) ? 4 * row_tiles(a) : 0;
+  return rows_ordered(a, k) ? 4 * row_tiles(a) : split_bytes(a, k, 2);  // few rows are split, many are ordered
 }
 int64_t grad_scratch(const cel_attn *a, const Keys &k, const char *fn) {
   CEL_TRY(check_attn(a, fn));
   CEL_TRY(check_keys(a, k, fn));
   CEL_TRY(check_grid(a, k.n, kKeyBlock, fn));
+  const int64_t split = split_bytes(a, k, 0);
+  if (split) return 4 * split_at(a, k) + split;
   return 4 * (order_at(a, k) + (rows_ordered(a, k) ? row_tiles(a) : 0) + (keys_ordered(a, k) ? key_tiles(k) : 0));
 }
 int put_in_order(const AttnArgs &A, hipStream_t s) {
@@ -1340,11 +1469,13 @@ int attention(const cel_attn *a, const Keys &k, const cel_rows *out, float *lse,
   A.k_ptr = k.ptr, A.U = k.n;
   A.out = rows_of(out);
   A.lse = lse;
+  A.splits = splits_of(a, k);
+  if (!scratch && (A.splits > 1 || rows_ordered(a, k))) return set_error(CEL_E_ARG, "%s: scratch is NULL", fn);
   if (rows_ordered(a, k)) {
-    if (!scratch) return set_error(CEL_E_ARG, "%s: scratch is NULL", fn);
     A.order = static_cast<int32_t *>(scratch);
     CEL_TRY(put_in_order(A, s));
   }
+  A.split = static_cast<float *>(scratch);
   return by_kind(a, k, [&](auto t, auto cross) { launch_attention<decltype(t), decltype(cross)::value>(A, s); });
 }
 int attention_grad(const cel_attn *a, const Keys &k, const cel_rows *out, const float *lse, const cel_rows *dout, void *scratch_,
@@ -1366,8 +1497,10 @@ int attention_grad(const cel_attn *a, const Keys &k, const cel_rows *out, const 
   if (k.n) A.dk = rows_of(dk), A.dv = rows_of(dv);
   A.lse = const_cast<float *>(lse);
   A.rows = scratch;
-  A.parts = parts_of(a, k.n);
+  A.parts = parts_of(a, k);
   A.part = scratch + part_at(a);
+  A.splits = splits_of(a, k);
+  A.split = scratch + split_at(a, k);
   int32_t *orders = reinterpret_cast<int32_t *>(scratch) + order_at(a, k);
   if (rows_ordered(a, k)) A.order = orders, orders += row_tiles(a);
   if (keys_ordered(a, k)) A.k_order = orders;

@@ -100,6 +100,45 @@ def test_tiles_in_order_of_their_length(T, U, n):
     check(*batch(T, U, 64, 16, 32, torch.bfloat16, T), lengths, sources)
 
 
+FEW = [([1], [6000]), ([1, 1, 1], [3000, 0, 4000]), ([40], [2000]), ([5, 0, 130, 2], [900, 700, 3000, 1]), ([17, 90], [5000, 60])]
+
+
+@pytest.mark.parametrize("lengths,sources", FEW)
+@pytest.mark.parametrize("d,dtype,H,K", [(64, torch.bfloat16, 4, 2), (128, torch.float16, 2, 2), (40, torch.float16, 6, 1), (96, torch.bfloat16, 1, 1)])
+def test_few_rows_share_their_keys(lengths, sources, d, dtype, H, K):
+    """Rows whose keys are dealt out to several workgroups, single tokens among them, and the other way round."""
+    T, U = sum(lengths), sum(sources)
+    got = check(*batch(T + 3, U + 70, H, K, d, dtype, T), lengths, sources, 2, 64)
+    check(*batch(U + 70, T + 3, H, K, d, dtype, T), sources, lengths, 64, 2)
+    again = run(*batch(T + 3, U + 70, H, K, d, dtype, T), ptr_of(lengths, 2), ptr_of(sources, 64))
+    assert all(torch.equal(got[n], again[n]) for n in got)
+
+
+@pytest.mark.parametrize("dtype", TYPES)
+def test_infinities_and_nan_where_keys_are_shared(dtype):
+    lengths, sources = [3, 2], [3000, 2500]
+    q, k, v, g = batch(5, 5500, 2, 1, 64, dtype, 7)
+    plain = run(q, k, v, g, ptr_of(lengths), ptr_of(sources))
+    k[3100], v[4000], g[4] = math.nan, math.inf, math.nan
+    got = run(q, k, v, g, ptr_of(lengths), ptr_of(sources))
+    for n, at in (("out", slice(0, 3)), ("dq", slice(0, 3)), ("dk", slice(0, 3000)), ("dv", slice(0, 3000))):
+        assert torch.equal(got[n][at], plain[n][at]), n
+    assert torch.equal(got["lse"][:, :3], plain["lse"][:, :3]) and bool(torch.isnan(got["out"][3:]).any())
+
+
+def test_scores_of_minus_infinity():
+    """A row all of whose scores are minus infinity has no weights (0 / 0), whether its keys are shared or not; one
+    with another score has that one's alone."""
+    for U in (60, 6000):
+        q, k, v, g = batch(2, U, 1, 1, 64, torch.bfloat16, 9)
+        q[:], k[:] = 1.0, -math.inf
+        out, lse = cel.cross_attention(q, k, v, ptr_of([2]), ptr_of([U]))
+        assert bool(torch.isnan(out).all()) and bool((lse == -math.inf).all())
+        k[U // 2] = 0.5
+        out, lse = cel.cross_attention(q, k, v, ptr_of([2]), ptr_of([U]))
+        assert torch.equal(out, v[U // 2].expand(2, 1, 64)) and float((lse - 4.0).abs().max()) <= 1e-5
+
+
 def test_as_many_keys_as_fit_one_tile_in_odd_places():
     """D is a sum in 32 bits for rows whose keys lie in one tile, wherever that tile is among a workgroup's."""
     lengths, sources = [1, 90, 2, 30, 128, 7], [100, 3, 64, 60, 1, 130]
