@@ -118,6 +118,18 @@ def test_one_long_row():
         assert bool((got[first:first + 80].cpu().numpy() == bits).all())
 
 
+def test_more_pieces_than_one_launch_counts():
+    """2^32 - 100 rows of one value: two launches, the second from row 2^32 - 257 on."""
+    if torch.cuda.mem_get_info()[0] < 40 << 30:
+        pytest.skip("needs 40 GiB of memory")
+    n = (1 << 32) - 100
+    x = torch.ones(n, 1, dtype=torch.bfloat16, device=DEV)
+    got = cel.dropout(x, 0.5, 3, out=x)
+    for first in (0, (1 << 31) - 7, n - 200):
+        keep, _ = kept(200, 1, 0.5, 3, 0, row0=first)
+        assert torch.equal(got[first:first + 200].cpu() > 0, keep)
+
+
 def test_replayed_graphs_go_on():
     """A step on the device that the graph itself advances: each replay has its own mask."""
     x = randn(64, 200, seed=6).bfloat16().to(DEV)
