@@ -9,8 +9,8 @@
 // A row is read once and its statistics are made where it lies, in registers, so
 // that nothing but y and z is kept for the backward pass and nothing is read twice.
 //
-// A team of W waves takes a row, 8 columns of each lane at a time, up to kMost
-// times; the teams of a workgroup take the rows of its range in turn.  Gradients
+// A team of W waves takes a row, eight columns a lane (beyond 8,192 columns kMost
+// times as many); the teams of a workgroup take the rows of its range in turn.  Gradients
 // of vectors are sums over rows: a lane adds its columns' over its team's rows, the teams
 // join theirs in LDS, and k_norm_sums adds the workgroups', all in a fixed order.
 // Where every sequence has a gate of its own, a workgroup walks its range in
@@ -73,6 +73,13 @@ __device__ inline NormArgs again() {
 struct Column {
   int at, lack;
   bool tail;  // of any lane of the wave
+  // lack, for comparisons that are made where they are used: the few waves with a tail make them anew for
+  // every row, and the others' scalar registers are not full of their results.
+  __device__ int lack_here() const {
+    int x = lack;
+    asm volatile("" : "+v"(x));
+    return x;
+  }
 };
 template <class T, bool NARROW>  // rows of less than eight columns
 __device__ inline Eight<T> load_piece(const T *row, Column c, int h) {
@@ -82,7 +89,7 @@ __device__ inline Eight<T> load_piece(const T *row, Column c, int h) {
 template <class T, bool NARROW>
 __device__ inline void piece_values(float (&f)[8], const Eight<T> &r, Column c, int h) {
   values<T>(f, r);
-  if (!NARROW && c.tail) shift_down(f, c.lack);
+  if (!NARROW && c.tail) shift_down(f, c.lack_here());
 }
 
 // The sequence that holds row t and the first row behind t that need not be in it; -1: none.
@@ -163,15 +170,23 @@ struct Row {
 #pragma unroll
     for (int u = 0; u < C; u++)
       if (c[u].tail) {
+        const int left = 8 - c[u].lack_here();
 #pragma unroll
-        for (int e = 0; e < 8; e++) v[u][e] = e < 8 - c[u].lack ? v[u][e] : 0.f;
+        for (int e = 0; e < 8; e++) v[u][e] = e < left ? v[u][e] : 0.f;
       }
   }
   template <class T>
   __device__ void store(char *p, int64_t at, const Column (&c)[C]) const {
 #pragma unroll
-    for (int u = 0; u < C; u++)
-      if (c[u].lack < 8) store_eight(reinterpret_cast<T *>(p) + at + c[u].at, v[u], 8 - c[u].lack);
+    for (int u = 0; u < C; u++) {
+      T *to = reinterpret_cast<T *>(p) + at + c[u].at;
+      if (!c[u].tail) {
+        store_eight(to, v[u], 8);
+      } else {
+        const int left = 8 - c[u].lack_here();
+        if (left > 0) store_eight(to, v[u], left);
+      }
+    }
   }
 };
 // N vectors of parameters, all loads before the first use; `none` where there is no such vector.
@@ -228,6 +243,11 @@ __device__ inline void gates_of(Row<C> &gate, const NormArgs &A, int s, const Co
 }
 
 // T: of f and z; R: of the stream x and y.  The next row is on its way while one is dealt with.
+// Bound by memory: 4,096 rows of 8,192, f in 16 bits and a stream in 32, 403 MB in 85 us (4.7 TB/s); all in
+// 16 bits without gate and second norm 268 MB in 45 us, part of them from the caches.  4,096 rows of 1,024 take 11 us, of which
+// start, the vectors' loads and a row's two or three sums are half.  What counts is that no load stands in a branch:
+// with each row's end as a branch of its own, 9,973 rows of 2,049 columns took 89 us instead of 39.
+// 16 columns a lane: 8 % faster without gate and second norm, 3 to 6 % slower with them.
 template <class T, class R, int C, int KIND, bool NARROW>
 __global__ void __launch_bounds__(64 * kWidest) k_residual_norm(NormArgs A) {
   __shared__ float s_red[2][kSums][kWidest];
@@ -352,12 +372,20 @@ __device__ inline void leave_sums(Row<C> &one, float *to_one, Row<C> &two, float
 }
 
 // The vectors' order in the sums that workgroups leave: pre, pre_bias, post, post_bias, gate.
-// A row's sums are taken together: means, where they come out first; squares and products with
-// g; and those with post e, which need t.  The factors are taken out of the products.
+// A row's sums over its waves are barriers, which all 16 waves of a compute unit wait in: they are taken together
+// as far as they do not need each other, means first where they come out, then squares and products with
+// g, then those with post e.  The next row's loads stand behind the last use of this one's, dy, dz and y before the second
+// half, so that both halves have some under way.
+// Bound by memory and these waits: 4,096 rows of 8,192 in 16 bits with both norms, gates and dropout 403 MB and 50 of sums in
+// 101 us (4.5 TB/s; with dy, dz and y loaded at a row's beginning 112); without gate and second norm
+// 335 MB in 69 us.  All of a row's sums at once (those with post e from the three parts of t) made one barrier
+// of two and spilled 35 registers: 133 us.  16 columns a lane, 8 waves: 127 us.  512 workgroups: 141 us, twice the sums to leave.
 template <class T, class R, int C, int KIND, bool NARROW>
 __global__ void __launch_bounds__(64 * kWidest) k_residual_norm_grad(NormArgs A) {
   extern __shared__ __align__(16) float s_dynamic[];
   __shared__ float s_red[2][kSums][kWidest];
+  __shared__ int s_sequence;
+  __shared__ int64_t s_end;
   constexpr bool bias = (KIND & kBias) != 0, branch = (KIND & kBranch) != 0;
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), team = A.waves.quotient(wave);
   RowSum sum{s_red, wave, team, A.W, 0};
@@ -397,13 +425,18 @@ __global__ void __launch_bounds__(64 * kWidest) k_residual_norm_grad(NormArgs A)
   for (int64_t from = first; from < last;) {
     int64_t to = last;
     if (branch && A.ptr) {
-      int64_t end;
-      s = sequence_at(A, from, s + 1, end);
-      to = min(last, end);
+      lds_barrier();  // the segment before has read its gates
+      if (threadIdx.x == 0) {  // one thread looks, so that all waves walk the same segments whatever happens to ptr
+        int64_t end;
+        s_sequence = sequence_at(A, from, s + 1, end);
+        s_end = min(last, end);
+      }
+      lds_barrier();
+      s = __builtin_amdgcn_readfirstlane(s_sequence);
+      to = first + __builtin_amdgcn_readfirstlane((int)(s_end - first));
       if (s >= 0) {
         vectors.at[kGate] = static_cast<const char *>(A.gate) + (int64_t)s * A.h * (A.wide ? 4 : sizeof(T));
         if (C == 1) {
-          lds_barrier();  // the segment before has read its gates
           vectors.stage(kGate);
           lds_barrier();
         }
@@ -445,14 +478,15 @@ __global__ void __launch_bounds__(64 * kWidest) k_residual_norm_grad(NormArgs A)
       if (branch && A.post) EACH(u, e) q[2] = fmaf(f.v[u][e], f.v[u][e], q[2]);
       if (A.pre || (branch && A.post)) sum(q);
       if (A.pre) {
-        const float r = rsqrtf(q[0] * over + A.eps), k = q[1] * over * r * r * r, b = m[1] * r;
+        const float r = rsqrtf(q[0] * over + A.eps), k = q[1] * over * r, b = m[1] * r;
+        EACH(u, e) y.v[u][e] *= r;
         if (real) {  // a row that is not there may have no norm
           EACH(u, e) {
-            d_pre.v[u][e] = fmaf(dz.v[u][e], y.v[u][e] * r, d_pre.v[u][e]);
+            d_pre.v[u][e] = fmaf(dz.v[u][e], y.v[u][e], d_pre.v[u][e]);
             if (bias) d_pre_bias.v[u][e] += dz.v[u][e];
           }
         }
-        EACH(u, e) dy.v[u][e] = fmaf(g.v[u][e], r, fmaf(y.v[u][e], -k, dy.v[u][e]));
+        EACH(u, e) dy.v[u][e] = fmaf(fmaf(y.v[u][e], -k, g.v[u][e]), r, dy.v[u][e]);
         if (A.center) {
           EACH(u, e) dy.v[u][e] -= b;
           dy.cut(c);
@@ -481,6 +515,8 @@ __global__ void __launch_bounds__(64 * kWidest) k_residual_norm_grad(NormArgs A)
 #pragma unroll
         for (int u = 0; u < C; u++) {
           bool k[8];
+          // the ten rounds' keys are made anew for every row, beside the vector unit: twenty scalar registers less
+          asm volatile("" : "+s"(mask.k0), "+s"(mask.k1));
           mask.kept(k, c[u].at >> 3, (uint32_t)t);
 #pragma unroll
           for (int e = 0; e < 8; e++) dy.v[u][e] = k[e] ? dy.v[u][e] * by : 0.f;
@@ -549,6 +585,7 @@ struct SumArgs {
   const int32_t *ptr;
   int32_t h, S, groups;
 };
+// Bound by latency: 256 workgroups' sums of three vectors of 8,192, 25 MB, in 7.6 us, of two of 1,024 in 3.8.
 // Vector blockIdx.y as the sum of the workgroups' slots, in their order; from
 // blockIdx.y = 4 on sequence blockIdx.y - 4's gate.  64 columns a workgroup, its waves share the slots.
 constexpr int kSumWaves = 16;

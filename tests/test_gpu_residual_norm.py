@@ -168,6 +168,14 @@ def test_no_eps_and_a_ragged_end():
     check(*make(13, 1030, post=True, gate=True, bias=True, seqs=[1, 4, 12]), eps=0.0, center=True)
 
 
+@pytest.mark.parametrize("size", [1e-15, 1e-8, 1e8, 1e15])
+def test_small_and_large_rows(size):
+    """Rows whose norm's factor, to the third power, 32 bits do not hold."""
+    f, x, dy, dz, v = make(20, 300, (f32, f32, f32), post=True, gate=True)
+    v["gate"] = v["gate"] * size
+    check(f * size, x * size, dy, dz, v, eps=0.0, p=0.1)
+
+
 def test_large_means_are_taken_out_first():
     """A layer norm of rows far from 0, whose mean square would swallow the variance."""
     f, x, dy, dz, v = make(30, 700, (f32, f32, f32), post=True)
