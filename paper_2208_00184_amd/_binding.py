@@ -866,12 +866,20 @@ def _like(t, dtype):
     return torch.empty_like(t) if dtype == t.dtype and t.is_contiguous() else t.new_empty(t.shape, dtype=dtype)
 
 
+def _may_meet(x, y, d):
+    """Whether blocks of different row strides interleave in a way that does not show them to be apart."""
+    if x[2] == y[2] or x[1] <= y[0] or y[1] <= x[0]:
+        return False
+    g = math.gcd(x[2], x[3], y[2], y[3])
+    return not d <= (x[0] - y[0]) % g <= g - d if g else True
+
+
 def _apart(fn, out, x, T, d, size, *others):
     """Refuses results (a block) that share memory within themselves, with x (a block, unless they are
     x itself, in place) or with other tensors."""
     if _folded(out, T, d):
         _refuse(f"{fn}: values of out share memory")
-    if out != x and _meet(out, x, T, d):
+    if out != x and (_meet(out, x, T, d) or _may_meet(out, x, d)):
         _refuse(f"{fn}: out shares memory with x without being it")
     for t in others:
         if t is not None and t.numel():
@@ -959,13 +967,12 @@ def rotary_grad(dout, positions, freqs, axes=None, pairs=False, out=None):
 def _mask(fn, p, seed, step):
     """-> what the kernels take; the step is a number, or a tensor on the device."""
     if not isinstance(step, torch.Tensor):
-        at = None
-        step &= (1 << 64) - 1
+        at, step = None, int(step) & (1 << 64) - 1
     elif step.numel() != 1 or step.dtype != torch.int64:
         _refuse(f"{fn}: step is not a number or one int64")
     else:
         at, step = step.data_ptr(), 0
-    return _Mask(p, seed & ((1 << 64) - 1), step if step < 1 << 63 else step - (1 << 64), at)
+    return _Mask(p, int(seed) & (1 << 64) - 1, step if step < 1 << 63 else step - (1 << 64), at)
 
 
 def _matrix(t):
@@ -1119,7 +1126,7 @@ def residual_norm(f, x, pre, post=None, gate=None, seq_ptr=None, pre_bias=None, 
     with norm(v) = v / sqrt(mean(v^2) + eps) over a row, of v less its mean with center=True (a layer norm).
     f [rows, hidden], the block's output, in bfloat16, float16 or float32; x, the residual stream before it, in
     the same type or float32; hidden up to 16384; rows any stride apart.  pre, pre_bias, post, post_bias: [hidden]
-    or None; gate: [hidden], or with seq_ptr (int32 [sequences + 1], on the device) [sequences, hidden], a row for
+    or None; gate: [hidden], or with seq_ptr (int32 [sequences + 1], on the device, up to 65,530) [sequences, hidden], a row for
     the rows seq_ptr[s] .. seq_ptr[s + 1] - 1; a row of no sequence has y = scale * x.  All vectors in one type, f's
     or float32.  The mask is that of dropout() for [rows, hidden].
     -> (y as x, z as f): the stream behind the block, and the next block's input (None without pre).  f = None: no

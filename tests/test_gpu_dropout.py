@@ -169,4 +169,8 @@ def test_refusals():
     wide = torch.zeros(9, 16, device=DEV)
     refused(wide[:8], 0.1, 1, out=wide[1:])
     refused(wide.flatten()[:128], 0.1, 1, out=wide.flatten()[1:129])
+    refused(wide[:4, :8], 0.1, 1, out=wide.flatten()[4:36].view(4, 8))  # rows of another stride between
+    cel.dropout(wide[:4, :8], 0.1, 1, out=wide[:4, 8:])
+    import numpy as np
+    assert torch.equal(cel.dropout(x, 0.5, np.int64(-3), step=np.int64(-1)), cel.dropout(x, 0.5, -3, step=-1))
     refused(x.clone().requires_grad_(), 0.1, 1)

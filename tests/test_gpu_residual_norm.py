@@ -65,7 +65,7 @@ def check(f, x, dy, dz, v, **how):
 
 
 @pytest.mark.parametrize("types", TYPES)
-@pytest.mark.parametrize("h", [1, 2, 7, 8, 9, 64, 100, 511, 512, 513, 1000, 1024, 1025, 2049, 3072 + 5, 4096, 8191, 8192])
+@pytest.mark.parametrize("h", [1, 2, 7, 8, 9, 64, 100, 511, 512, 513, 1000, 1024, 1025, 2049, 3077, 4096, 8191, 8192])
 def test_widths(h, types):
     check(*make(19, h, types, post=True, gate=True, bias=True, seed=h), p=0.2, seed=h, scale=0.5)
     check(*make(19, h, types, seed=h), center=True)

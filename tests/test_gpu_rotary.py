@@ -41,7 +41,7 @@ def check(x, positions, freqs, axes=None, pairs=False, error=STEP):
 @pytest.mark.parametrize("pairs", [False, True])
 @pytest.mark.parametrize("dtype", TYPES)
 @pytest.mark.parametrize("d,P", [(64, 32), (128, 64), (80, 32), (96, 48), (40, 20), (1, 0), (2, 1), (3, 1), (7, 3), (17, 8),
-                                 (33, 9), (255, 127), (256, 64), (64, 0)])
+                                 (33, 9), (255, 127), (256, 64), (64, 0), (4096, 2048), (4096, 0), (4095, 1500)])
 def test_sizes(d, P, dtype, pairs):
     x = randn(37, 5, d, seed=d).to(dtype).to(DEV)
     check(x, torch.arange(37, device=DEV), freqs_of(P), pairs=pairs)
@@ -184,5 +184,9 @@ def test_refusals():
     refused(x, pos, f, out=torch.empty(1, 2, 16, device=DEV).expand(8, 2, 16))
     wide = torch.zeros(9, 2, 16, device=DEV)
     refused(wide[:8], pos, f, out=wide[1:])
+    refused(wide[:8], pos, f, out=wide.flatten()[8:264].view(8, 2, 16))
+    both = torch.zeros(8, 3, 2, 16, device=DEV)
+    refused(both[:, 0], pos, f, out=both.flatten()[32:288].view(8, 2, 16))  # rows of another stride between
+    cel.rotary(both[:, 0], pos, f, out=both[:, 2])
     refused(x, pos, f, out=x.flip(0)[:8].transpose(0, 1).contiguous().transpose(0, 1)[:, :1])
     refused(x.clone().requires_grad_(), pos, f)
