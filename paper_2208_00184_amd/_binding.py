@@ -700,8 +700,8 @@ def _attention(fn, q, k, v, scale, *ptrs):
     index = _device_of(fn, q=q, k=k, v=v, **dict(zip(("seq_ptr", "key_ptr"), ptrs)))
     with _on(index):
         a, keep = _attn(fn, q, k, v, ptrs[0], scale, *ptrs[1:])
-        out = torch.empty(q.shape, dtype=q.dtype, device=q.device)
-        lse = torch.empty((a.heads, a.tokens), dtype=torch.float32, device=q.device)
+        out = _like(q, q.dtype)
+        lse = q.new_empty((a.heads, a.tokens), dtype=torch.float32)
         rows = _Rows(out.data_ptr(), a.heads * a.dim, a.dim)
         if len(ptrs) == 1:
             _check(lib().cel_attention(C.byref(a), C.byref(rows), lse.data_ptr(), _raw_stream(index)))
@@ -729,7 +729,7 @@ def _attention_grad(fn, dout, q, k, v, out, lse, scale, grads, *ptrs):
         lse = lse.contiguous()
         given = grads is not None
         if not given:
-            grads = tuple(torch.empty(t.shape, dtype=q.dtype, device=q.device) for t in (q, k, v))
+            grads = tuple(_like(t, q.dtype) for t in (q, k, v))
         elif len(grads) != 3:
             _refuse(f"{fn}: grads are not three tensors")
         else:

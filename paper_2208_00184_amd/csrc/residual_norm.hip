@@ -566,7 +566,9 @@ __global__ void __launch_bounds__(64 * kWidest) k_residual_norm_grad(NormArgs A)
       if (real) dy.template store<T>(A.z, t * A.z_row, c);
     }
     if (branch && A.gate && open) {
-      leave_sums(d_gate, A.part + (4 * A.slots + blockIdx.x + (A.ptr ? s : 0)) * A.h, d_gate, nullptr, A, c, team, s_join);
+      float *slot = A.part + (4 * A.slots + blockIdx.x + (A.ptr ? s : 0)) * A.h;
+      if (to - from > 1) leave_sums(d_gate, slot, d_gate, nullptr, A, c, team, s_join);
+      else if (team == 0) d_gate.template store<float>(reinterpret_cast<char *>(slot), 0, c);  // one row, of the first team
       d_gate.fill(0.f);
     }
     from = to;
@@ -636,7 +638,9 @@ Shape shape_of(const cel_norm_args *a, int waves, int64_t most) {
   s.C = eights > 64 * kWidest ? kMost : 1;
   s.W = (eights + 64 * s.C - 1) / (64 * s.C);
   s.teams = std::max(1, waves / s.W);
-  const int64_t groups = std::max<int64_t>(1, std::min(most, (a->rows + s.teams - 1) / s.teams));
+  // With sequences shorter than the teams are many, a workgroup's would stand idle while it walks them one by one.
+  const int64_t each = a->seq_ptr ? std::min<int64_t>(s.teams, a->rows / std::max(a->n_seq, 1) + 1) : s.teams;
+  const int64_t groups = std::max<int64_t>(1, std::min(most, (a->rows + each - 1) / each));
   s.per = std::max<int64_t>(1, (a->rows + groups - 1) / groups);
   s.groups = (a->rows + s.per - 1) / s.per;
   return s;
