@@ -566,9 +566,12 @@ def _refuse(what):
     raise CelError(E_ARG, what)
 
 
+_HERE = nullcontext()
+
+
 def _on(index):
     """The device as the current one for the launches of a call."""
-    return nullcontext() if index == torch.cuda.current_device() else torch.cuda.device(index)
+    return _HERE if index == torch.cuda.current_device() else torch.cuda.device(index)
 
 
 def _raw_stream(index):
@@ -1047,7 +1050,14 @@ _VECTORS = ("pre", "pre_bias", "post", "post_bias", "gate")
 def _norm(fn, tensors, vectors, seq_ptr, scale, p, seed, step, eps, center):
     """-> (device, type of f, descriptor, matrices, tensors to keep alive): checks that residual_norm and
     residual_norm_grad share.  tensors: (name, tensor or None, whether it is as the stream), the stream's own first."""
-    given = {name: t for name, t, _ in tensors if t is not None}
+    name, stream, _ = tensors[0]
+    given = {name: stream}
+    like = None
+    for name, t, as_stream in tensors:
+        if t is not None:
+            given[name] = t
+            if not as_stream and like is None:
+                like = t
     for name, t in zip(_VECTORS, vectors):
         if t is not None:
             given[name] = t
@@ -1056,18 +1066,13 @@ def _norm(fn, tensors, vectors, seq_ptr, scale, p, seed, step, eps, center):
     if isinstance(step, torch.Tensor):
         given["step"] = step
     index = _device_of(fn, **given)
-    stream = tensors[0][1]
     shape, dtype = stream.shape, stream.dtype
     if len(shape) != 2 or dtype not in _TYPES:
         _refuse(f"{fn}: the stream is not [rows, hidden] in bfloat16, float16 or float32")
     T, h = shape
-    kind = None
-    for _, t, as_stream in tensors:
-        if t is not None and not as_stream:
-            kind = t.dtype
-            break
-    if kind is None:
-        kind = vectors[0].dtype if dtype == torch.float32 and vectors[0] is not None else dtype
+    if like is None and dtype == torch.float32:
+        like = vectors[0]
+    kind = dtype if like is None else like.dtype
     if kind not in _TYPES or (dtype != kind and dtype != torch.float32):
         _refuse(f"{fn}: a stream in {dtype} beside blocks in {kind}")
     keep, matrices = [], []
@@ -1078,14 +1083,14 @@ def _norm(fn, tensors, vectors, seq_ptr, scale, p, seed, step, eps, center):
         want = dtype if as_stream else kind
         if t.shape != shape or t.dtype != want:
             _refuse(f"{fn}: {name} is {tuple(t.shape)} {t.dtype} beside a stream of {tuple(shape)}, {want} wanted")
-        if t.is_contiguous():
-            stride = h
-        else:
+        stride = h
+        if not t.is_contiguous():
             m = _matrix(t)
             if m is None:
                 t = t.clone(memory_format=torch.contiguous_format)
                 keep.append(t)
-            stride = h if m is None else m[2]
+            else:
+                stride = m[2]
         matrices.append(C.byref(_Matrix(t.data_ptr(), stride)))
     S, ptr = 0, None
     if seq_ptr is not None:

@@ -284,6 +284,9 @@ def test_refusals():
     ptr = torch.tensor([0, 8], dtype=torch.int32, device=DEV)
     norm, grad = cel.residual_norm, cel.residual_norm_grad
     refused(norm, f[0], x, pre)
+    refused(norm, f, None, pre)
+    refused(norm, "f", x, pre)
+    refused(norm, f, x, 1.0)
     refused(norm, f, x[:7], pre)
     refused(norm, f, x.half(), pre)
     refused(norm, f.float(), x, pre)
