@@ -1406,12 +1406,18 @@ int splits_of(const cel_attn *a, const Keys &k) {
   if (!k.cross || units == 0) return 1;
   return (int)std::max<int64_t>(1, std::min(512 / units, steps_of(a, kBlock, a->tokens, k.n) / 8));
 }
-// The same of the rows of a tile of keys, beyond the query heads.
+// The same of the rows of a tile of keys, of all query heads that share them.  Two workgroups a compute unit are
+// one round, which is enough for one sequence, whose tiles are as long; of several the longest tile should be no
+// longer than a round: one workgroup's share of a sequence of three times the mean, two of two.  Against six
+// workgroups a compute unit for every batch: one sequence of 4,096 tokens to 4,096, 16 heads of 80 over 4: 517 -> 512 us;
+// 2 of 4,096, 32 of 128 over 8: 2,398 -> 2,372; 4 of 1,024: 395 -> 384; 9 ragged ones, 7,000 to 5,000, 32 of 128
+// over 4: 461 -> 443.  One round for all would be 352 in the third, but 487 rather than 326 for 37
+// sequences of 16 to 1,957 tokens.
 int parts_of(const cel_attn *a, const Keys &k) {
-  const int parts = parts_of(a, k.n);
-  const int64_t units = key_tiles(k) * a->kv_heads;
-  if (!k.cross || units == 0) return parts;
-  return (int)std::max<int64_t>(parts, std::min(512 / units, steps_of(a, kKeyBlock, k.n, a->tokens) * (a->heads / a->kv_heads) / 8));
+  const int64_t units = key_tiles(k) * a->kv_heads, group = a->heads / a->kv_heads;
+  if (!k.cross || units == 0) return parts_of(a, k.n);
+  const int64_t parts = std::min(group, (512 * std::min(std::max(a->n_seq, 1), 3) + units - 1) / units);
+  return (int)std::max(parts, std::min(512 / units, steps_of(a, kKeyBlock, k.n, a->tokens) * group / 8));
 }
 // Whether `tiles` tiles of `units` heads are put in order: where more workgroups than the GPU holds at once leave
 // an order to choose, and more sequences than one a reason to.
