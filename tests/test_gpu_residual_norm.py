@@ -215,6 +215,25 @@ def test_strides_and_copies():
         assert torch.equal(dx, plain[2]) and torch.equal(df, plain[3]) and all(torch.equal(grads[n], plain[4][n]) for n in grads)
 
 
+@pytest.mark.parametrize("types", [(bf16, bf16, bf16), (f16, f32, f32)])
+@pytest.mark.parametrize("h", [5, 61, 120, 2049])
+def test_vectors_that_begin_anywhere(h, types):
+    """At any multiple of their type's size, beside other values."""
+    f, x, dy, dz, v = make(33, h, types, post=True, gate=True, bias=True, seqs=[0, 10, 31])
+    plain = check(f, x, dy, dz, v, p=0.1)
+    for first in (1, 3):
+        w = dict(v)
+        for n, t in v.items():
+            if n != "seq_ptr":
+                at = torch.full((t.numel() + first + 9,), float("nan"), dtype=t.dtype, device=DEV)
+                w[n] = at[first:first + t.numel()].view(t.shape)
+                w[n].copy_(t)
+        y, z = cel.residual_norm(f, x, **w, p=0.1)
+        assert torch.equal(y, plain[0]) and torch.equal(z, plain[1])
+        dx, df, grads = cel.residual_norm_grad(dy, dz, f, y, **w, p=0.1)
+        assert torch.equal(dx, plain[2]) and torch.equal(df, plain[3]) and all(torch.equal(grads[n], plain[4][n]) for n in grads)
+
+
 def test_the_same_inputs_give_the_same_bits():
     f, x, dy, dz, v = make(5000, 264, post=True, gate=True, bias=True, seqs=[0, 700, 702, 4000, 5000])
     a, b = (cel.residual_norm_grad(dy, dz, f, x, **v, p=0.1) for _ in range(2))
