@@ -1233,14 +1233,16 @@ __global__ void __launch_bounds__(256) k_attention_unite(AttnArgs A) {
     for (int p = 0; p < A.splits; p++) m = fmaxf(m, stats[p * rows][0]);
     for (int p = 0; p < A.splits; p++) {
       const f32x2 x = stats[p * rows];
-      if (x[0] == -INFINITY) continue;  // a share without a key that the row sees
-      const float w = exp2_((x[0] - m) * scale);
+      // A share without a maximum has no key that the row sees, and sums of 0; or only scores of minus infinity or
+      // that are no numbers, and the sums tell: 0 times what is no number stays that.
+      const float w = x[0] == -INFINITY ? 0.f : exp2_((x[0] - m) * scale);
       l += x[1] * w;
       sum += *reinterpret_cast<const acc4 *>(A.split + (p * rows + row) * A.d + c) * w;
     }
-    by = stats[0][1] < 0.f ? 0.f : 1.f / l;
-    if (by == 0.f) sum = acc4{0, 0, 0, 0};
-    if (c == 0) A.lse[row] = m == -INFINITY ? -INFINITY : (m * scale + __builtin_amdgcn_logf(l)) * kLn2;
+    const bool real = !(stats[0][1] < 0.f);
+    by = real ? 1.f / l : 0.f;
+    if (!real) sum = acc4{0, 0, 0, 0};
+    if (c == 0) A.lse[row] = real ? ((m == -INFINITY ? 0.f : m * scale) + __builtin_amdgcn_logf(l)) * kLn2 : -INFINITY;
   }
   const Rows &x = DQ ? A.dq : A.out;
   *reinterpret_cast<u32x2 *>(x.p + 2 * ((int64_t)i * x.row + (int64_t)head * x.head + c)) =

@@ -126,6 +126,45 @@ def test_infinities_and_nan_where_keys_are_shared(dtype):
     assert torch.equal(got["lse"][:, :3], plain["lse"][:, :3]) and bool(torch.isnan(got["out"][3:]).any())
 
 
+@pytest.mark.parametrize("dtype,H,K,d", [(torch.bfloat16, 2, 1, 64), (torch.float16, 4, 4, 128), (torch.bfloat16, 16, 4, 40)])
+def test_no_numbers_in_all_that_a_row_sees_of_a_share(dtype, H, K, d):
+    """Each row's keys are 2,753 and 2,747, dealt out 512 or more to a workgroup: of a share, the first three rows
+    see key 2,752 alone (where 86 tiles are shared by ten), or all keys are no numbers.  A weight that is no number
+    makes the row's result none, as for few keys."""
+    lengths, sources = [3, 2], [2753, 2747]
+    p, kp = ptr_of(lengths), ptr_of(sources)
+    q, k, v, g = batch(5, 5500, H, K, d, dtype, 8)
+    plain = run(q, k, v, g, p, kp)
+    for keys in (slice(2752, 2753), slice(0, 2753), slice(512, 1600), slice(1000, 1001)):
+        bad = k.clone()
+        bad[keys] = math.nan
+        got = run(q, bad, v, g, p, kp)
+        for n in ("out", "dq"):
+            assert bool(torch.isnan(got[n][:3]).all()) and torch.equal(got[n][3:], plain[n][3:]), (keys, n)
+        assert bool(torch.isnan(got["lse"][:, :3]).all()) and torch.equal(got["lse"][:, 3:], plain["lse"][:, 3:]), keys
+        for n in ("dk", "dv"):
+            assert bool(torch.isnan(got[n][:2753]).all()) and torch.equal(got[n][2753:], plain[n][2753:]), (keys, n)
+
+
+@pytest.mark.parametrize("U", [60, 700, 16384])
+def test_one_token_and_no_numbers(U):
+    """The same pattern however many keys there are, and so workgroups that share them."""
+    q, k, v, g = batch(1, U, 2, 1, 64, torch.bfloat16, U)
+    p, kp = ptr_of([1]), ptr_of([U])
+    bad = k.clone()
+    bad[U // 3:2 * U // 3] = math.nan
+    out, lse = cel.cross_attention(q, bad, v, p, kp)
+    assert bool(torch.isnan(out).all()) and bool(torch.isnan(lse).all())
+    out, lse = cel.cross_attention(q * math.nan, k, v, p, kp)
+    assert bool(torch.isnan(out).all()) and bool(torch.isnan(lse).all())
+    # keys of weight 0 with infinite values: 0 times infinity
+    q[:], low, wide = 1.0, k.clone(), v.clone()
+    low[U // 3:2 * U // 3], wide[U // 2, :, 5] = -math.inf, math.inf
+    out, lse = cel.cross_attention(q, low, wide, p, kp)
+    assert bool(torch.isnan(out[..., 5]).all()) and bool(torch.isfinite(out[..., :5]).all()) and bool(torch.isfinite(out[..., 6:]).all())
+    assert bool(torch.isfinite(lse).all())
+
+
 def test_scores_of_minus_infinity():
     """A row all of whose scores are minus infinity has no weights (0 / 0), whether its keys are shared or not; one
     with another score has that one's alone."""
