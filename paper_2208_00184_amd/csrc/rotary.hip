@@ -31,12 +31,16 @@ struct RotArgs {
   float sign;
 };
 
+// In a cosine's place: the pair has no axis and is copied, not turned by 0, which would make an
+// infinity's partner no number.
+constexpr float kStays = 2.f;
+
 // Sine and cosine of pair p's angle at token t.  With the product's and the
 // factor's rest the turns are exact to 2^-52 of one up to positions of 2^53.
 __device__ inline void angle(const RotArgs &A, int p, int t, float &c, float &s) {
 #pragma clang fp contract(off)  // n is the rounded product: low is what that lacks
   const int axis = A.axes ? A.axes[p] : 0;
-  c = 1.f, s = 0.f;
+  c = kStays, s = 0.f;
   if (axis < 0 || axis >= A.n_axes) return;
   const int64_t at = axis * A.axis_stride + t;
   const double pos = A.wide_positions ? (double)static_cast<const int64_t *>(A.positions)[at] : (double)static_cast<const int32_t *>(A.positions)[at];
@@ -102,29 +106,36 @@ __global__ void __launch_bounds__(kThreads) k_rotary(RotArgs A) {
     }
     if (!in) continue;
     float c[8], s[8];
+    bool all = turns;  // whether every pair of the eight turns
 #pragma unroll
     for (int e = 0; e < 8; e++) {
       c[e] = 1.f, s[e] = 0.f;
       if (turns && 8 * (int)j + e < A.P) {
         const float2 y = s_angle[t * A.P + 8 * j + e];
         c[e] = y.x, s[e] = y.y;
+        all = all && y.x != kStays;
       }
     }
+    // pair e: (u[e], v[e]), or the neighbours 2 e and 2 e + 1 of the sixteen
+    auto turn = [&](float (&u)[8], float (&v)[8], int e) {
+      float &p = PAIRS ? (e < 4 ? u[2 * e & 7] : v[2 * e & 7]) : u[e];
+      float &q = PAIRS ? (e < 4 ? u[(2 * e + 1) & 7] : v[(2 * e + 1) & 7]) : v[e];
+      const float p0 = p, q0 = q;
+      p = p0 * c[e] - q0 * s[e];
+      q = q0 * c[e] + p0 * s[e];
+    };
     for (int h = h0; h < A.H; h += A.share) {
       if (h > (int)h0) load(h);
       float u[8], v[8];
       values<T>(u, ra);
       values<T>(v, rb);
-      if (turns) {
+      if (all) {
 #pragma unroll
-        for (int e = 0; e < 8; e++) {
-          // pair e: (u[e], v[e]), or the neighbours 2 e and 2 e + 1 of the sixteen
-          float &p = PAIRS ? (e < 4 ? u[2 * e & 7] : v[2 * e & 7]) : u[e];
-          float &q = PAIRS ? (e < 4 ? u[(2 * e + 1) & 7] : v[(2 * e + 1) & 7]) : v[e];
-          const float p0 = p, q0 = q;
-          p = p0 * c[e] - q0 * s[e];
-          q = q0 * c[e] + p0 * s[e];
-        }
+        for (int e = 0; e < 8; e++) turn(u, v, e);
+      } else if (turns) {
+#pragma unroll
+        for (int e = 0; e < 8; e++)
+          if (c[e] != kStays) turn(u, v, e);
       }
       store_eight(out + h * A.out_head + a, u, left_a);
       store_eight(out + h * A.out_head + b, v, left_b);

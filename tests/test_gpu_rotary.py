@@ -81,6 +81,34 @@ def test_axes_that_do_not_exist():
     assert torch.equal(got[..., [2, 10]], x[..., [2, 10]])
 
 
+@pytest.mark.parametrize("pairs", [False, True])
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("d,P", [(64, 32), (40, 13), (7, 3), (256, 128)])
+def test_pairs_without_an_axis_keep_their_bits(d, P, dtype, pairs):
+    """Whatever their other value is: infinities, NaN, and the sign of zero."""
+    x = randn(29, 3, d, seed=d)
+    for n, odd in enumerate((float("inf"), float("nan"), -float("inf"), -0.0, 0.0)):
+        x.flatten()[n::7] = odd
+    x = x.to(dtype).to(DEV)
+    axes = torch.tensor([(-1, 0, 2, 1, 2 ** 31 - 1)[p % 5] for p in range(P)], dtype=torch.int32, device=DEV)
+    positions = torch.arange(58, device=DEV).view(2, 29)
+    still = torch.zeros(d, dtype=torch.bool, device=DEV)
+    for p in range(P):
+        if p % 5 in (0, 2, 4):
+            still[[2 * p, 2 * p + 1] if pairs else [p, p + P]] = True
+    still[2 * P:] = True
+    bits = {2: torch.int16, 4: torch.int32}[x.element_size()]
+    for f in (cel.rotary, cel.rotary_grad):
+        got = f(x, positions, freqs_of(P), axes=axes, pairs=pairs)
+        assert torch.equal(got[..., still].view(bits), x[..., still].view(bits))
+        clean = f(x.nan_to_num(0.0, 0.0, 0.0), positions, freqs_of(P), axes=axes, pairs=pairs)
+        both = torch.isfinite(got) & torch.isfinite(x)
+        assert torch.equal(got[both], clean[both])  # the others turn as ever
+        again = x.clone()
+        f(again, positions, freqs_of(P), axes=axes, pairs=pairs, out=again)
+        assert torch.equal(again.view(bits), got.view(bits))
+
+
 @pytest.mark.parametrize("far", [2 ** 20, 2 ** 31 - 64, 2 ** 40, 2 ** 52, -2 ** 45])
 def test_far_positions(far):
     """Against angles of numpy's long doubles (64 bits of fraction): at 2^52 a product in 64 bits alone is off by half a turn."""
