@@ -554,7 +554,8 @@ typedef struct {
 } cel_norm_args;
 
 /* Everything is in 32 bits up to the one rounding of y and of z, which
- * is the norm of y before its rounding.
+ * is the norm of y before its rounding.  A row whose sum of squares 32 bits do
+ * not hold (values of some 10^17 and more) has a norm of 0, here and in the gradient.
  * Inputs: f, or NULL: z is the norm of x (no post, gate or dropout, scale 1,
  * y is not written); x.  Outputs: y; z where there is pre.  They share no
  * memory with an input nor each other.  Strides >= hidden.

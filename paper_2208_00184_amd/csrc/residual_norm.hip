@@ -478,7 +478,7 @@ __global__ void __launch_bounds__(64 * kWidest) k_residual_norm_grad(NormArgs A)
       if (branch && A.post) EACH(u, e) q[2] = fmaf(f.v[u][e], f.v[u][e], q[2]);
       if (A.pre || (branch && A.post)) sum(q);
       if (A.pre) {
-        const float r = rsqrtf(q[0] * over + A.eps), k = q[1] * over * r, b = m[1] * r;
+        const float r = rsqrtf(q[0] * over + A.eps), k = r == 0.f ? 0.f : q[1] * over * r, b = m[1] * r;
         EACH(u, e) y.v[u][e] *= r;
         if (real) {  // a row that is not there may have no norm
           EACH(u, e) {
@@ -507,11 +507,12 @@ __global__ void __launch_bounds__(64 * kWidest) k_residual_norm_grad(NormArgs A)
         if (real) dy.template store<T>(A.z, t * A.z_row, c);
         continue;
       }
-      // From here on dy is t where the mask keeps it, times the mask's factor and r: r is in every product that follows but
-      // one, so that f need not be multiplied by it.
+      // From here on dy is t where the mask keeps it, times the mask's factor and, without biases, r, which is in every product
+      // that follows but one, so that f need not be multiplied by it.  dpost_bias has no r, and to divide by it is no way
+      // back where f's squares pass 32 bits and r is 0: with biases f becomes N.
       const float r = branch && A.post ? rsqrtf(q[2] * over + A.eps) : 1.f;
       if (mask.least) {
-        const float by = mask.by * r;
+        const float by = bias ? mask.by : mask.by * r;
 #pragma unroll
         for (int u = 0; u < C; u++) {
           bool k[8];
@@ -521,9 +522,10 @@ __global__ void __launch_bounds__(64 * kWidest) k_residual_norm_grad(NormArgs A)
 #pragma unroll
           for (int e = 0; e < 8; e++) dy.v[u][e] = k[e] ? dy.v[u][e] * by : 0.f;
         }
-      } else if (branch && A.post) {
+      } else if (!bias && branch && A.post) {
         EACH(u, e) dy.v[u][e] *= r;
       }
+      if (bias && branch && A.post) EACH(u, e) f.v[u][e] *= r;
       if (branch && A.gate) {
         if (A.post) {
           vectors.get(g, kPost, c);
@@ -531,7 +533,7 @@ __global__ void __launch_bounds__(64 * kWidest) k_residual_norm_grad(NormArgs A)
           if (bias && A.post_bias) {
             Row<C> b;
             vectors.get(b, kPostBias, c);
-            EACH(u, e) g.v[u][e] = fmaf(b.v[u][e], 1.f / r, g.v[u][e]);
+            EACH(u, e) g.v[u][e] += b.v[u][e];
           }
           if (real) EACH(u, e) d_gate.v[u][e] = fmaf(dy.v[u][e], g.v[u][e], d_gate.v[u][e]);
         } else if (real) {
@@ -543,7 +545,7 @@ __global__ void __launch_bounds__(64 * kWidest) k_residual_norm_grad(NormArgs A)
       if (branch && A.post) {
         if (real) {
           EACH(u, e) d_post.v[u][e] = fmaf(dy.v[u][e], f.v[u][e], d_post.v[u][e]);
-          if (bias && A.post_bias) EACH(u, e) d_post_bias.v[u][e] = fmaf(dy.v[u][e], 1.f / r, d_post_bias.v[u][e]);
+          if (bias && A.post_bias) EACH(u, e) d_post_bias.v[u][e] += dy.v[u][e];
         }
         vectors.get(g, kPost, c);
         float p[1] = {0.f};
@@ -560,8 +562,9 @@ __global__ void __launch_bounds__(64 * kWidest) k_residual_norm_grad(NormArgs A)
         } else {
           sum(p);
         }
-        p[0] *= over * r * r;
+        p[0] *= bias ? over : over * r * r;
         EACH(u, e) dy.v[u][e] = fmaf(f.v[u][e], -p[0], dy.v[u][e]);
+        if (bias) EACH(u, e) dy.v[u][e] *= r;
       }
       if (real) dy.template store<T>(A.z, t * A.z_row, c);
     }

@@ -195,6 +195,43 @@ def test_infinities_stay_in_their_row():
     assert torch.equal(dx[rows], dx1[rows]) and torch.equal(df[rows], df1[rows])
 
 
+@pytest.mark.parametrize("types", [(bf16, bf16, bf16), (bf16, f32, f32), (f32, f32, f32)])
+@pytest.mark.parametrize("h", [200, 2049, 9000])
+@pytest.mark.parametrize("center", [False, True])
+@pytest.mark.parametrize("p", [0.0, 0.2])
+def test_rows_whose_squares_32_bits_do_not_hold(types, h, center, p):
+    """A row of finite values with a sum of squares beyond 2^128 has a norm of 0: what it gives to sums is what a row of
+    zeros gives, and nothing of it is no number."""
+    f, x, dy, dz, v = make(24, h, types, post=True, gate=True, bias=True, seed=h)
+    f[3] = 0.0
+    zero = f.clone()
+    f[3, 0::2], f[3, 1::2] = 3e19, -3e19
+    if h % 2:
+        f[3, -1] = 0.0
+    how = dict(p=p, seed=5, center=center)
+    y, z = cel.residual_norm(zero, x, **v, **how)
+    assert all(torch.equal(a, b) for a, b in zip(cel.residual_norm(f, x, **v, **how), (y, z)))
+    got, want = (cel.residual_norm_grad(dy, dz, t, y, **v, **how) for t in (f, zero))
+    rows = torch.arange(24, device=DEV) != 3
+    assert torch.equal(got[0], want[0]) and torch.equal(got[1][rows], want[1][rows]) and not bool(got[1][3].any())
+    assert all(torch.equal(got[2][n], want[2][n]) for n in want[2]), {n: bool(torch.isnan(g).any()) for n, g in got[2].items()}
+
+
+@pytest.mark.parametrize("h", [200, 2049])
+def test_a_stream_whose_squares_32_bits_do_not_hold(h):
+    """The same of the norm before the next block, with gradients whose products with the row 32 bits do not hold either."""
+    f, x, dy, dz, v = make(24, h, (f32, f32, f32), bias=True, seed=h)
+    x[3] = 3e19
+    dz[3] = 2e19
+    y, z = cel.residual_norm(None, x, v["pre"], pre_bias=v["pre_bias"])
+    assert torch.equal(z[3], v["pre_bias"])
+    dx, _, grads = cel.residual_norm_grad(dy, dz, None, y, v["pre"], pre_bias=v["pre_bias"])
+    assert torch.equal(dx[3], dy[3])
+    dz[3] = 0.0
+    _, _, less = cel.residual_norm_grad(dy, dz, None, y, v["pre"], pre_bias=v["pre_bias"])
+    assert torch.equal(grads["pre"], less["pre"])
+
+
 def test_strides_and_copies():
     f, x, dy, dz, v = make(30, 120, post=True, gate=True, bias=True)
     plain = check(f, x, dy, dz, v, p=0.1)
