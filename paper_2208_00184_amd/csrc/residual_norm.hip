@@ -507,12 +507,10 @@ __global__ void __launch_bounds__(64 * kWidest) k_residual_norm_grad(NormArgs A)
         if (real) dy.template store<T>(A.z, t * A.z_row, c);
         continue;
       }
-      // From here on dy is t where the mask keeps it, times the mask's factor and, without biases, r, which is in every product
-      // that follows but one, so that f need not be multiplied by it.  dpost_bias has no r, and to divide by it is no way
-      // back where f's squares pass 32 bits and r is 0: with biases f becomes N.
+      // f becomes N: with r in dy instead, the products that lack one of the two would have to be divided by it, or
+      // pass 32 bits where r is 0 for a row whose squares did.
       const float r = branch && A.post ? rsqrtf(q[2] * over + A.eps) : 1.f;
       if (mask.least) {
-        const float by = bias ? mask.by : mask.by * r;
 #pragma unroll
         for (int u = 0; u < C; u++) {
           bool k[8];
@@ -520,12 +518,10 @@ __global__ void __launch_bounds__(64 * kWidest) k_residual_norm_grad(NormArgs A)
           asm volatile("" : "+s"(mask.k0), "+s"(mask.k1));
           mask.kept(k, c[u].at >> 3, (uint32_t)t);
 #pragma unroll
-          for (int e = 0; e < 8; e++) dy.v[u][e] = k[e] ? dy.v[u][e] * by : 0.f;
+          for (int e = 0; e < 8; e++) dy.v[u][e] = k[e] ? dy.v[u][e] * mask.by : 0.f;
         }
-      } else if (!bias && branch && A.post) {
-        EACH(u, e) dy.v[u][e] *= r;
       }
-      if (bias && branch && A.post) EACH(u, e) f.v[u][e] *= r;
+      if (branch && A.post) EACH(u, e) f.v[u][e] *= r;
       if (branch && A.gate) {
         if (A.post) {
           vectors.get(g, kPost, c);
@@ -562,9 +558,8 @@ __global__ void __launch_bounds__(64 * kWidest) k_residual_norm_grad(NormArgs A)
         } else {
           sum(p);
         }
-        p[0] *= bias ? over : over * r * r;
-        EACH(u, e) dy.v[u][e] = fmaf(f.v[u][e], -p[0], dy.v[u][e]);
-        if (bias) EACH(u, e) dy.v[u][e] *= r;
+        p[0] *= over;
+        EACH(u, e) dy.v[u][e] = fmaf(f.v[u][e], -p[0], dy.v[u][e]) * r;
       }
       if (real) dy.template store<T>(A.z, t * A.z_row, c);
     }

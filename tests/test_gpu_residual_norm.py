@@ -217,6 +217,22 @@ def test_rows_whose_squares_32_bits_do_not_hold(types, h, center, p):
     assert all(torch.equal(got[2][n], want[2][n]) for n in want[2]), {n: bool(torch.isnan(g).any()) for n, g in got[2].items()}
 
 
+@pytest.mark.parametrize("h", [200, 2049, 9000])
+@pytest.mark.parametrize("p", [0.0, 0.2])
+def test_such_rows_beside_large_weights(h, p):
+    """Without biases, and where the row's values times the weights behind its norm pass 32 bits."""
+    f, x, dy, dz, v = make(24, h, (f32, f32, f32), post=True, gate=True, seed=h)
+    v["post"] = v["post"] * 16
+    f[3] = 0.0
+    zero = f.clone()
+    f[3, 0::2], f[3, 1::2] = 1e38, -1e38
+    y, z = cel.residual_norm(zero, x, **v, p=p, seed=5)
+    assert all(torch.equal(a, b) for a, b in zip(cel.residual_norm(f, x, **v, p=p, seed=5), (y, z)))
+    got, want = (cel.residual_norm_grad(dy, dz, t, y, **v, p=p, seed=5) for t in (f, zero))
+    assert all(torch.equal(got[2][n], want[2][n]) for n in want[2]), {n: bool(torch.isnan(g).any()) for n, g in got[2].items()}
+    assert not bool(got[1][3].any())
+
+
 @pytest.mark.parametrize("h", [200, 2049])
 def test_a_stream_whose_squares_32_bits_do_not_hold(h):
     """The same of the norm before the next block, with gradients whose products with the row 32 bits do not hold either."""
