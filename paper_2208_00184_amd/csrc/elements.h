@@ -107,6 +107,16 @@ struct Mask {
 #pragma unroll
     for (int e = 0; e < 8; e++) k[e] = (e & 1 ? x.w[e / 2] >> 16 : x.w[e / 2] & 0xffffu) >= least;
   }
+  // The conditions as bits, for later; x where condition e of them holds, else 0.
+  __device__ static uint32_t bits(const bool (&k)[8]) {
+    uint32_t b = 0;
+#pragma unroll
+    for (int e = 7; e >= 0; e--) b = b + b + k[e];
+    return b;
+  }
+  __device__ static float where(uint32_t b, int e, float x) {
+    return __uint_as_float(__float_as_uint(x) & (uint32_t)__builtin_amdgcn_sbfe((int)b, e, 1));
+  }
   // What is dropped becomes 0 whatever it was.
   __device__ void apply(float (&f)[8], const bool (&k)[8]) const {
 #pragma unroll

@@ -510,6 +510,9 @@ __global__ void __launch_bounds__(64 * kWidest) k_residual_norm_grad(NormArgs A)
       // f becomes N: with r in dy instead, the products that lack one of the two would have to be divided by it, or
       // pass 32 bits where r is 0 for a row whose squares did.
       const float r = branch && A.post ? rsqrtf(q[2] * over + A.eps) : 1.f;
+      // What the mask keeps, a bit each, since n and t times the gate are 0 where it drops, whatever they are; as conditions
+      // held so long they would fill the scalar registers.
+      uint32_t kept[C];
       if (mask.least) {
 #pragma unroll
         for (int u = 0; u < C; u++) {
@@ -517,8 +520,9 @@ __global__ void __launch_bounds__(64 * kWidest) k_residual_norm_grad(NormArgs A)
           // the ten rounds' keys are made anew for every row, beside the vector unit: twenty scalar registers less
           asm volatile("" : "+s"(mask.k0), "+s"(mask.k1));
           mask.kept(k, c[u].at >> 3, (uint32_t)t);
+          if (branch) kept[u] = Mask::bits(k);
 #pragma unroll
-          for (int e = 0; e < 8; e++) dy.v[u][e] = k[e] ? dy.v[u][e] * mask.by : 0.f;
+          for (int e = 0; e < 8; e++) dy.v[u][e] = branch || k[e] ? dy.v[u][e] * mask.by : 0.f;
         }
       }
       if (branch && A.post) EACH(u, e) f.v[u][e] *= r;
@@ -531,13 +535,15 @@ __global__ void __launch_bounds__(64 * kWidest) k_residual_norm_grad(NormArgs A)
             vectors.get(b, kPostBias, c);
             EACH(u, e) g.v[u][e] += b.v[u][e];
           }
-          if (real) EACH(u, e) d_gate.v[u][e] = fmaf(dy.v[u][e], g.v[u][e], d_gate.v[u][e]);
-        } else if (real) {
-          EACH(u, e) d_gate.v[u][e] = fmaf(dy.v[u][e], f.v[u][e], d_gate.v[u][e]);
+        } else {
+          g = f;
         }
+        if (mask.least) EACH(u, e) g.v[u][e] = Mask::where(kept[u], e, g.v[u][e]);
+        if (real) EACH(u, e) d_gate.v[u][e] = fmaf(dy.v[u][e], g.v[u][e], d_gate.v[u][e]);
         vectors.get(g, kGate, c);
         EACH(u, e) dy.v[u][e] *= g.v[u][e];
       }
+      if (branch && mask.least) EACH(u, e) dy.v[u][e] = Mask::where(kept[u], e, dy.v[u][e]);
       if (branch && A.post) {
         if (real) {
           EACH(u, e) d_post.v[u][e] = fmaf(dy.v[u][e], f.v[u][e], d_post.v[u][e]);

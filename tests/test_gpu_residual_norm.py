@@ -12,7 +12,7 @@ if not torch.cuda.is_available():  # collected on CPU, skipped there
     pytest.skip("needs a ROCm GPU", allow_module_level=True)
 
 import paper_2208_00184_amd as cel  # noqa: E402
-from block_reference import Joint, randn, within  # noqa: E402
+from block_reference import Joint, kept, randn, within  # noqa: E402
 
 DEV = "cuda:0"
 bf16, f16, f32 = torch.bfloat16, torch.float16, torch.float32
@@ -195,6 +195,52 @@ def test_infinities_stay_in_their_row():
     assert torch.equal(dx[rows], dx1[rows]) and torch.equal(df[rows], df1[rows])
 
 
+@pytest.mark.parametrize("types", TYPES)
+@pytest.mark.parametrize("h", [5, 200, 2049, 9000])
+@pytest.mark.parametrize("seqs", [None, [0, 3, 3, 20]])
+def test_no_numbers_where_the_mask_drops(types, h, seqs):
+    """A gate, dropout and no norm of f: what is dropped is as 0, whatever it was, in the gradients too."""
+    f, x, dy, dz, v = make(24, h, types, gate=True, seqs=seqs, seed=h)
+    keep, _ = kept(24, h, 0.3, 5, 2)
+    zero, bad = f.clone(), f.clone()
+    zero[~keep.to(DEV)] = 0.0
+    for n, x0 in enumerate((float("inf"), float("nan"), -float("inf"))):
+        some = ~keep & (torch.arange(24 * h).view(24, h) % 3 == n)
+        bad[some.to(DEV)] = x0
+    how = dict(p=0.3, seed=5, step=2, scale=0.5)
+    got, want = [], []
+    for to, t in ((got, bad), (want, zero)):
+        y, z = cel.residual_norm(t, x, **v, **how)
+        dx, df, grads = cel.residual_norm_grad(dy, dz, t, y, **v, **how)
+        to.extend([y, z, dx, df, *grads.values()])
+    assert all(bool(torch.isfinite(t).all()) for t in got) and all(torch.equal(a, b) for a, b in zip(got, want))
+
+
+@pytest.mark.parametrize("types", TYPES)
+@pytest.mark.parametrize("h", [200, 2049, 9000])
+@pytest.mark.parametrize("bias", [False, True])
+def test_a_dropped_infinity_before_the_norm(types, h, bias):
+    """Its row's norm is 0 but there, and what is dropped there gives nothing to the gate's gradient: the same sums as
+    of a row of zeros."""
+    f, x, dy, dz, v = make(24, h, types, post=True, gate=True, bias=bias, seed=h)
+    keep, _ = kept(24, h, 0.3, 5, 2)
+    at = int((~keep[7]).nonzero()[1])
+    f[7] = 0.0
+    zero = f.clone()
+    f[7, at] = float("inf")
+    how = dict(p=0.3, seed=5, step=2)
+    y, z = cel.residual_norm(zero, x, **v, **how)
+    got, want = (cel.residual_norm_grad(dy, dz, t, y, **v, **how) for t in (f, zero))
+    assert all(torch.equal(a, b) for a, b in zip(cel.residual_norm(f, x, **v, **how), (y, z)))
+    assert torch.equal(got[0], want[0])
+    for n in ("gate", "pre") + ("pre_bias", "post_bias") * bias:
+        assert torch.equal(got[2][n], want[2][n]), n
+    others = torch.arange(h, device=DEV) != at
+    assert torch.equal(got[2]["post"][others], want[2]["post"][others])
+    rows = torch.arange(24, device=DEV) != 7
+    assert torch.equal(got[1][rows], want[1][rows])
+
+
 @pytest.mark.parametrize("types", [(bf16, bf16, bf16), (bf16, f32, f32), (f32, f32, f32)])
 @pytest.mark.parametrize("h", [200, 2049, 9000])
 @pytest.mark.parametrize("center", [False, True])
@@ -246,6 +292,19 @@ def test_a_stream_whose_squares_32_bits_do_not_hold(h):
     dz[3] = 0.0
     _, _, less = cel.residual_norm_grad(dy, dz, None, y, v["pre"], pre_bias=v["pre_bias"])
     assert torch.equal(grads["pre"], less["pre"])
+
+
+@pytest.mark.parametrize("types", TYPES)
+@pytest.mark.parametrize("seqs", [None, [0, 3, 3, 20]])
+def test_infinite_gates_where_the_mask_drops(types, seqs):
+    f, x, dy, dz, v = make(24, 200, types, gate=True, seqs=seqs)
+    v["gate"][..., 11], v["gate"][..., 12] = float("inf"), float("nan")
+    keep, _ = kept(24, 200, 0.3, 5, 0)
+    _, df, _ = cel.residual_norm_grad(dy, dz, f, x, **v, p=0.3, seed=5)
+    assert not bool(df[~keep.to(DEV)].any())
+    there = keep[:, 11:13].to(DEV)
+    there[20 if seqs else 24:] = False  # rows of no sequence
+    assert not bool(torch.isfinite(df[:, 11:13][there]).any())
 
 
 def test_strides_and_copies():
