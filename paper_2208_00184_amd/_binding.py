@@ -1047,9 +1047,10 @@ def dropout(x, p, seed, step=0, out=None):
 _VECTORS = ("pre", "pre_bias", "post", "post_bias", "gate")
 
 
-def _norm(fn, tensors, vectors, seq_ptr, scale, p, seed, step, eps, center):
+def _norm(fn, tensors, vectors, seq_ptr, scale, p, seed, step, eps, center, kind=None):
     """-> (device, type of f, descriptor, matrices, tensors to keep alive): checks that residual_norm and
-    residual_norm_grad share.  tensors: (name, tensor or None, whether it is as the stream), the stream's own first."""
+    residual_norm_grad share.  tensors: (name, tensor or None, whether it is as the stream), the stream's own first; kind:
+    the type of f, if it is asked for."""
     name, stream, _ = tensors[0]
     given = {name: stream}
     like = None
@@ -1072,7 +1073,8 @@ def _norm(fn, tensors, vectors, seq_ptr, scale, p, seed, step, eps, center):
     T, h = shape
     if like is None and dtype == torch.float32:
         like = vectors[0]
-    kind = dtype if like is None else like.dtype
+    if kind is None:
+        kind = dtype if like is None else like.dtype
     if kind not in _TYPES or (dtype != kind and dtype != torch.float32):
         _refuse(f"{fn}: a stream in {dtype} beside blocks in {kind}")
     keep, matrices = [], []
@@ -1121,7 +1123,7 @@ def _norm(fn, tensors, vectors, seq_ptr, scale, p, seed, step, eps, center):
 
 
 def residual_norm(f, x, pre, post=None, gate=None, seq_ptr=None, pre_bias=None, post_bias=None, scale=1.0, p=0.0, seed=0, step=0,
-                  eps=1e-6, center=False):
+                  eps=1e-6, center=False, dtype=None):
     """The end of a block and the beginning of the next, in one pass:
 
         n = norm(f) * post + post_bias   (f itself without post)
@@ -1135,10 +1137,11 @@ def residual_norm(f, x, pre, post=None, gate=None, seq_ptr=None, pre_bias=None, 
     the rows seq_ptr[s] .. seq_ptr[s + 1] - 1; a row of no sequence has y = scale * x.  All vectors in one type, f's
     or float32.  The mask is that of dropout() for [rows, hidden].
     -> (y as x, z as f): the stream behind the block, and the next block's input (None without pre).  f = None: no
-    block yet, -> (x, norm(x) * pre + pre_bias)."""
+    block yet, -> (x, norm(x) * pre + pre_bias), the latter in dtype: x's type, or any of the three beside a float32 x,
+    with pre in the same or float32 (None: x's type, or pre's where x is float32)."""
     fn = "residual_norm"
     index, kind, a, (xm, fm), keep = _norm(fn, (("x", x, True), ("f", f, False)), (pre, pre_bias, post, post_bias, gate), seq_ptr,
-                                           scale, p, seed, step, eps, center)
+                                           scale, p, seed, step, eps, center, dtype)
     with _on(index):
         h = a.hidden
         y, z = x if f is None else _like(x, x.dtype), None if pre is None else _like(x, kind)

@@ -450,3 +450,36 @@ def test_refusals():
     refused(grad, dy.float(), dz, f, x, pre)
     refused(grad, dy, dz.float(), f, x, pre)
     refused(grad, dy, dz[:7], f, x, pre)
+
+
+def test_the_first_norms_type():
+    """A 32-bit stream and vectors beside blocks in 16 bits: the first norm, too, has the blocks' type where asked."""
+    for h in (7, 264, 9000):
+        f, x, dy, dz, v = make(33, h, (bf16, f32, f32), bias=True)
+        args = dict(pre_bias=v["pre_bias"], center=True)
+        y, wide = cel.residual_norm(None, x, v["pre"], **args)
+        assert wide.dtype == f32
+        for t in (bf16, f16, f32):
+            same, z = cel.residual_norm(None, x, v["pre"], dtype=t, **args)
+            assert same is x and z.dtype == t and torch.equal(z, wide.to(t))
+        for t in (bf16, f16):  # 16-bit vectors, as before, give their own
+            assert torch.equal(cel.residual_norm(None, x, v["pre"].to(t))[1], cel.residual_norm(None, x, v["pre"].to(t), dtype=t)[1])
+        joint = Joint(v["pre"], pre_bias=v["pre_bias"], center=True)
+        dx, df, grads = cel.residual_norm_grad(dy, dz, None, x, v["pre"], **args)
+        want = joint.backward(dy, dz, None, x)
+        within(dx, *want["dx"]), within(grads["pre"], *want["pre"]), within(grads["pre_bias"], *want["pre_bias"])
+        assert df is None
+
+    def refused(f, x, pre, **how):
+        with pytest.raises(cel.CelError) as e:
+            cel.residual_norm(f, x, pre, **how)
+        assert e.value.code == -1
+
+    f, x, _, _, v = make(8, 40, (bf16, f32, f32))
+    cel.residual_norm(f, x, v["pre"], dtype=bf16)
+    refused(f, x, v["pre"], dtype=f32)
+    refused(f, x, v["pre"], dtype=f16)
+    refused(None, x, v["pre"], dtype=torch.float64)
+    refused(None, x, v["pre"].half(), dtype=bf16)
+    refused(None, x.half(), v["pre"], dtype=bf16)
+    refused(None, x.half(), v["pre"], dtype=f32)
