@@ -193,7 +193,7 @@ def whole_step(rec, table, freqs, last, layers, ids, targets, states, seq_ptr, s
     x = rec.run("embed", lambda t, i: cel.embed(t, i, scale=c), table, ids)
     names = [(n, j) for n in range(len(layers)) for j in JOINTS]
     following = [layers[n][f"pre {j}"] for n, j in names[1:]] + [last]  # the norm behind each part
-    x, z = rec.run("norm", lambda x: cel.residual_norm(None, x, layers[0]["pre self"]), x)
+    x, z = rec.run("norm", lambda x, w: cel.residual_norm(None, x, w), x, layers[0]["pre self"])
     saved, first = [], x
     for (n, joint), after in zip(names, following):
         w = layers[n]
@@ -216,8 +216,8 @@ def whole_step(rec, table, freqs, last, layers, ids, targets, states, seq_ptr, s
             inner = rec.run(f"dropout {n}", lambda u: cel.dropout(torch.nn.functional.silu(u), drop, 1000 + n, step=step), u)
             kept = z, u
             f = rec.run(f"down {n}", mm, inner, w["down"])
-        x, z = rec.run(f"joint {joint} {n}", lambda f, x: cel.residual_norm(f, x, after, post=w[f"post {joint}"], gate=w[f"gate {joint}"],
-                                                                          **join(n, joint)), f, x)
+        x, z = rec.run(f"joint {joint} {n}", lambda f, x, after, post, gate: cel.residual_norm(f, x, after, post=post, gate=gate, **join(n, joint)),
+                       f, x, after, w[f"post {joint}"], w[f"gate {joint}"])
         saved.append((kept, inner, f, x))
 
     def loss_and_gradient(z, table):
@@ -231,9 +231,9 @@ def whole_step(rec, table, freqs, last, layers, ids, targets, states, seq_ptr, s
     dx, dstates, grads, vectors = None, torch.zeros_like(states), [{} for _ in layers], {}
     for (n, joint), after, (kept, inner, f, y) in reversed(list(zip(names, following, saved))):
         w, g = layers[n], grads[n]
-        how = dict(post=w[f"post {joint}"], gate=w[f"gate {joint}"], **join(n, joint))
         dx, df, dpre, g[f"post {joint}"], g[f"gate {joint}"] = rec.run(
-            f"joint' {joint} {n}", lambda *a: in_order(*cel.residual_norm_grad(*a, after, **how)), dx, dz, f, y)
+            f"joint' {joint} {n}", lambda *a: in_order(*cel.residual_norm_grad(*a, **join(n, joint))), dx, dz, f, y, after,
+            w[f"post {joint}"], w[f"gate {joint}"])
         vectors[n, joint] = dpre  # of the part behind this one
         out_weight, in_weight = dict(self=("out", "qkv"), cross=("cross", "query"), inner=("down", "up"))[joint]
         g[out_weight] = rec.run(f"{out_weight} weight' {n}", tmm, inner, df)
@@ -268,7 +268,7 @@ def whole_step(rec, table, freqs, last, layers, ids, targets, states, seq_ptr, s
             din = rec.run(f"dropout' {n}", lambda g, u: torch.ops.aten.silu_backward(cel.dropout(g, drop, 1000 + n, step=step), u), dinner, u)
         g[in_weight] = rec.run(f"{in_weight} weight' {n}", tmm, z, din)
         dz = rec.run(f"{in_weight}' {n}", mmt, din, w[in_weight])
-    dx, _, dpre, _, _ = rec.run("norm'", lambda *a: in_order(*cel.residual_norm_grad(*a[:2], None, a[2], layers[0]["pre self"])), dx, dz, first)
+    dx, _, dpre, _, _ = rec.run("norm'", lambda dx, dz, x, w: in_order(*cel.residual_norm_grad(dx, dz, None, x, w)), dx, dz, first, layers[0]["pre self"])
     for (n, joint), before in zip(names, [dpre] + [vectors[k] for k in names[:-1]]):
         grads[n][f"pre {joint}"] = before
     in_grad = rec.run("embed'", lambda g, i: cel.embed_grad(g, i, table.shape[0], scale=c, dtype=torch.float32), dx, ids)

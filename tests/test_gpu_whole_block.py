@@ -110,3 +110,12 @@ def test_the_step_runs_and_is_placed(example):
     # backwards 6, 8 and 6, then norm, embed and table
     assert wl.n == 3 + 2 * 16 + 2 + 2 * 14 + 3 + 2 * 20 + 3
     assert node_dev.shape[0] == wl.n and int(node_dev.max()) < 3 and int(wl.w.sum()) // 3 <= ms
+
+
+def test_every_source_is_read_by_an_operation(example):
+    """The vectors of the norms and gates among them: whoever reads one has an edge from it, forward and backward."""
+    _, wl, _, _ = example.main(
+        "--whole --blocks 2 --hidden 128 --heads 4 --kv-heads 2 --vocab 500 --tokens 300 --states 200 --sequences 5 --devices 3 --steps 1".split())
+    src, _ = wl.edges()
+    readers = [int((src == n).sum()) for n in range(3 + 2 * 16)]
+    assert min(readers) >= 1 and min(readers[3:]) >= 2, readers  # each weight and vector forward and backward
