@@ -1343,26 +1343,30 @@ void by_dim(int d, F f) {
 }
 template <class T, bool CROSS>
 void launch_attention(const AttnArgs &A, hipStream_t s) {
-  KTimer kt(s, "k_attention");
-  by_dim(A.d, [&](auto dp, auto dc) {
-    constexpr int DP = decltype(dp)::value, DC = decltype(dc)::value;
-    const dim3 grid(A.tiles * A.H, A.splits);
-    if (split_keys(A)) k_attention<T, DP, DC, 2, CROSS><<<grid, 2 * kWaves * 64, 0, s>>>(A);
-    else k_attention<T, DP, DC, 1, CROSS><<<grid, kWaves * 64, 0, s>>>(A);
-  });
+  {
+    KTimer kt(s, "k_attention");
+    by_dim(A.d, [&](auto dp, auto dc) {
+      constexpr int DP = decltype(dp)::value, DC = decltype(dc)::value;
+      const dim3 grid(A.tiles * A.H, A.splits);
+      if (split_keys(A)) k_attention<T, DP, DC, 2, CROSS><<<grid, 2 * kWaves * 64, 0, s>>>(A);
+      else k_attention<T, DP, DC, 1, CROSS><<<grid, kWaves * 64, 0, s>>>(A);
+    });
+  }
   if constexpr (CROSS) unite<T, false>(A, s);
 }
 template <class T, bool CROSS>
 void launch_dq(const AttnArgs &A, hipStream_t s) {
-  KTimer kt(s, "k_attention_dq");
-  by_dim(A.d, [&](auto dp, auto dc) {
-    constexpr int DP = decltype(dp)::value, DC = decltype(dc)::value;
-    const dim3 grid(A.tiles * A.H, A.splits);
-    if constexpr (DC <= 64) {  // beyond, two groups' dq does not fit in the registers (60 -> 126 us at 2,048 tokens)
-      if (split_keys(A)) return k_attention_dq<T, DP, DC, 2, CROSS><<<grid, 2 * kWaves * 64, 0, s>>>(A);
-    }
-    k_attention_dq<T, DP, DC, 1, CROSS><<<grid, kWaves * 64, 0, s>>>(A);
-  });
+  {
+    KTimer kt(s, "k_attention_dq");
+    by_dim(A.d, [&](auto dp, auto dc) {
+      constexpr int DP = decltype(dp)::value, DC = decltype(dc)::value;
+      const dim3 grid(A.tiles * A.H, A.splits);
+      if constexpr (DC <= 64) {  // beyond, two groups' dq does not fit in the registers (60 -> 126 us at 2,048 tokens)
+        if (split_keys(A)) return k_attention_dq<T, DP, DC, 2, CROSS><<<grid, 2 * kWaves * 64, 0, s>>>(A);
+      }
+      k_attention_dq<T, DP, DC, 1, CROSS><<<grid, kWaves * 64, 0, s>>>(A);
+    });
+  }
   if constexpr (CROSS) unite<T, true>(A, s);
 }
 template <class T, bool CROSS>

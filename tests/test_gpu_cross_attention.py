@@ -274,6 +274,30 @@ def test_inside_a_graph():
         assert all(torch.equal(x, want[n]) for n, x in run(q, k, v, g, p, kp).items())
 
 
+def test_kernel_times_do_not_hold_each_other():
+    """Of one token on many states, whose keys are shared: the kernels' times together are no longer than the calls'."""
+    q, k, v, g = batch(1, 16384, 16, 4, 128, torch.bfloat16, 2)
+    p, kp = ptr_of([1]), ptr_of([16384])
+    run(q, k, v, g, p, kp)
+    torch.cuda.synchronize()
+    was = cel.timing(True)
+    try:
+        cel.kernel_stats(reset=True)
+        whole = 0.0
+        for _ in range(50):
+            a, b = torch.cuda.Event(enable_timing=True), torch.cuda.Event(enable_timing=True)
+            a.record()
+            run(q, k, v, g, p, kp)
+            b.record()
+            b.synchronize()
+            whole += a.elapsed_time(b)
+        stats = cel.kernel_stats(reset=True)
+    finally:
+        cel.timing(was)
+    assert stats["k_attention"][0] == stats["k_attention_dq"][0] == 50 and stats["k_attention_unite"][0] == 100
+    assert sum(ms for _, ms in stats.values()) <= whole
+
+
 def test_gradients_against_differences():
     """Of sums of float16 results at steps that 16 bits hold exactly: out's own roundings leave 2^-11 |out| of a value,
     independent ones, over the step; the second-order term is step^2 times the size of third derivatives."""
