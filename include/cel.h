@@ -586,7 +586,8 @@ int cel_residual_norm_grad(const cel_norm_args *a, const cel_matrix *dy, const c
                            const cel_matrix *y, void *scratch, const cel_matrix *dx, const cel_matrix *df,
                            const cel_norm_grads *g, hipStream_t stream);
 
-/* Bytes of scratch that cel_residual_norm_grad takes, or CEL_E_ARG. */
+/* Bytes of scratch that cel_residual_norm_grad takes, or CEL_E_ARG: five vectors in 32 bits for each of 256
+ * workgroups and, with seq_ptr, of n_seq sequences. */
 int64_t cel_residual_norm_grad_scratch(const cel_norm_args *a);
 
 /* Diagnostics: per-kernel device time.  After cel_timing(1), every call

@@ -1159,8 +1159,9 @@ __global__ void __launch_bounds__(256) k_attention_join(AttnArgs A) {
 // The tiles of rows (blockIdx.x = 0) and of keys (1) in the order of how many steps
 // they walk, the longest first: with lengths apart from each other on the two sides, how long a tile
 // takes does not follow from where it is, and a long one that starts at a launch's end is
-// waited for alone.  37 sequences of 16 to 1,957 tokens and 0 to 1,288 states, 24 heads of 80 over 4:
-// forward 107 -> 94 us, dq 137 -> 123, dk and dv 206 -> 160, for 5 us here.
+// waited for alone.  37 sequences of 16 to 1,957 tokens and 0 to 1,288 states, 24 heads of 80 over 4, between events:
+// forward 98 -> 79 us, dq 122 -> 101, dk and dv 186 -> 126, together 411 -> 328, for 5 us here, twice.  Lengths lie on
+// the device, so that a batch of equal ones pays too: two of 4,096, 32 heads of 128 over 8, 2,270 -> 2,277.
 constexpr int kOrderB = 1024, kOrderMost = 4096;  // threads; tiles that are ordered, at most
 __global__ void __launch_bounds__(kOrderB) k_attention_order(AttnArgs A) {
   __shared__ int s_at[kOrderB], s_sum[kOrderB / 64];
@@ -1214,7 +1215,8 @@ __global__ void __launch_bounds__(kOrderB) k_attention_order(AttnArgs A) {
 }
 
 // Rows of the forward pass (DQ: of dq) as the sums of the shares of their keys, in the keys' order,
-// the forward pass's over the largest of their maxima.
+// the forward pass's over the largest of their maxima.  Bound by latency: 32 shares of 16 rows of 128, 0.3 MB, in
+// 20 us forward, two loops of dependent loads.
 template <class T, bool DQ>
 __global__ void __launch_bounds__(256) k_attention_unite(AttnArgs A) {
   const int64_t rows = (int64_t)A.H * A.T, at = ((int64_t)blockIdx.x * 256 + threadIdx.x) * 4;
@@ -1327,7 +1329,10 @@ bool split_keys(const AttnArgs &A) { return A.splits == 1 && (int64_t)A.tiles * 
 // wide (a power of two, for the chunks' order), products run over DC dimensions, in
 // the steps of 16 or 32 that each has.  Heads of 65 to 80 (against 96 for them; the same
 // bits): 37 ragged sequences, 24 heads of 80 over 4, all three kernels: 397 -> 387 us, their
-// cross attention 332 -> 325; one of 4,096 to 4,096, 16 heads over 4: 535 -> 518.
+// cross attention 332 -> 325; one of 4,096 to 4,096, 16 heads over 4: 535 -> 518.  Heads of 33 to 48 and of 97 to 112
+// run as 64 and 128, though steps of 16 would win there too (that cross attention with heads of 48 262 -> 254 us, of 112
+// 411 -> 400; two sequences of 4,096, 32 heads over 8: 1,273 -> 1,176 and 2,301 -> 2,225): they are
+// some twenty kernels more for each of the two.
 template <class F>
 void by_dim(int d, F f) {
   typedef std::integral_constant<int, 32> c32;
@@ -1404,8 +1409,8 @@ int64_t steps_of(const cel_attn *a, int tile, int64_t n, int64_t m) {
 }
 // Into how many workgroups the keys of a tile of rows are dealt out where there are few rows: as many as give
 // every compute unit two, of eight steps at least, which win back the 4 us of uniting their sums.
-// One token of 16 heads of 128 over 4, 16,384 states: 205 -> 42 us; 16 sequences of one token and
-// 1,500 states each: 389 -> 43; with the gradient 300 tokens of 4 heads of 128 over 2, 8,000 states: 317 -> 94,
+// One token of 16 heads of 128 over 4, 16,384 states: 205 -> 33 us; 16 sequences of one token and
+// 1,500 states each: 389 -> 45; with the gradient 300 tokens of 4 heads of 128 over 2, 8,000 states: 317 -> 88,
 // and 8,000 tokens of 2 heads of 64 over 1, 300 states (whose rows are dealt out): 122 -> 52.
 int splits_of(const cel_attn *a, const Keys &k) {
   const int64_t units = row_tiles(a) * a->heads;

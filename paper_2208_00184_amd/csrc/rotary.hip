@@ -59,7 +59,8 @@ __device__ inline void angle(const RotArgs &A, int p, int t, float &c, float &s)
 // pairs and turns them in one head after the other.  Bound by memory: 4,096 tokens of 72 heads of 128,
 // 16 bits, in 28 us, 151 MB at 5.4 TB/s, part of them from the caches; 9,973 of 28 heads of 80 in 17 us.  With angles made
 // anew for every eight heads 42 and 39 us; with two, four or eight heads' loads on their way at once,
-// which takes registers from further waves, 29, 35 and 33 us, and 17, 21 and 24.
+// which takes registers from further waves, 29, 35 and 33 us, and 17, 21 and 24.  In 32 bits 57 us for 302 MB, with
+// neighbours as pairs 76: a thread's sixteen are 64 bytes then, and each of its loads takes 16 of every 64.
 template <class T, bool PAIRS>
 __global__ void __launch_bounds__(kThreads) k_rotary(RotArgs A) {
   extern __shared__ float2 s_angle[];  // [tokens][P]
