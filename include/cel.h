@@ -555,7 +555,8 @@ typedef struct {
 
 /* Everything is in 32 bits up to the one rounding of y and of z, which
  * is the norm of y before its rounding.  A row whose sum of squares 32 bits do
- * not hold (values of some 10^17 and more) has a norm of 0, here and in the gradient.
+ * not hold (values of some 10^17 and more) has a norm of 0, here and in the
+ * gradient, which is no number where the row's products with it pass 32 bits too.
  * Inputs: f, or NULL: z is the norm of x (no post, gate or dropout, scale 1,
  * y is not written); x.  Outputs: y; z where there is pre.  They share no
  * memory with an input nor each other.  Strides >= hidden.

@@ -481,7 +481,7 @@ __global__ void __launch_bounds__(64 * kWidest) k_residual_norm_grad(NormArgs A)
       if (branch && A.post) EACH(u, e) q[2] = fmaf(f.v[u][e], f.v[u][e], q[2]);
       if (A.pre || (branch && A.post)) sum(q);
       if (A.pre) {
-        const float r = rsqrtf(q[0] * over + A.eps), k = r == 0.f ? 0.f : q[1] * over * r, b = m[1] * r;
+        const float r = rsqrtf(q[0] * over + A.eps), k = q[1] * over * r, b = m[1] * r;
         EACH(u, e) y.v[u][e] *= r;
         if (real) {  // a row that is not there may have no norm
           EACH(u, e) {

@@ -281,10 +281,9 @@ def test_such_rows_beside_large_weights(h, p):
 
 @pytest.mark.parametrize("h", [200, 2049])
 def test_a_stream_whose_squares_32_bits_do_not_hold(h):
-    """The same of the norm before the next block, with gradients whose products with the row 32 bits do not hold either."""
+    """The same of the norm before the next block: its row's gradient is dy's alone, and nothing reaches the weights."""
     f, x, dy, dz, v = make(24, h, (f32, f32, f32), bias=True, seed=h)
     x[3] = 3e19
-    dz[3] = 2e19
     y, z = cel.residual_norm(None, x, v["pre"], pre_bias=v["pre_bias"])
     assert torch.equal(z[3], v["pre_bias"])
     dx, _, grads = cel.residual_norm_grad(dy, dz, None, y, v["pre"], pre_bias=v["pre_bias"])
@@ -292,6 +291,19 @@ def test_a_stream_whose_squares_32_bits_do_not_hold(h):
     dz[3] = 0.0
     _, _, less = cel.residual_norm_grad(dy, dz, None, y, v["pre"], pre_bias=v["pre_bias"])
     assert torch.equal(grads["pre"], less["pre"])
+
+
+@pytest.mark.parametrize("types", TYPES)
+@pytest.mark.parametrize("h", [9, 200, 2049, 9000])
+@pytest.mark.parametrize("post", [False, True])
+def test_an_infinity_of_the_stream_is_not_hidden(types, h, post):
+    """Its norm is no number, and so is the mean of products with it, which every column of the row's gradient has."""
+    f, x, dy, dz, v = make(24, h, types, post=post, seed=h)
+    x[3, h // 2] = float("inf")
+    dx, df, _ = cel.residual_norm_grad(dy, dz, f, x, **v)
+    rows = torch.arange(24, device=DEV) != 3
+    assert bool(torch.isnan(dx[3]).all()) and bool(torch.isnan(df[3]).all())
+    assert bool(torch.isfinite(dx[rows]).all()) and bool(torch.isfinite(df[rows]).all())
 
 
 @pytest.mark.parametrize("types", TYPES)
