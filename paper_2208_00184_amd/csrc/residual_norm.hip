@@ -315,8 +315,9 @@ __global__ void __launch_bounds__(64 * kWidest) k_residual_norm(NormArgs A) {
 }
 
 // The vectors that the gradient's rows need, where rows have need of the registers: in 32 bits in
-// LDS, each padded with zeros to whole eights; or of rows beyond 8,192 columns, whose vectors LDS does not hold, read anew.
+// LDS, each padded with zeros to whole eights and eight more, which lanes past the row's end read; or of rows beyond 8,192 columns, whose vectors LDS does not hold, read anew.
 enum { kPre, kPost, kGate, kPostBias };
+__host__ __device__ inline int padded_of(int h) { return ((h + 7) & ~7) + 8; }
 template <class T>
 struct Vectors {
   float *lds;
@@ -394,7 +395,7 @@ __global__ void __launch_bounds__(64 * kWidest) k_residual_norm_grad(NormArgs A)
   RowSum sum{s_red, wave, team, A.W, 0};
   Column c[C];
   columns_of(c, A, team);
-  const int padded = (A.h + 7) & ~7;
+  const int padded = padded_of(A.h);
   Vectors<T> vectors{s_dynamic, {A.pre, A.post, A.ptr ? nullptr : A.gate, A.post_bias}, A.wide, A.h, padded};
   float *const s_join = s_dynamic + (C == 1 ? vectors_of(KIND) * padded : 0);
   const int64_t first = blockIdx.x * A.per, last = min(A.T, first + A.per);
@@ -490,10 +491,8 @@ __global__ void __launch_bounds__(64 * kWidest) k_residual_norm_grad(NormArgs A)
           }
         }
         EACH(u, e) dy.v[u][e] = fmaf(fmaf(y.v[u][e], -k, g.v[u][e]), r, dy.v[u][e]);
-        if (A.center) {
-          EACH(u, e) dy.v[u][e] -= b;
-          dy.cut(c);
-        }
+        if (A.center) EACH(u, e) dy.v[u][e] -= b;
+        dy.cut(c);  // k may be no number, and a sum over the row follows
       }
       if (A.scale == 1.f) {
         if (real) dy.template store<R>(A.y, t * A.y_row, c);
@@ -784,7 +783,7 @@ extern "C" int cel_residual_norm_grad(const cel_norm_args *a, const cel_matrix *
     int rc = CEL_OK;
     by_type(a, s, [&](auto t, auto r, auto c, auto kind, auto narrow) {
       const auto kernel = k_residual_norm_grad<decltype(t), decltype(r), decltype(c)::value, decltype(kind)::value, decltype(narrow)::value>;
-      const int lds = 4 * ((s.C == 1 ? vectors_of(kind) * ((A.h + 7) & ~7) : 0) + (s.teams > 1 ? (kind & kBias ? 2 : 1) * s.teams * A.h : 0));
+      const int lds = 4 * ((s.C == 1 ? vectors_of(kind) * padded_of(A.h) : 0) + (s.teams > 1 ? (kind & kBias ? 2 : 1) * s.teams * A.h : 0));
       rc = [&]() -> int {
         if (lds > 65536) CEL_HIP(hipFuncSetAttribute(reinterpret_cast<const void *>(kernel), hipFuncAttributeMaxDynamicSharedMemorySize, lds));
         kernel<<<(unsigned)s.groups, 64 * s.W * s.teams, lds, st>>>(A);

@@ -319,6 +319,37 @@ def test_infinite_gates_where_the_mask_drops(types, seqs):
     assert not bool(torch.isfinite(df[:, 11:13][there]).any())
 
 
+@pytest.mark.parametrize("types", TYPES)
+@pytest.mark.parametrize("h", [9, 40, 200, 520, 1000, 3077])
+@pytest.mark.parametrize("seqs", [None, [0, 3, 3, 20]])
+def test_infinite_gates_at_the_rows_end(types, h, seqs):
+    """Behind a norm of f: where the mask drops the gate's column, the rest of the row's gradient is as with any gate."""
+    f, x, dy, dz, v = make(24, h, types, post=True, gate=True, seqs=seqs, seed=h)
+    keep, _ = kept(24, h, 0.5, 5, 0)
+    for at in {h - 1, h - 8, h - 9}:
+        row = ~keep[:, at]
+        if seqs:
+            row[20:] = False
+        want = cel.residual_norm_grad(dy, dz, f, x, **v, p=0.5, seed=5)[1][row.to(DEV)]
+        for value in (float("inf"), float("nan")):
+            w = dict(v, gate=v["gate"].clone())
+            w["gate"][..., at] = value
+            got = cel.residual_norm_grad(dy, dz, f, x, **w, p=0.5, seed=5)[1][row.to(DEV)]
+            assert row.any() and torch.equal(got, want), (at, value)
+
+
+@pytest.mark.parametrize("types", TYPES)
+@pytest.mark.parametrize("h", [3, 9, 17])
+def test_gradients_that_are_no_numbers_and_dropped(types, h):
+    """A row all of whose values the mask drops has df = 0, whatever reaches the stream's gradient."""
+    f, x, dy, dz, v = make(400, h, types, post=True, seed=h)
+    keep, _ = kept(400, h, 0.9, 5, 0)
+    rows = ~keep.any(1)
+    dz[:, 0] = float("inf")
+    _, df, _ = cel.residual_norm_grad(dy, dz, f, x, **v, p=0.9, seed=5)
+    assert int(rows.sum()) > 20 and not bool(df[rows.to(DEV)].any())
+
+
 def test_strides_and_copies():
     f, x, dy, dz, v = make(30, 120, post=True, gate=True, bias=True)
     plain = check(f, x, dy, dz, v, p=0.1)
