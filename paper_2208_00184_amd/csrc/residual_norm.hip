@@ -378,12 +378,12 @@ __device__ inline void leave_sums(Row<C> &one, float *to_one, Row<C> &two, float
 // g, then those with post e.  The next row's loads stand behind the last use of this one's, dy, dz and y before the second
 // half, so that both halves have some under way.
 // Bound by memory and these waits: 4,096 rows of 8,192 in 16 bits with both norms, gates and dropout 403 MB and 50 of sums in
-// 105 us (4.3 TB/s), 2 of them since f is multiplied by r, 2 since dropped products are chosen; without gate and second norm
+// 106 us (4.3 TB/s), 2 of them since f is multiplied by r, 2 since dropped products are chosen; without gate and second norm
 // 335 MB in 69 us.  Tried beside 101: dy, dz and y loaded at a row's beginning 112; all of a row's sums at once (those with
 // post e from the three parts of t), one barrier of two, 35 registers spilled, 133; 16 columns a lane, 8 waves, 127; 512 workgroups
 // 141, twice the sums to leave.  At 513 to 1,024 columns 16 a lane saved 1 to 3 % (8,192 rows of 1,000: 36.6 -> 35.6, forward
 // 16.3 -> 14.7) for a further instance of each kernel.  Beyond 8,192 columns a lane's 16 spill some 200 registers: 2,048 rows of
-// 16,384, 403 MB, in 325 us.
+// 16,384, 403 MB, in 336 us.
 template <class T, class R, int C, int KIND, bool NARROW>
 __global__ void __launch_bounds__(64 * kWidest) k_residual_norm_grad(NormArgs A) {
   extern __shared__ __align__(16) float s_dynamic[];
