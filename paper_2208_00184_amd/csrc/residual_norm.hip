@@ -315,7 +315,8 @@ __global__ void __launch_bounds__(64 * kWidest) k_residual_norm(NormArgs A) {
 }
 
 // The vectors that the gradient's rows need, where rows have need of the registers: in 32 bits in
-// LDS, each padded with zeros to whole eights and eight more, which lanes past the row's end read; or of rows beyond 8,192 columns, whose vectors LDS does not hold, read anew.
+// LDS, each padded with zeros to whole eights and eight more, which lanes past the row's end read; or of
+// rows beyond 8,192 columns, whose vectors LDS does not hold, read anew.
 enum { kPre, kPost, kGate, kPostBias };
 __host__ __device__ inline int padded_of(int h) { return ((h + 7) & ~7) + 8; }
 template <class T>
